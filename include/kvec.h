@@ -28,6 +28,15 @@
  *                     the consumer of the compacted cache: one decode token's
  *                     attention over the kept K/V (Sec. 4.1 keeps them for the
  *                     decoding phase).
+ *   kvec_prefill_attention
+ *                     the producer of those normalisers: a prompt's attention
+ *                     (causal, or a sliding window with sinks) and its row
+ *                     log-sum-exp.
+ *   kvec_paged_append, kvec_paged_decode, kvec_paged_evict
+ *                     the decoding phase over a paged cache: new tokens normed,
+ *                     rotated and written into it; one token's attention over
+ *                     it, which also accumulates the weight every slot
+ *                     receives; its eviction by that accumulated weight.
  *   kvec_score_lse, kvec_evict_model_lse
  *                     the same scores and step when the caller already holds
  *                     the softmax normaliser of every window row: K-VEC runs
@@ -356,6 +365,188 @@ kvec_status kvec_decode_attention_noalloc(const kvec_config* cfg,
                                           const void* k_cache, const void* v_cache,
                                           const int64_t cache_strides[2], int32_t n_ctx,
                                           const int32_t* idx, float* out, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * The prompt's attention
+ * ------------------------------------------------------------------------- */
+
+/* Shape of one attention over a prompt. */
+typedef struct kvec_attention_config {
+  int32_t batch;       /* sequences, 1..65535 */
+  int32_t n_kv_heads;  /* H, 1..1024 */
+  int32_t n_q_heads;   /* multiple of H; G = n_q_heads / H in 1..16 */
+  int32_t head_dim;    /* d in {64, 128} */
+  int32_t q_len;       /* query rows per sequence, 1..2^20 */
+  int32_t kv_len;      /* keys per sequence, 1..2^20 */
+  int32_t window;      /* keys a row sees, its own included; 0: all before it */
+  int32_t n_sinks;     /* >= 0: first keys that stay visible behind the window */
+  int32_t dtype;       /* kvec_dtype of q, k, v and out */
+} kvec_attention_config;
+
+/* Workspace bytes of kvec_prefill_attention (host-only; may be 0). */
+kvec_status kvec_prefill_workspace_size(const kvec_attention_config* cfg, size_t* bytes);
+
+/* Attention of a prompt, or of a chunk at its end, and the log-sum-exp of every
+ * row.  The rows of a sequence with nq query rows and nk keys are its last:
+ * row r stands at position p = nk - nq + r, and
+ *   out[b][j][r] = sum_t softmax_t(q_{b,j,r} . k_{b,h,t} / sqrt(d)) v_{b,h,t},
+ *   lse[b][j][r] = ln sum_t exp(q_{b,j,r} . k_{b,h,t} / sqrt(d)),  h = j / G,
+ * over the keys t <= p with t > p - window (window 0: every t <= p) or
+ * t < n_sinks.  A row that sees no key (nq > nk) gets zeros and lse = -inf.
+ *   q        device, cfg->dtype [batch][n_q_heads][q_len][d] (post-RoPE),
+ *            strides q_strides = {batch, head, row}.
+ *   k, v     device, cfg->dtype [batch][H][kv_len][d], strides {batch, head, t}.
+ *   q_lens, kv_lens
+ *            nullable device int32 [batch]: nq and nk of every sequence (null:
+ *            q_len and kv_len; values are taken into 0..q_len and 0..kv_len).
+ *            Rows r >= nq of out and lse are left as they are, keys t >= nk are
+ *            not read.
+ *   out      device out, cfg->dtype [batch][n_q_heads][q_len][d], strides
+ *            out_strides = {batch, head, row}; rounded once.
+ *   lse      nullable device out, fp32 [batch][n_q_heads][q_len], strides
+ *            lse_strides = {batch, head}, rows contiguous.  With window = 0 its
+ *            last O' rows are the lse of kvec_score_lse.
+ *   ws       device workspace of kvec_prefill_workspace_size() bytes (may be
+ *            null when that is 0).
+ * Softmax statistics and sums are fp32; with bf16 inputs the probabilities are
+ * rounded to bf16 for the product with V.  The keys below nk have to be finite:
+ * a NaN or infinity there can reach rows near it that do not see it.
+ * kv_len rows of the k or v stride must span less than 2 GiB, and batch *
+ * n_q_heads * q_len must be below 2^31 (else KVEC_ERR_UNSUPPORTED). */
+kvec_status kvec_prefill_attention(const kvec_attention_config* cfg,
+                                   const void* q, const int64_t q_strides[3],
+                                   const void* k, const int64_t k_strides[3],
+                                   const void* v, const int64_t v_strides[3],
+                                   const int32_t* q_lens, const int32_t* kv_lens,
+                                   void* out, const int64_t out_strides[3],
+                                   float* lse, const int64_t lse_strides[2],
+                                   void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * The decoding phase over a paged cache
+ *
+ * A cache is a pool of n_pages pages of page_size tokens for H KV heads, K and
+ * V pools with the same strides pool_strides = {page, head, row} in elements.
+ * Slot s of sequence b is row s % page_size of page
+ * page_table[b][s / page_size].  Heads may hold different tokens in one slot
+ * (the eviction is per head).  Beside K and V a slot may carry, per head,
+ *   acc  fp32  [n_pages][H][page_size]  the attention weight it has received
+ *   pos  int32 [n_pages][H][page_size]  the position of its token
+ * (both contiguous).  A page id outside 0..n_pages-1 is never followed: its
+ * slots are not visible, not written and not moved.  Pages that two sequences
+ * share may be read by both; kvec_paged_decode with acc and kvec_paged_evict
+ * need every page in one place of the table.  A contiguous cache
+ * [batch][H][capacity][d] is the paged one with page_size = capacity and one
+ * page per sequence.
+ * ------------------------------------------------------------------------- */
+
+typedef struct kvec_paged_config {
+  int32_t batch;       /* sequences, 1..65535 */
+  int32_t n_kv_heads;  /* H, 1..1024 */
+  int32_t n_q_heads;   /* multiple of H; G = n_q_heads / H in 1..16 */
+  int32_t head_dim;    /* d in {64, 128} */
+  int32_t page_size;   /* tokens per page, a multiple of 16 */
+  int32_t n_pages;     /* pages in the pool */
+  int32_t max_pages;   /* entries per row of the page table; times page_size <= 2^20 */
+  int32_t dtype;       /* kvec_dtype of q, k, v and the pools */
+} kvec_paged_config;
+
+/* New tokens of any sequences: queries and keys normed per head (optional),
+ * rotated by their position (optional), keys and values written into the pools.
+ * For every token n and head, over the head dimension:
+ *   y = x / sqrt(mean(x^2) + eps) * weight          (weight null: y = x)
+ *   (y_i, y_{i+R/2}) rotated by positions[n] * inv_freq[i], i < R/2
+ * (rotate-half over the first R = rot_dim dimensions, the others pass).
+ *   n_tokens   0 is a valid call that does nothing; at most 2^24.
+ *   q, k, v    device, cfg->dtype [n_tokens][n_q_heads or H][d], strides
+ *              {token, head}: three views of one projection's output will do.
+ *   q_weight, k_weight  nullable device, cfg->dtype [d].
+ *   eps        >= 0.
+ *   positions  device int32 [n_tokens].
+ *   inv_freq   device float64 [rot_dim / 2] (null only with rot_dim 0).  Angles are
+ *              computed in 64 bits, so far positions keep their precision.
+ *   rot_dim    R, a multiple of 16 in 0..d.
+ *   slots      device int64 [n_tokens]: page * page_size + row of the pool that
+ *              takes the token; one outside 0..n_pages*page_size-1 (-1 for the
+ *              padding of a batch) writes no key and no value.  Two tokens of
+ *              one call must not share a slot.
+ *   q_out      device out, cfg->dtype [n_tokens][n_q_heads][d], strides {token,
+ *              head}; may be q itself with q's strides.
+ *   k_pool, v_pool  device out, strides pool_strides.
+ *   acc, pos   nullable: set to 0 and to the token's position for every head.
+ * One rounding, at the end.  No workspace. */
+kvec_status kvec_paged_append(const kvec_paged_config* cfg, int32_t n_tokens,
+                              const void* q, const int64_t q_strides[2],
+                              const void* k, const int64_t k_strides[2],
+                              const void* v, const int64_t v_strides[2],
+                              const void* q_weight, const void* k_weight, float eps,
+                              const int32_t* positions, const double* inv_freq, int32_t rot_dim,
+                              const int64_t* slots,
+                              void* q_out, const int64_t q_out_strides[2],
+                              void* k_pool, void* v_pool, const int64_t pool_strides[3],
+                              float* acc, int32_t* pos, hipStream_t stream);
+
+/* Workspace bytes of kvec_paged_decode (host-only). */
+kvec_status kvec_paged_decode_workspace_size(const kvec_paged_config* cfg, int32_t max_len,
+                                             int32_t with_acc, size_t* bytes);
+
+/* One new token's attention over the paged cache (its key and value appended
+ * before).  For every sequence b of n = lens[b] slots and query head j:
+ *   out[b][j] = sum_s p_{j,s} v_{h,s},  p_{j,s} = softmax_s(q_j . k_{h,s} / sqrt(d)),
+ * h = j / G, over the slots s < n with s >= n - window (window 0: all) or
+ * s < n_sinks.  window and n_sinks count slots, so they are for a cache that
+ * keeps its tokens in order (kvec_paged_evict moves some).
+ *   q           device, cfg->dtype [batch][n_q_heads][d], strides {batch, head}.
+ *   page_table  device int32 [batch][max_pages].
+ *   lens        device int32 [batch] (taken into 0..max_len).
+ *   max_len     host bound of lens, 1..max_pages * page_size; sizes the work.
+ *   out         device out, fp32 [batch][n_q_heads][d], contiguous; zeros for a
+ *               sequence with no visible slot.
+ *   lse         nullable device out, fp32 [batch][n_q_heads]: ln of the softmax
+ *               normaliser (-inf with no visible slot).
+ *   acc         nullable device in/out: acc[s] += mean over the G query heads of
+ *               p_{j,s}, every visible slot (always the same bits: no atomics).
+ *   ws          device workspace of kvec_paged_decode_workspace_size() bytes.
+ * What masked and missing slots hold (NaN too) never matters. */
+kvec_status kvec_paged_decode(const kvec_paged_config* cfg,
+                              const void* q, const int64_t q_strides[2],
+                              const void* k_pool, const void* v_pool,
+                              const int64_t pool_strides[3],
+                              const int32_t* page_table, const int32_t* lens, int32_t max_len,
+                              int32_t window, int32_t n_sinks,
+                              float* out, float* lse, float* acc,
+                              void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Workspace bytes of kvec_paged_evict (host-only). */
+kvec_status kvec_paged_evict_workspace_size(const kvec_paged_config* cfg, int32_t max_len,
+                                            int32_t budget, size_t* bytes);
+
+/* Eviction of the paged cache by accumulated attention weight, in place.  Every
+ * head of a sequence with n = lens[b] > budget slots keeps `budget` of them:
+ * first the protected ones (position < n_sinks, or >= n_seen[b] - window), then
+ * by acc descending; ties go to the lower slot, NaN weights rank last.  Kept
+ * slots below the budget stay where they are; the i-th kept slot behind it, in
+ * ascending order, moves (K, V, acc, pos) to the i-th evicted slot below it.  So
+ * no more rows move than were evicted.  Other sequences keep everything.  Slots
+ * behind the budget are left as they are, their pages are free.
+ *   budget      slots kept per head, 1..2^20.
+ *   window, n_sinks   >= 0, window + n_sinks <= budget.
+ *   lens        device int32 [batch] (taken into 0..max_len).
+ *   n_seen      device int32 [batch]: tokens the sequence has seen, one more
+ *               than its newest position (may be lens when nothing was evicted).
+ *   max_len     as for kvec_paged_decode.
+ *   acc, pos    device in/out.
+ *   kept        nullable device out, int32 [batch][H][budget]: the slot that each
+ *               slot's content came from; -1 behind n.
+ *   lens_out    device out, int32 [batch]: min(n, budget); may be lens.
+ *   ws          device workspace of kvec_paged_evict_workspace_size() bytes. */
+kvec_status kvec_paged_evict(const kvec_paged_config* cfg, int32_t budget,
+                             int32_t window, int32_t n_sinks,
+                             void* k_pool, void* v_pool, const int64_t pool_strides[3],
+                             const int32_t* page_table, const int32_t* lens,
+                             const int32_t* n_seen, int32_t max_len,
+                             float* acc, int32_t* pos, int32_t* kept, int32_t* lens_out,
+                             void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* Static description of a status code. */
 const char* kvec_status_string(kvec_status status);

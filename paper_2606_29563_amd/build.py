@@ -16,7 +16,10 @@ BUILD_DIR = os.path.join(ROOT, "_build")
 # (source, object name, extra flags): the step kernel is instantiated once per
 # (dtype, head_dim) pair, in parallel translation units
 SOURCES = [("kvec_api.hip", "kvec_api", []), ("kvec_pipeline.hip", "kvec_pipeline", []),
-           ("kvec_decode.hip", "kvec_decode", [])] + [
+           ("kvec_decode.hip", "kvec_decode", []), ("kvec_serve_api.hip", "kvec_serve_api", []),
+           ("kvec_prefill.hip", "kvec_prefill", []), ("kvec_append.hip", "kvec_append", []),
+           ("kvec_paged_decode.hip", "kvec_paged_decode", []),
+           ("kvec_paged_evict.hip", "kvec_paged_evict", [])] + [
     ("kvec_step_inst.hip", f"kvec_step_{tt.lower()}_d{d}{'_long' if long == 'true' else ''}",
      [f"-DKVEC_INST_TT={tt}", f"-DKVEC_INST_D={d}", f"-DKVEC_INST_LONG={long}"])
     for tt, long in (("BF16", "false"), ("F32", "false"), ("BF16", "true")) for d in (64, 128)]

@@ -175,29 +175,10 @@ using namespace kvec;
 
 namespace {
 
-bool aligned16(const void* p) { return p && ((uintptr_t)p & 15u) == 0; }
-
-bool strides_ok(const int64_t* s, int n, int esize) {
-  if (!s) return false;
-  for (int i = 0; i < n; ++i)
-    if (s[i] < 0 || (s[i] * esize) % 16 != 0) return false;
-  return true;
-}
-
 // The score passes address the keys of one (batch, head) with 32-bit buffer
 // offsets: T rows of k_strides[t] elements must span less than 2 GiB.
 bool keys_addressable(const Problem& P, int64_t t_stride) {
   return (int64_t)P.T * t_stride * P.esize < ((int64_t)1 << 31);
-}
-
-kvec_status dev(hipError_t e) { return e == hipSuccess ? KVEC_OK : KVEC_ERR_DEVICE; }
-
-// Caller-supplied row normalisers: fp32, 4-byte aligned, non-negative strides.
-bool lse_ok(const float* lse, const int64_t* s, int n) {
-  if (!lse || ((uintptr_t)lse & 3u) != 0 || !s) return false;
-  for (int i = 0; i < n; ++i)
-    if (s[i] < 0) return false;
-  return true;
 }
 
 kvec_status check_ws(const Geometry& g, void* ws, size_t ws_bytes) {

@@ -1,0 +1,156 @@
+// Attention of 16 query columns over keys in LDS, on gfx950 matrix instructions:
+// the wave-level building block of the paged decode and of the prompt's
+// attention.
+//
+// Both products are computed transposed, S^T = K Q^T and O^T = V^T P^T, with
+// the 16x16x32 bf16 (or 16x16x4 f32) matrix instruction.  The output lane of
+// S^T holds four keys (4c .. 4c+3, c = lane / 16) of query column lane % 16,
+// which is what the second product wants of P^T as its right operand when the
+// reduction index runs over the keys in the order the lanes hold them: P never
+// leaves its registers.  A query's softmax state (maximum, sum) lies in the
+// four lanes of its column, and O^T has the same columns, so rescaling needs
+// no lane exchange either.
+//
+// K and V rows arrive by direct global-to-LDS copies of whole rows, in groups
+// of 16 keys; the 16-byte piece p of key n is stored at position
+// p ^ (n mod 16), so that the column reads of a fragment fall in distinct
+// banks.  V^T fragments of bf16 come from the transposing LDS read: in a group
+// of 16 lanes, lane i gives the address of elements 4 (i % 4) .. + 3 of row
+// i / 4 and receives element i of the four rows.
+#pragma once
+
+#include "kvec_score_dev.h"
+
+namespace kvec {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// A group of 16 rows in LDS and the copies that bring it there.
+template <class TT, int D>
+struct RowGroup {
+  static constexpr int ES = elem_bytes<TT>();
+  static constexpr int CPR = D * ES / 16;                // 16-byte pieces per row
+  static constexpr int SWZ = (CPR < 16 ? CPR : 16) - 1;  // piece swizzle mask
+  static constexpr int BYTES = 16 * CPR * 16;
+  static constexpr int NI = CPR / 4;                     // 1 KiB copies per group
+  static constexpr int RPI = 64 / CPR;                   // rows per copy
+};
+
+// Four elements of row `row` from each of 16 rows, transposed (see above): rows
+// 4c .. 4c+3 of the group at `grp`, column 16 t + lane % 16.
+template <int D>
+__device__ __forceinline__ s16x4 vt_read(const char* grp, int t, int lane) {
+  using RG = RowGroup<BF16, D>;
+  const int n = lane & 15, row = 4 * (lane >> 4) + (n >> 2);
+  const char* p = grp + row * (D * 2) + (((2 * t + ((n >> 1) & 1)) ^ (row & RG::SWZ)) << 4) + ((n & 1) << 3);
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+}
+
+// Softmax state and output of 16 query columns, NG groups of 16 keys a step.
+// SPLIT: bf16 probabilities as the sum of two bf16 numbers (2^-17 relative
+// instead of 2^-9), at twice the V products.
+template <class TT, int D, int NG, bool SPLIT>
+struct Columns16 {
+  using RG = RowGroup<TT, D>;
+  static constexpr int DT = D / 16;
+  Frag<TT, D> q;
+  float m, l;  // maximum (base-2 logits) of the column; this lane's part of the sum
+  f32x4 o[DT];
+
+  __device__ __forceinline__ void clear() {
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int t = 0; t < DT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // Products of the columns with the 16 keys at `grp`; lane: keys 4c + i.
+  __device__ __forceinline__ f32x4 logits(const char* grp, int lane) const {
+    Frag<TT, D> k;
+    k.load_lds(reinterpret_cast<const uint4*>(grp), lane & 15, lane >> 4, RG::SWZ);
+    return mma(k, q, f32x4{0.f, 0.f, 0.f, 0.f});
+  }
+
+  // One step of the online softmax: x are base-2 logits, -inf where masked.
+  // A column that has seen no key keeps m = -inf, and the exponentials use 0
+  // for it: 2^(-inf - 0) = 0 instead of 2^(-inf + inf).
+  __device__ __forceinline__ void absorb(const f32x4 (&x)[NG], const char* vgrp, int lane) {
+    float mx = m;
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+      mx = fmaxf(mx, fmaxf(fmaxf(x[g][0], x[g][1]), fmaxf(x[g][2], x[g][3])));
+    mx = col_max4(mx);
+    const float ref = mx == -INFINITY ? 0.f : mx;
+    const float f = __builtin_amdgcn_exp2f(m - ref);
+    m = mx;
+    l *= f;
+    f32x4 p[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[g][i] = __builtin_amdgcn_exp2f(x[g][i] - ref);
+        l += p[g][i];
+      }
+    if (__any(f != 1.f)) {
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[t][i] *= f;
+    }
+    if constexpr (__is_same(TT, BF16)) {
+      static_assert(NG == 2, "one 32-key product per step");
+      bf16x8 hi, lo;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float v = p[i >> 2][i & 3];
+        hi[i] = (__bf16)v;
+        if (SPLIT) lo[i] = (__bf16)(v - (float)hi[i]);
+      }
+#pragma unroll
+      for (int t = 0; t < DT; ++t) {
+        const s16x4 a0 = vt_read<D>(vgrp, t, lane), a1 = vt_read<D>(vgrp + RG::BYTES, t, lane);
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        const bf16x8 a = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+        o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, hi, o[t], 0, 0, 0);
+        if (SPLIT) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, lo, o[t], 0, 0, 0);
+      }
+    } else {
+      const int n = lane & 15, c = lane >> 4;
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int row = 4 * c + i;
+          const char* pr = vgrp + g * RG::BYTES + row * (D * 4) + ((n & 3) << 2);
+#pragma unroll
+          for (int t = 0; t < DT; ++t) {
+            const float a = *reinterpret_cast<const float*>(pr + (((4 * t + (n >> 2)) ^ (row & RG::SWZ)) << 4));
+            o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, p[g][i], o[t], 0, 0, 0);
+          }
+        }
+    }
+  }
+};
+
+// Copies of one group of 16 rows: lane part of the byte offsets.
+template <class TT, int D>
+__device__ __forceinline__ int row_in_copy(int i, int lane) { return i * RowGroup<TT, D>::RPI + lane / RowGroup<TT, D>::CPR; }
+template <class TT, int D>
+__device__ __forceinline__ int piece_in_copy(int i, int lane) {
+  using RG = RowGroup<TT, D>;
+  return (lane % RG::CPR) ^ (row_in_copy<TT, D>(i, lane) & RG::SWZ);
+}
+
+// Merge of (m2, l2, a2) into (m, l, a); m = -inf means an empty state.
+__device__ __forceinline__ void state_merge(float& m, float& l, float& a, float m2, float l2, float a2) {
+  const float mm = fmaxf(m, m2);
+  const float ref = mm == -INFINITY ? 0.f : mm;
+  const float f1 = __builtin_amdgcn_exp2f(m - ref), f2 = __builtin_amdgcn_exp2f(m2 - ref);
+  l = l * f1 + l2 * f2;
+  a = a * f1 + a2 * f2;
+  m = mm;
+}
+
+}  // namespace kvec

@@ -158,6 +158,26 @@ hipError_t run_decode(const Geometry& g, const void* q, const int64_t qs[2], con
                       const void* v, const int64_t cs[2], int n_ctx, const int32_t* idx, float* out,
                       void* ws, hipStream_t s);
 
+// Argument checks of the C ABI.
+inline bool aligned16(const void* p) { return p && ((uintptr_t)p & 15u) == 0; }
+
+inline bool strides_ok(const int64_t* s, int n, int esize) {
+  if (!s) return false;
+  for (int i = 0; i < n; ++i)
+    if (s[i] < 0 || (s[i] * esize) % 16 != 0) return false;
+  return true;
+}
+
+inline kvec_status dev(hipError_t e) { return e == hipSuccess ? KVEC_OK : KVEC_ERR_DEVICE; }
+
+// Caller-supplied row normalisers: fp32, 4-byte aligned, non-negative strides.
+inline bool lse_ok(const float* lse, const int64_t* s, int n) {
+  if (!lse || ((uintptr_t)lse & 3u) != 0 || !s) return false;
+  for (int i = 0; i < n; ++i)
+    if (s[i] < 0) return false;
+  return true;
+}
+
 // ---------------------------------------------------------------------------
 // Device helpers
 // ---------------------------------------------------------------------------

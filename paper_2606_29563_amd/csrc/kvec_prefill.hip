@@ -1,0 +1,240 @@
+// A prompt's attention (causal, or a sliding window with sinks) and the
+// log-sum-exp of its rows.
+//
+// The G query heads of a KV head are packed into the rows of a tile: packed row
+// i of a (sequence, KV head) is query row i / G of head i % G, so a tile reads
+// every K and V row once for all of them, and few query rows still fill it.
+// A work-group goes over the key tiles that some row of it sees: those of the
+// sinks, then those from the oldest row's window to the newest row's own key.
+// Only tiles at an edge of what is visible are masked.  Few rows over many keys
+// are split over the keys, with the partial states joined by a second launch.
+#include "kvec_attn_dev.h"
+#include "kvec_serve.h"
+
+namespace kvec {
+namespace {
+
+struct PfArgs {
+  PrefillArgs p;
+  int S, tiles;
+  float* part;  // [b][HQ][q_len][S][D + 2] when S > 1
+  float sc;
+};
+
+// What a tile of packed rows sees, in tiles of KT keys.
+template <int KT>
+struct Span {
+  int nq, nk, shift;       // rows, keys, position of row 0
+  int p_lo, p_hi;          // positions of the tile's first and last row
+  int ns, g0, n;           // key tiles of the sinks; first of the window; in all
+  int window, sinks;
+  bool any;                // the tile holds rows
+  __device__ __forceinline__ Span(const PrefillArgs& a, int b, int row0, int rows) {
+    nq = a.q_lens ? min(max(a.q_lens[b], 0), a.q_len) : a.q_len;
+    nk = a.kv_lens ? min(max(a.kv_lens[b], 0), a.kv_len) : a.kv_len;
+    window = a.window;
+    sinks = a.sinks;
+    shift = nk - nq;
+    const int r0 = row0 / a.G, r1 = min((row0 + rows - 1) / a.G, nq - 1);
+    any = r0 < nq;
+    p_lo = shift + r0;
+    p_hi = shift + r1;
+    const int end = any ? max(p_hi + 1, 0) : 0;
+    const int lo = window > 0 ? max(p_lo - window + 1, 0) : 0;
+    g0 = lo / KT;
+    ns = window > 0 ? min((min(sinks, end) + KT - 1) / KT, g0) : 0;
+    n = end > 0 ? ns + (end + KT - 1) / KT - g0 : 0;
+  }
+  __device__ __forceinline__ int key0(int t) const { return (t < ns ? t : g0 + t - ns) * KT; }
+  // every row of the tile sees all keys of [t0, t0 + KT)
+  __device__ __forceinline__ bool open(int t0) const {
+    return t0 + KT - 1 <= p_lo && (window == 0 || t0 > p_hi - window || t0 + KT <= sinks);
+  }
+  __device__ __forceinline__ bool sees(int t, int p) const {
+    return t <= p && (window == 0 || t > p - window || t < sinks);
+  }
+};
+
+constexpr int kPfThreads = 256;
+constexpr int kPfRows = 64;  // packed rows per work-group, 16 per wave
+constexpr int kPfKeys = 32;
+
+template <class TT, int D>
+__global__ __launch_bounds__(kPfThreads) void pf_rows16(PfArgs a) {
+  using RG = RowGroup<TT, D>;
+  constexpr int NG = __is_same(TT, BF16) ? 2 : 1, ES = RG::ES;
+  constexpr int GRPS = kPfKeys / 16;
+  constexpr int BUF = 2 * GRPS * RG::BYTES;       // K groups, then V groups
+  constexpr int PER = 2 * GRPS * RG::NI / 4;      // copies per wave and tile
+  __shared__ __align__(1024) char smem[2 * BUF];
+  const PrefillArgs& p = a.p;
+  const int tile = a.tiles - 1 - (int)blockIdx.x / a.S, split = blockIdx.x % a.S;
+  const int h = blockIdx.y, b = blockIdx.z, G = p.G;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int n = lane & 15, c = lane >> 4;
+  const Span<kPfKeys> sp(p, b, tile * kPfRows, kPfRows);
+  if (!sp.any) return;
+  const int i = tile * kPfRows + w * 16 + n, r = i / G, j = h * G + i % G;
+  const bool live = r < sp.nq;
+  const int pos = live ? sp.shift + r : -1;
+  const int per = (sp.n + a.S - 1) / a.S;
+  const int t0 = min(split * per, sp.n), t1 = min(t0 + per, sp.n);
+
+  Columns16<TT, D, NG, false> col;
+  col.clear();
+  col.q.zero();
+  if (live) col.q.load(p.q + ((int64_t)b * p.qs[0] + (int64_t)j * p.qs[1] + (int64_t)r * p.qs[2]) * ES, c);
+
+  const int kstr = (int)(p.ks[2] * ES), vstr = (int)(p.vs[2] * ES);
+  const int last = max(sp.nk - 1, 0);
+  const auto kr = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<char*>(p.k) + ((int64_t)b * p.ks[0] + (int64_t)h * p.ks[1]) * ES, 0, last * kstr + D * ES, kBufferWord3);
+  const auto vr = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<char*>(p.v) + ((int64_t)b * p.vs[0] + (int64_t)h * p.vs[1]) * ES, 0, last * vstr + D * ES, kBufferWord3);
+  auto copy = [&](int u, int t) {
+    const int key0 = sp.key0(t);
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      const int at = w * PER + q;  // copy of the tile: K's, then V's
+      const bool is_v = at >= GRPS * RG::NI;
+      const int in = is_v ? at - GRPS * RG::NI : at;
+      const int row = row_in_copy<TT, D>(in % RG::NI, lane) + in / RG::NI * 16;
+      const int off = key0 + row < sp.nk ? (key0 + row) * (is_v ? vstr : kstr) + piece_in_copy<TT, D>(in % RG::NI, lane) * 16
+                                         : kOutOfRange;
+      auto* dst = (__attribute__((address_space(3))) char*)(smem + u * BUF + at * 1024);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(is_v ? vr : kr, dst, 16, off, 0, 0, 0);
+    }
+  };
+  if (t0 < t1) copy(0, t0);
+  for (int t = t0; t < t1; ++t) {
+    const int u = (t - t0) & 1;
+    wait_vmem<0>();
+    lds_barrier();  // the tile is there, and every wave is done with the other buffer
+    if (t + 1 < t1) copy(u ^ 1, t + 1);
+    const char* kb = smem + u * BUF;
+    const int key0 = sp.key0(t);
+    const bool open = sp.open(key0) && live;
+#pragma unroll
+    for (int g0 = 0; g0 < GRPS; g0 += NG) {
+      f32x4 x[NG];
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        x[g] = col.logits(kb + (g0 + g) * RG::BYTES, lane);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int key = key0 + 16 * (g0 + g) + 4 * c + e;
+          x[g][e] = open || sp.sees(key, pos) ? x[g][e] * a.sc : -INFINITY;
+        }
+      }
+      col.absorb(x, kb + (GRPS + g0) * RG::BYTES, lane);
+    }
+  }
+  col.l = col_sum4(col.l);
+  if (!live) return;
+  const int64_t row = ((int64_t)b * p.HQ + j) * p.q_len + r;
+  if (a.S > 1) {
+    float* pp = a.part + (row * a.S + split) * (D + 2);
+    if (c == 0) {
+      pp[0] = col.m;
+      pp[1] = col.l;
+    }
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) pp[2 + 16 * t + 4 * c + e] = col.o[t][e];
+    return;
+  }
+  const float inv = col.m == -INFINITY ? 0.f : 1.f / col.l;
+  char* dst = p.out + ((int64_t)b * p.os[0] + (int64_t)j * p.os[1] + (int64_t)r * p.os[2]) * ES;
+#pragma unroll
+  for (int t = 0; t < D / 16; ++t) {
+    if constexpr (ES == 2) {
+      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+      bf16x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = (__bf16)(col.o[t][e] * inv);
+      *reinterpret_cast<bf16x4*>(dst + (16 * t + 4 * c) * 2) = v;
+    } else {
+      *reinterpret_cast<f32x4*>(dst + (16 * t + 4 * c) * 4) = col.o[t] * inv;
+    }
+  }
+  if (p.lse && c == 0)
+    p.lse[(int64_t)b * p.ls[0] + (int64_t)j * p.ls[1] + r] =
+        col.m == -INFINITY ? -INFINITY : (col.m + log2f(col.l)) * 0.69314718055994531f;
+}
+
+// Join the splits of one row: grid (q_len, HQ, batch), one thread per element.
+template <class T, int D>
+__global__ __launch_bounds__(D) void pf_join(PfArgs a) {
+  const PrefillArgs& p = a.p;
+  const int r = blockIdx.x, j = blockIdx.y, b = blockIdx.z, e = threadIdx.x;
+  const int nq = p.q_lens ? min(max(p.q_lens[b], 0), p.q_len) : p.q_len;
+  if (r >= nq) return;
+  const float* pp = a.part + (((int64_t)b * p.HQ + j) * p.q_len + r) * a.S * (D + 2);
+  float m = -INFINITY, l = 0.f, o = 0.f;
+  for (int s = 0; s < a.S; ++s, pp += D + 2) state_merge(m, l, o, pp[0], pp[1], pp[2 + e]);
+  T* dst = reinterpret_cast<T*>(p.out) + (int64_t)b * p.os[0] + (int64_t)j * p.os[1] + (int64_t)r * p.os[2];
+  dst[e] = (T)(m == -INFINITY ? 0.f : o / l);
+  if (p.lse && e == 0)
+    p.lse[(int64_t)b * p.ls[0] + (int64_t)j * p.ls[1] + r] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+
+struct PfPlan {
+  int S, tiles;
+  size_t bytes;
+};
+
+// Splits over the keys: where the row tiles are fewer than 512 work-groups, as
+// many as that takes, of at least eight key tiles each.
+PfPlan pf_plan(const PrefillArgs& a) {
+  PfPlan pl;
+  pl.tiles = (int)(((int64_t)a.q_len * a.G + kPfRows - 1) / kPfRows);
+  const int64_t groups = (int64_t)pl.tiles * a.batch * a.H;
+  int64_t keys = a.kv_len;
+  if (a.window > 0) {
+    const int64_t most = (int64_t)a.window + a.sinks + kPfRows;
+    if (most < keys) keys = most;
+  }
+  const int64_t most_s = keys / (8 * kPfKeys);
+  int64_t S = groups >= 512 ? 1 : (512 + groups - 1) / groups;
+  if (S > most_s) S = most_s;
+  if (S > 64) S = 64;
+  pl.S = S < 1 ? 1 : (int)S;
+  pl.bytes = pl.S > 1 ? (size_t)a.batch * a.HQ * a.q_len * pl.S * (a.D + 2) * 4 : 0;
+  return pl;
+}
+
+}  // namespace
+
+size_t prefill_ws(const PrefillArgs& a) { return pf_plan(a).bytes; }
+
+hipError_t run_prefill(const PrefillArgs& p, char* ws, hipStream_t s) {
+  const PfPlan pl = pf_plan(p);
+  PfArgs a;
+  a.p = p;
+  a.S = pl.S;
+  a.tiles = pl.tiles;
+  a.part = reinterpret_cast<float*>(ws);
+  a.sc = (float)(1.4426950408889634 / sqrt((double)p.D));
+  const dim3 grid((unsigned)(pl.tiles * pl.S), p.H, p.batch);
+  if (p.esize == 2) {
+    if (p.D == 64) hipLaunchKernelGGL((pf_rows16<BF16, 64>), grid, dim3(kPfThreads), 0, s, a);
+    else hipLaunchKernelGGL((pf_rows16<BF16, 128>), grid, dim3(kPfThreads), 0, s, a);
+  } else {
+    if (p.D == 64) hipLaunchKernelGGL((pf_rows16<F32, 64>), grid, dim3(kPfThreads), 0, s, a);
+    else hipLaunchKernelGGL((pf_rows16<F32, 128>), grid, dim3(kPfThreads), 0, s, a);
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || pl.S == 1) return e;
+  const dim3 jgrid(p.q_len, p.HQ, p.batch);
+  if (p.esize == 2) {
+    if (p.D == 64) hipLaunchKernelGGL((pf_join<__bf16, 64>), jgrid, dim3(64), 0, s, a);
+    else hipLaunchKernelGGL((pf_join<__bf16, 128>), jgrid, dim3(128), 0, s, a);
+  } else {
+    if (p.D == 64) hipLaunchKernelGGL((pf_join<float, 64>), jgrid, dim3(64), 0, s, a);
+    else hipLaunchKernelGGL((pf_join<float, 128>), jgrid, dim3(128), 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace kvec

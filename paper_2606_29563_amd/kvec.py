@@ -83,6 +83,51 @@ class Config:
         return (self.seq_len + 63) // 64
 
 
+class kvec_attention_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_kv_heads", "n_q_heads", "head_dim", "q_len",
+                                              "kv_len", "window", "n_sinks", "dtype")]
+
+
+class kvec_paged_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_kv_heads", "n_q_heads", "head_dim",
+                                              "page_size", "n_pages", "max_pages", "dtype")]
+
+
+@dataclass
+class AttentionConfig:
+    """Python view of kvec_attention_config."""
+    batch: int
+    n_kv_heads: int
+    n_q_heads: int
+    head_dim: int
+    q_len: int
+    kv_len: int
+    window: int = 0
+    n_sinks: int = 0
+    dtype: int = KVEC_BF16
+
+    def c(self) -> kvec_attention_config:
+        return kvec_attention_config(self.batch, self.n_kv_heads, self.n_q_heads, self.head_dim,
+                                     self.q_len, self.kv_len, self.window, self.n_sinks, self.dtype)
+
+
+@dataclass
+class PagedConfig:
+    """Python view of kvec_paged_config."""
+    batch: int
+    n_kv_heads: int
+    n_q_heads: int
+    head_dim: int
+    page_size: int
+    n_pages: int
+    max_pages: int
+    dtype: int = KVEC_BF16
+
+    def c(self) -> kvec_paged_config:
+        return kvec_paged_config(self.batch, self.n_kv_heads, self.n_q_heads, self.head_dim,
+                                 self.page_size, self.n_pages, self.max_pages, self.dtype)
+
+
 _lib = None
 
 EXPORTS = ["kvec_workspace_size", "kvec_score", "kvec_score_lse", "kvec_select_cover",
@@ -91,6 +136,9 @@ EXPORTS = ["kvec_workspace_size", "kvec_score", "kvec_score_lse", "kvec_select_c
            "kvec_evict_model_lse_steps",
            "kvec_profile_points", "kvec_profile_points_lse", "kvec_coverage",
            "kvec_decode_workspace_size", "kvec_decode_attention", "kvec_decode_attention_noalloc",
+           "kvec_prefill_workspace_size", "kvec_prefill_attention", "kvec_paged_append",
+           "kvec_paged_decode_workspace_size", "kvec_paged_decode",
+           "kvec_paged_evict_workspace_size", "kvec_paged_evict",
            "kvec_status_string"]
 
 
@@ -130,6 +178,19 @@ def load() -> ctypes.CDLL:
     lib.kvec_decode_attention.argtypes = [P, vp, I64x, vp, vp, I64x, i32, vp, vp, vp, sz, vp]
     lib.kvec_profile_points.argtypes = [P]
     lib.kvec_profile_points_lse.argtypes = [P]
+    A, C = ctypes.POINTER(kvec_attention_config), ctypes.POINTER(kvec_paged_config)
+    f32 = ctypes.c_float
+    lib.kvec_prefill_workspace_size.argtypes = [A, ctypes.POINTER(sz)]
+    lib.kvec_prefill_attention.argtypes = [A, vp, I64x, vp, I64x, vp, I64x, vp, vp, vp, I64x, vp, I64x,
+                                           vp, sz, vp]
+    lib.kvec_paged_append.argtypes = [C, i32, vp, I64x, vp, I64x, vp, I64x, vp, vp, f32, vp, vp, i32, vp,
+                                      vp, I64x, vp, vp, I64x, vp, vp, vp]
+    lib.kvec_paged_decode_workspace_size.argtypes = [C, i32, i32, ctypes.POINTER(sz)]
+    lib.kvec_paged_decode.argtypes = [C, vp, I64x, vp, vp, I64x, vp, vp, i32, i32, i32, vp, vp, vp, vp,
+                                      sz, vp]
+    lib.kvec_paged_evict_workspace_size.argtypes = [C, i32, i32, ctypes.POINTER(sz)]
+    lib.kvec_paged_evict.argtypes = [C, i32, i32, i32, vp, vp, I64x, vp, vp, vp, i32, vp, vp, vp, vp, vp,
+                                     sz, vp]
     lib.kvec_status_string.argtypes = [ctypes.c_int]
     lib.kvec_status_string.restype = ctypes.c_char_p
     for name in EXPORTS:
@@ -363,3 +424,159 @@ def kvec_decode_attention_noalloc(cfg: Config, q, k_cache, v_cache, out, idx=Non
                                                 _ptr(k_cache), _ptr(v_cache), _strides(k_cache, 2),
                                                 n, _ptr(idx), _ptr(out), _stream(stream)),
            "kvec_decode_attention_noalloc")
+
+
+def _rows(t, shape, dtype, what: str):
+    """Checks a tensor of rows (its last dimension contiguous); its leading element strides."""
+    assert tuple(t.shape) == tuple(shape), f"{what} must be {tuple(shape)}, not {tuple(t.shape)}"
+    assert t.dtype == dtype, f"{what} must be {dtype}"
+    return _strides(t, len(shape) - 1)
+
+
+def _dense(t, shape, dtype, what: str) -> int | None:
+    """Checks a contiguous tensor (None passes); its address."""
+    if t is None:
+        return None
+    assert tuple(t.shape) == tuple(shape) and t.is_contiguous(), \
+        f"{what} must be contiguous {tuple(shape)}, not {tuple(t.shape)}"
+    assert t.dtype == dtype, f"{what} must be {dtype}"
+    return t.data_ptr()
+
+
+def _torch_dtype(dtype: int):
+    import torch
+    return torch.bfloat16 if dtype == KVEC_BF16 else torch.float32
+
+
+def _on_device(t, tensors, stream, call, what: str) -> None:
+    """call(stream handle) with t's device current, on its current stream unless one is given."""
+    import torch
+    assert t.is_cuda, f"{what}: the tensors must be on a GPU"
+    for x in tensors:
+        assert x is None or x.device == t.device, f"{what}: the tensors must share a device"
+    if t.device.index == torch.cuda.current_device():
+        _check(call(_stream(stream)), what)
+    else:
+        with torch.cuda.device(t.device):
+            _check(call(_stream(stream)), what)
+
+
+def _ws(ws):
+    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+
+
+def kvec_prefill_workspace_size(cfg: AttentionConfig) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().kvec_prefill_workspace_size(ctypes.byref(cfg.c()), ctypes.byref(out)),
+           "kvec_prefill_workspace_size")
+    return out.value
+
+
+def kvec_prefill_attention(cfg: AttentionConfig, q, k, v, out, ws=None, lse=None, q_lens=None,
+                           kv_lens=None, stream=None) -> None:
+    """q, out [b][HQ][q_len][d]; k, v [b][H][kv_len][d] (any leading strides); lse fp32
+    [b][HQ][q_len], rows contiguous; q_lens, kv_lens int32 [b].  ws may be None when
+    kvec_prefill_workspace_size(cfg) is 0."""
+    import torch
+    dt = _torch_dtype(cfg.dtype)
+    rows = (cfg.batch, cfg.n_q_heads, cfg.q_len, cfg.head_dim)
+    keys = (cfg.batch, cfg.n_kv_heads, cfg.kv_len, cfg.head_dim)
+    qs, os_ = _rows(q, rows, dt, "q"), _rows(out, rows, dt, "out")
+    ks, vs = _rows(k, keys, dt, "k"), _rows(v, keys, dt, "v")
+    ls = None if lse is None else _rows(lse, rows[:3], torch.float32, "lse")
+    ql = _dense(q_lens, (cfg.batch,), torch.int32, "q_lens")
+    kl = _dense(kv_lens, (cfg.batch,), torch.int32, "kv_lens")
+    lib, c, (wp, wn) = load(), cfg.c(), _ws(ws)
+    _on_device(q, (k, v, out, ws, lse, q_lens, kv_lens), stream, lambda st: lib.kvec_prefill_attention(
+        ctypes.byref(c), _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, ql, kl, _ptr(out), os_, _ptr(lse), ls, wp,
+        wn, st), "kvec_prefill_attention")
+
+
+def _pools(cfg: PagedConfig, k_pool, v_pool):
+    shape = (cfg.n_pages, cfg.n_kv_heads, cfg.page_size, cfg.head_dim)
+    dt = _torch_dtype(cfg.dtype)
+    ps = _rows(k_pool, shape, dt, "k_pool")
+    _rows(v_pool, shape, dt, "v_pool")
+    assert k_pool.stride() == v_pool.stride(), "K and V pools share their strides"
+    return ps
+
+
+def kvec_paged_append(cfg: PagedConfig, q, k, v, positions, slots, q_out, k_pool, v_pool, q_weight=None,
+                      k_weight=None, eps=1e-6, inv_freq=None, acc=None, pos=None, stream=None) -> None:
+    """q, q_out [n][HQ][d], k, v [n][H][d] (any token and head strides), positions int32
+    [n], slots int64 [n] (page * page_size + row; -1: not stored), pools
+    [n_pages][H][page_size][d]; weights [d] (None: no norm); inv_freq float64 [rot_dim / 2]
+    (None: no rotation); acc fp32 and pos int32 [n_pages][H][page_size]."""
+    import torch
+    dt, n, d = _torch_dtype(cfg.dtype), q.shape[0], cfg.head_dim
+    qs, os_ = _rows(q, (n, cfg.n_q_heads, d), dt, "q"), _rows(q_out, (n, cfg.n_q_heads, d), dt, "q_out")
+    ks, vs = _rows(k, (n, cfg.n_kv_heads, d), dt, "k"), _rows(v, (n, cfg.n_kv_heads, d), dt, "v")
+    ps = _pools(cfg, k_pool, v_pool)
+    meta = (cfg.n_pages, cfg.n_kv_heads, cfg.page_size)
+    at, sl = _dense(positions, (n,), torch.int32, "positions"), _dense(slots, (n,), torch.int64, "slots")
+    wq, wk = _dense(q_weight, (d,), dt, "q_weight"), _dense(k_weight, (d,), dt, "k_weight")
+    ac, po = _dense(acc, meta, torch.float32, "acc"), _dense(pos, meta, torch.int32, "pos")
+    rot = 0 if inv_freq is None else 2 * inv_freq.shape[0]
+    fr = None if inv_freq is None else _dense(inv_freq, (rot // 2,), torch.float64, "inv_freq")
+    lib, c = load(), cfg.c()
+    _on_device(k_pool, (q, k, v, positions, slots, q_out, v_pool, q_weight, k_weight, inv_freq, acc, pos),
+               stream, lambda st: lib.kvec_paged_append(
+        ctypes.byref(c), n, _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, wq, wk, eps, at, fr, rot, sl, _ptr(q_out),
+        os_, _ptr(k_pool), _ptr(v_pool), ps, ac, po, st), "kvec_paged_append")
+
+
+def kvec_paged_decode_workspace_size(cfg: PagedConfig, max_len: int | None = None,
+                                     with_acc: bool = False) -> int:
+    out = ctypes.c_size_t(0)
+    n = cfg.max_pages * cfg.page_size if max_len is None else max_len
+    _check(load().kvec_paged_decode_workspace_size(ctypes.byref(cfg.c()), n, int(with_acc),
+                                                   ctypes.byref(out)), "kvec_paged_decode_workspace_size")
+    return out.value
+
+
+def kvec_paged_decode(cfg: PagedConfig, q, k_pool, v_pool, page_table, lens, out, ws, max_len=None,
+                      window=0, n_sinks=0, lse=None, acc=None, stream=None) -> None:
+    """q [b][HQ][d]; pools [n_pages][H][page_size][d] (K and V with the same strides);
+    page_table int32 [b][max_pages]; lens int32 [b]; out fp32 [b][HQ][d]; lse fp32
+    [b][HQ]; acc fp32 [n_pages][H][page_size]."""
+    import torch
+    b, HQ, d = cfg.batch, cfg.n_q_heads, cfg.head_dim
+    qs, ps = _rows(q, (b, HQ, d), _torch_dtype(cfg.dtype), "q"), _pools(cfg, k_pool, v_pool)
+    tb = _dense(page_table, (b, cfg.max_pages), torch.int32, "page_table")
+    ln, op = _dense(lens, (b,), torch.int32, "lens"), _dense(out, (b, HQ, d), torch.float32, "out")
+    lp = _dense(lse, (b, HQ), torch.float32, "lse")
+    ac = _dense(acc, (cfg.n_pages, cfg.n_kv_heads, cfg.page_size), torch.float32, "acc")
+    n = cfg.max_pages * cfg.page_size if max_len is None else max_len
+    lib, c, (wp, wn) = load(), cfg.c(), _ws(ws)
+    _on_device(q, (k_pool, v_pool, page_table, lens, out, ws, lse, acc), stream,
+               lambda st: lib.kvec_paged_decode(ctypes.byref(c), _ptr(q), qs, _ptr(k_pool), _ptr(v_pool), ps,
+                                                tb, ln, n, window, n_sinks, op, lp, ac, wp, wn, st),
+               "kvec_paged_decode")
+
+
+def kvec_paged_evict_workspace_size(cfg: PagedConfig, max_len: int | None, budget: int) -> int:
+    out = ctypes.c_size_t(0)
+    n = cfg.max_pages * cfg.page_size if max_len is None else max_len
+    _check(load().kvec_paged_evict_workspace_size(ctypes.byref(cfg.c()), n, budget, ctypes.byref(out)),
+           "kvec_paged_evict_workspace_size")
+    return out.value
+
+
+def kvec_paged_evict(cfg: PagedConfig, budget: int, k_pool, v_pool, page_table, lens, n_seen, acc, pos,
+                     lens_out, ws, window=0, n_sinks=0, kept=None, max_len=None, stream=None) -> None:
+    """Pools and tables as in kvec_paged_decode; acc fp32 and pos int32
+    [n_pages][H][page_size]; lens, n_seen, lens_out int32 [b] (lens_out may be lens);
+    kept int32 [b][H][budget]."""
+    import torch
+    b, H = cfg.batch, cfg.n_kv_heads
+    ps, meta = _pools(cfg, k_pool, v_pool), (cfg.n_pages, H, cfg.page_size)
+    tb = _dense(page_table, (b, cfg.max_pages), torch.int32, "page_table")
+    ln, ns = _dense(lens, (b,), torch.int32, "lens"), _dense(n_seen, (b,), torch.int32, "n_seen")
+    lo, ac = _dense(lens_out, (b,), torch.int32, "lens_out"), _dense(acc, meta, torch.float32, "acc")
+    po, kp = _dense(pos, meta, torch.int32, "pos"), _dense(kept, (b, H, budget), torch.int32, "kept")
+    n = cfg.max_pages * cfg.page_size if max_len is None else max_len
+    lib, c, (wp, wn) = load(), cfg.c(), _ws(ws)
+    _on_device(k_pool, (v_pool, page_table, lens, n_seen, acc, pos, lens_out, ws, kept), stream,
+               lambda st: lib.kvec_paged_evict(ctypes.byref(c), budget, window, n_sinks, _ptr(k_pool),
+                                               _ptr(v_pool), ps, tb, ln, ns, n, ac, po, kp, lo, wp, wn, st),
+               "kvec_paged_evict")
