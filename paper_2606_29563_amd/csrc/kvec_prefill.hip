@@ -55,6 +55,33 @@ struct Span {
   }
 };
 
+// Work-group -> (sequence and KV head, row tile, split), longest tiles first.
+// Work-groups go round the eight XCDs, each with an L2 of its own: all that read
+// the K and V of one head run on the same XCD, or, with fewer than eight heads,
+// on as few as that takes.
+__device__ __forceinline__ bool pf_item(const PfArgs& a, int* bh, int* tile, int* split) {
+  const int BH = a.p.batch * a.p.H, items = a.tiles * a.S, id = blockIdx.x;
+  int it;
+  if (BH % 8 == 0) {
+    *bh = (id & 7) + 8 * ((id >> 3) / items);
+    it = (id >> 3) % items;
+  } else if (8 % BH == 0) {
+    *bh = (id & 7) % BH;
+    it = (id >> 3) * (8 / BH) + (id & 7) / BH;
+  } else {
+    *bh = id % BH;
+    it = id / BH;
+  }
+  if (it >= items) return false;
+  *tile = a.tiles - 1 - it / a.S;
+  *split = it % a.S;
+  return true;
+}
+inline unsigned pf_grid(const PfArgs& a) {
+  const int64_t BH = (int64_t)a.p.batch * a.p.H, items = (int64_t)a.tiles * a.S;
+  return (unsigned)(8 % BH == 0 ? (items + 8 / BH - 1) / (8 / BH) * 8 : items * BH);
+}
+
 constexpr int kPfThreads = 256;
 constexpr int kPfRows = 64;  // packed rows per work-group, 16 per wave
 constexpr int kPfKeys = 32;
@@ -68,8 +95,10 @@ __global__ __launch_bounds__(kPfThreads) void pf_rows16(PfArgs a) {
   constexpr int PER = 2 * GRPS * RG::NI / 4;      // copies per wave and tile
   __shared__ __align__(1024) char smem[2 * BUF];
   const PrefillArgs& p = a.p;
-  const int tile = a.tiles - 1 - (int)blockIdx.x / a.S, split = blockIdx.x % a.S;
-  const int h = blockIdx.y, b = blockIdx.z, G = p.G;
+  const int G = p.G;
+  int bh, tile, split;
+  if (!pf_item(a, &bh, &tile, &split)) return;
+  const int b = bh / p.H, h = bh % p.H;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int n = lane & 15, c = lane >> 4;
   const Span<kPfKeys> sp(p, b, tile * kPfRows, kPfRows);
@@ -163,6 +192,213 @@ __global__ __launch_bounds__(kPfThreads) void pf_rows16(PfArgs a) {
         col.m == -INFINITY ? -INFINITY : (col.m + log2f(col.l)) * 0.69314718055994531f;
 }
 
+// Long prompts, bf16: a work-group of four waves takes 128 packed rows, a wave
+// 32 of them as the columns of 32x32x16 products (S^T = K Q^T, O^T = V^T P^T; see
+// kvec_attn_dev.h for why P stays in its registers: here the output lane holds
+// keys 8 (i / 4) + 4 (lane / 32) + i % 4 of column lane % 32, and the V product's
+// reduction runs over the keys in that order).  Tiles of 64 keys are copied
+// into one of two LDS buffers while the other is used; one barrier per tile.
+//
+// The softmax keeps a reference per column instead of the running maximum: O and
+// the sum are rescaled only when a tile's maximum exceeds the reference by more
+// than 8 (a factor of 256), so most tiles skip the pass over O.  The quotient
+// O / l does not depend on the reference, float32 sums of terms up to 2^8 lose
+// nothing, and the bf16 rounding of P is relative.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+constexpr int kPf32Rows = 128, kPf32Keys = 64;
+
+// 16-byte piece p of row r is stored at position p ^ swizzle(r) of the row, so
+// that the 16 lanes of a fragment read (16 rows, one piece) and the 32 lanes of a
+// transposing read (four rows, four pieces) fall in distinct banks.
+template <int D>
+__device__ __forceinline__ int k_swizzle(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
+template <int D>
+__device__ __forceinline__ int v_swizzle(int r) {
+  return D == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
+}
+
+template <class TT, int D>
+__device__ __forceinline__ void rows32(const PfArgs& a) {
+  constexpr int ES = elem_bytes<TT>();
+  constexpr int CPR = D / 8, RPI = 64 / CPR;  // pieces per row, rows per copy
+  constexpr int HALF = kPf32Keys * D * 2;     // bytes of the K (or V) rows of a tile
+  constexpr int PER = HALF / 1024 / 4;        // copies per wave of each
+  constexpr int KS = D / 16, DT = D / 32;
+  __shared__ __align__(1024) char smem[2 * 2 * HALF];
+  const PrefillArgs& p = a.p;
+  const int G = p.G;
+  int bh, tile, split;
+  if (!pf_item(a, &bh, &tile, &split)) return;
+  const int b = bh / p.H, h = bh % p.H;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int n = lane & 31, hh = lane >> 5;
+  const Span<kPf32Keys> sp(p, b, tile * kPf32Rows, kPf32Rows);
+  if (!sp.any) return;
+  const int i = tile * kPf32Rows + w * 32 + n, r = i / G, j = h * G + i % G;
+  const bool live = r < sp.nq;
+  const int pos = live ? sp.shift + r : -1;
+  const int per = (sp.n + a.S - 1) / a.S;
+  const int t0 = min(split * per, sp.n), t1 = min(t0 + per, sp.n);
+
+  bf16x8 qf[KS];
+  {
+    const char* q = p.q + ((int64_t)b * p.qs[0] + (int64_t)j * p.qs[1] + (int64_t)r * p.qs[2]) * ES;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      qf[ks] = __builtin_bit_cast(bf16x8, live ? reinterpret_cast<const uint4*>(q)[2 * ks + hh] : make_uint4(0, 0, 0, 0));
+  }
+  const int kstr = (int)(p.ks[2] * ES), vstr = (int)(p.vs[2] * ES);
+  const int last = max(sp.nk - 1, 0);
+  const auto kr = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<char*>(p.k) + ((int64_t)b * p.ks[0] + (int64_t)h * p.ks[1]) * ES, 0, last * kstr + D * ES, kBufferWord3);
+  const auto vr = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<char*>(p.v) + ((int64_t)b * p.vs[0] + (int64_t)h * p.vs[1]) * ES, 0, last * vstr + D * ES, kBufferWord3);
+  int krow[PER], kpc[PER], vpc[PER];
+#pragma unroll
+  for (int q = 0; q < PER; ++q) {
+    krow[q] = (w * PER + q) * RPI + lane / CPR;
+    kpc[q] = ((lane % CPR) ^ k_swizzle<D>(krow[q])) * 16;
+    vpc[q] = ((lane % CPR) ^ v_swizzle<D>(krow[q])) * 16;
+  }
+  auto copy = [&](int u, int t) {
+    const int key0 = sp.key0(t);
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      auto* dk = (__attribute__((address_space(3))) char*)(smem + u * 2 * HALF + (w * PER + q) * 1024);
+      auto* dv = (__attribute__((address_space(3))) char*)(smem + u * 2 * HALF + HALF + (w * PER + q) * 1024);
+      const bool in = key0 + krow[q] < sp.nk;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, dk, 16, in ? (key0 + krow[q]) * kstr + kpc[q] : kOutOfRange, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, dv, 16, in ? (key0 + krow[q]) * vstr + vpc[q] : kOutOfRange, 0, 0, 0);
+    }
+  };
+
+  // lane part of the LDS addresses: fragments of K, transposed reads of V
+  int koff[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) koff[ks] = n * D * 2 + ((2 * ks + hh) ^ k_swizzle<D>(n)) * 16;
+  const int vrow = 4 * hh + ((lane & 15) >> 2);  // row of the lane in a step's first four and last four
+  int voff[DT][2];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int row = vrow + 8 * e, piece = 4 * dt + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+      voff[dt][e] = row * D * 2 + (piece ^ v_swizzle<D>(row)) * 16 + (lane & 1) * 8;
+    }
+
+  f32x16 o[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
+  float m = -INFINITY, l = 0.f;  // reference (base-2 logits); this lane's part of the sum
+
+  if (t0 < t1) copy(0, t0);
+  for (int t = t0; t < t1; ++t) {
+    const int u = (t - t0) & 1;
+    wait_vmem<0>();
+    lds_barrier();  // the tile is there, and every wave is done with the other buffer
+    if (t + 1 < t1) copy(u ^ 1, t + 1);
+    const char* kb = smem + u * 2 * HALF;
+    const char* vb = kb + HALF;
+    f32x16 x[2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[g][e] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const bf16x8 kf = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(kb + g * 32 * D * 2 + koff[ks]));
+        x[g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], x[g], 0, 0, 0);
+      }
+    const int key0 = sp.key0(t);
+    if (!sp.open(key0)) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (!sp.sees(key0 + 32 * g + 8 * (e >> 2) + 4 * hh + (e & 3), pos)) x[g][e] = -INFINITY;
+    }
+    float mx = fmaxf(x[0][0], x[1][0]);
+#pragma unroll
+    for (int e = 1; e < 16; ++e) mx = fmaxf(fmaxf(mx, x[0][e]), x[1][e]);
+    {
+      float a0 = mx, b0 = mx;
+      lane_swap32(a0, b0);
+      mx = fmaxf(a0, b0) * a.sc;
+    }
+    // a column without a visible key so far keeps the reference -inf, used as 0
+    if (__any(mx > m + 8.f || (m == -INFINITY && mx != -INFINITY))) {
+      const float mm = fmaxf(m, mx), ref = mm == -INFINITY ? 0.f : mm;
+      const float f = __builtin_amdgcn_exp2f(m - ref);
+      m = mm;
+      l *= f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[dt][e] *= f;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    bf16x8 pf[4];
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float v = __builtin_amdgcn_exp2f(fmaf(x[g][e], a.sc, -ref));
+        l += v;
+        pf[2 * g + (e >> 3)][e & 7] = (__bf16)v;
+      }
+#pragma unroll
+    for (int ss = 0; ss < 4; ++ss)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const char* vs = vb + ss * 16 * D * 2;
+        const s16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + voff[dt][0]));
+        const s16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + voff[dt][1]));
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[ss], o[dt], 0, 0, 0);
+      }
+  }
+  {
+    float a0 = l, b0 = l;
+    lane_swap32(a0, b0);
+    l = a0 + b0;
+  }
+  if (!live) return;
+  if (a.S > 1) {
+    float* pp = a.part + ((((int64_t)b * p.HQ + j) * p.q_len + r) * a.S + split) * (D + 2);
+    if (hh == 0) {
+      pp[0] = m;
+      pp[1] = l;
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) pp[2 + 32 * dt + 8 * (e >> 2) + 4 * hh + (e & 3)] = o[dt][e];
+    return;
+  }
+  const float inv = m == -INFINITY ? 0.f : 1.f / l;
+  char* dst = p.out + ((int64_t)b * p.os[0] + (int64_t)j * p.os[1] + (int64_t)r * p.os[2]) * ES;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+      bf16x4 v;
+#pragma unroll
+      for (int f = 0; f < 4; ++f) v[f] = (__bf16)(o[dt][e + f] * inv);
+      *reinterpret_cast<bf16x4*>(dst + (32 * dt + 2 * e + 4 * hh) * 2) = v;
+    }
+  if (p.lse && hh == 0)
+    p.lse[(int64_t)b * p.ls[0] + (int64_t)j * p.ls[1] + r] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+
+template <class TT, int D>
+__global__ __launch_bounds__(kPfThreads, 2) void pf_rows32(PfArgs a) { rows32<TT, D>(a); }
+
 // Join the splits of one row: grid (q_len, HQ, batch), one thread per element.
 template <class T, int D>
 __global__ __launch_bounds__(D) void pf_join(PfArgs a) {
@@ -180,22 +416,26 @@ __global__ __launch_bounds__(D) void pf_join(PfArgs a) {
 }
 
 struct PfPlan {
+  bool wide;  // pf_rows32 instead of pf_rows16
   int S, tiles;
   size_t bytes;
 };
 
-// Splits over the keys: where the row tiles are fewer than 512 work-groups, as
-// many as that takes, of at least eight key tiles each.
+// Kernel and splits over the keys: where the row tiles are fewer than 512
+// work-groups, as many splits as that takes, of at least 256 keys each.
 PfPlan pf_plan(const PrefillArgs& a) {
   PfPlan pl;
-  pl.tiles = (int)(((int64_t)a.q_len * a.G + kPfRows - 1) / kPfRows);
+  const int64_t packed = (int64_t)a.q_len * a.G;
+  pl.wide = a.esize == 2 && packed > kPfRows;
+  const int rows = pl.wide ? kPf32Rows : kPfRows;
+  pl.tiles = (int)((packed + rows - 1) / rows);
   const int64_t groups = (int64_t)pl.tiles * a.batch * a.H;
   int64_t keys = a.kv_len;
   if (a.window > 0) {
-    const int64_t most = (int64_t)a.window + a.sinks + kPfRows;
+    const int64_t most = (int64_t)a.window + a.sinks + rows;
     if (most < keys) keys = most;
   }
-  const int64_t most_s = keys / (8 * kPfKeys);
+  const int64_t most_s = keys / 256;
   int64_t S = groups >= 512 ? 1 : (512 + groups - 1) / groups;
   if (S > most_s) S = most_s;
   if (S > 64) S = 64;
@@ -216,8 +456,11 @@ hipError_t run_prefill(const PrefillArgs& p, char* ws, hipStream_t s) {
   a.tiles = pl.tiles;
   a.part = reinterpret_cast<float*>(ws);
   a.sc = (float)(1.4426950408889634 / sqrt((double)p.D));
-  const dim3 grid((unsigned)(pl.tiles * pl.S), p.H, p.batch);
-  if (p.esize == 2) {
+  const dim3 grid(pf_grid(a));
+  if (pl.wide) {
+    if (p.D == 64) hipLaunchKernelGGL((pf_rows32<BF16, 64>), grid, dim3(kPfThreads), 0, s, a);
+    else hipLaunchKernelGGL((pf_rows32<BF16, 128>), grid, dim3(kPfThreads), 0, s, a);
+  } else if (p.esize == 2) {
     if (p.D == 64) hipLaunchKernelGGL((pf_rows16<BF16, 64>), grid, dim3(kPfThreads), 0, s, a);
     else hipLaunchKernelGGL((pf_rows16<BF16, 128>), grid, dim3(kPfThreads), 0, s, a);
   } else {

@@ -93,7 +93,7 @@ class kvec_paged_config(ctypes.Structure):
                                               "page_size", "n_pages", "max_pages", "dtype")]
 
 
-@dataclass
+@dataclass(frozen=True)
 class AttentionConfig:
     """Python view of kvec_attention_config."""
     batch: int
@@ -106,12 +106,18 @@ class AttentionConfig:
     n_sinks: int = 0
     dtype: int = KVEC_BF16
 
+    def __post_init__(self):
+        # what every call needs of the configuration, made once
+        q, k = (self.batch, self.n_q_heads, self.q_len), (self.batch, self.n_kv_heads, self.kv_len)
+        _fix(self, kvec_attention_config(self.batch, self.n_kv_heads, self.n_q_heads, self.head_dim,
+                                         self.q_len, self.kv_len, self.window, self.n_sinks, self.dtype),
+             q_shape=q + (self.head_dim,), k_shape=k + (self.head_dim,), lse_shape=q, len_shape=(self.batch,))
+
     def c(self) -> kvec_attention_config:
-        return kvec_attention_config(self.batch, self.n_kv_heads, self.n_q_heads, self.head_dim,
-                                     self.q_len, self.kv_len, self.window, self.n_sinks, self.dtype)
+        return self._c
 
 
-@dataclass
+@dataclass(frozen=True)
 class PagedConfig:
     """Python view of kvec_paged_config."""
     batch: int
@@ -123,9 +129,22 @@ class PagedConfig:
     max_pages: int
     dtype: int = KVEC_BF16
 
+    def __post_init__(self):
+        meta = (self.n_pages, self.n_kv_heads, self.page_size)
+        _fix(self, kvec_paged_config(self.batch, self.n_kv_heads, self.n_q_heads, self.head_dim,
+                                     self.page_size, self.n_pages, self.max_pages, self.dtype),
+             meta_shape=meta, pool_shape=meta + (self.head_dim,), table_shape=(self.batch, self.max_pages),
+             len_shape=(self.batch,), lse_shape=(self.batch, self.n_q_heads),
+             q_shape=(self.batch, self.n_q_heads, self.head_dim))
+
     def c(self) -> kvec_paged_config:
-        return kvec_paged_config(self.batch, self.n_kv_heads, self.n_q_heads, self.head_dim,
-                                 self.page_size, self.n_pages, self.max_pages, self.dtype)
+        return self._c
+
+
+def _fix(cfg, c, **more) -> None:
+    """Keeps the C view of a frozen configuration, a reference to it and the shapes it implies."""
+    for name, value in dict(_c=c, ref=ctypes.byref(c), **more).items():
+        object.__setattr__(cfg, name, value)
 
 
 _lib = None
@@ -426,39 +445,53 @@ def kvec_decode_attention_noalloc(cfg: Config, q, k_cache, v_cache, out, idx=Non
            "kvec_decode_attention_noalloc")
 
 
-def _rows(t, shape, dtype, what: str):
-    """Checks a tensor of rows (its last dimension contiguous); its leading element strides."""
-    assert tuple(t.shape) == tuple(shape), f"{what} must be {tuple(shape)}, not {tuple(t.shape)}"
-    assert t.dtype == dtype, f"{what} must be {dtype}"
-    return _strides(t, len(shape) - 1)
+_I64x2, _I64x3 = ctypes.c_int64 * 2, ctypes.c_int64 * 3
+
+
+def _rows2(t, shape, dtype, what: str):
+    """Checks a tensor [.][.][d] of rows, its last dimension contiguous; its leading strides."""
+    st = t.stride()
+    assert t.shape == shape, f"{what} must be {shape}, not {tuple(t.shape)}"
+    assert t.dtype is dtype and st[2] == 1, f"{what} must be {dtype}, its last dimension contiguous"
+    return _I64x2(st[0], st[1])
+
+
+def _rows3(t, shape, dtype, what: str):
+    """As _rows2 for [.][.][.][d]."""
+    st = t.stride()
+    assert t.shape == shape, f"{what} must be {shape}, not {tuple(t.shape)}"
+    assert t.dtype is dtype and st[3] == 1, f"{what} must be {dtype}, its last dimension contiguous"
+    return _I64x3(st[0], st[1], st[2])
 
 
 def _dense(t, shape, dtype, what: str) -> int | None:
     """Checks a contiguous tensor (None passes); its address."""
     if t is None:
         return None
-    assert tuple(t.shape) == tuple(shape) and t.is_contiguous(), \
-        f"{what} must be contiguous {tuple(shape)}, not {tuple(t.shape)}"
-    assert t.dtype == dtype, f"{what} must be {dtype}"
+    assert t.shape == shape and t.is_contiguous(), f"{what} must be contiguous {shape}, not {tuple(t.shape)}"
+    assert t.dtype is dtype, f"{what} must be {dtype}"
     return t.data_ptr()
 
 
-def _torch_dtype(dtype: int):
+def _call(name: str, stream, tensors, *args) -> None:
+    """The library's call `name` with the tensors' device current, on its current stream
+    unless one is given.  The tensors (None passes) must share one GPU."""
     import torch
-    return torch.bfloat16 if dtype == KVEC_BF16 else torch.float32
-
-
-def _on_device(t, tensors, stream, call, what: str) -> None:
-    """call(stream handle) with t's device current, on its current stream unless one is given."""
-    import torch
-    assert t.is_cuda, f"{what}: the tensors must be on a GPU"
-    for x in tensors:
-        assert x is None or x.device == t.device, f"{what}: the tensors must share a device"
-    if t.device.index == torch.cuda.current_device():
-        _check(call(_stream(stream)), what)
+    dev = tensors[0].get_device()
+    assert dev >= 0, f"{name}: the tensors must be on a GPU"
+    for t in tensors:
+        assert t is None or t.get_device() == dev, f"{name}: the tensors must share a device"
+    if dev == torch.cuda.current_device():
+        _check(getattr(load(), name)(*args, _stream(stream)), name)
     else:
-        with torch.cuda.device(t.device):
-            _check(call(_stream(stream)), what)
+        with torch.cuda.device(dev):
+            _check(getattr(load(), name)(*args, _stream(stream)), name)
+
+
+def _types(cfg):
+    """(element type, float32, int32) of a configuration's tensors."""
+    import torch
+    return torch.bfloat16 if cfg.dtype == KVEC_BF16 else torch.float32, torch.float32, torch.int32
 
 
 def _ws(ws):
@@ -467,8 +500,7 @@ def _ws(ws):
 
 def kvec_prefill_workspace_size(cfg: AttentionConfig) -> int:
     out = ctypes.c_size_t(0)
-    _check(load().kvec_prefill_workspace_size(ctypes.byref(cfg.c()), ctypes.byref(out)),
-           "kvec_prefill_workspace_size")
+    _check(load().kvec_prefill_workspace_size(cfg.ref, ctypes.byref(out)), "kvec_prefill_workspace_size")
     return out.value
 
 
@@ -477,26 +509,19 @@ def kvec_prefill_attention(cfg: AttentionConfig, q, k, v, out, ws=None, lse=None
     """q, out [b][HQ][q_len][d]; k, v [b][H][kv_len][d] (any leading strides); lse fp32
     [b][HQ][q_len], rows contiguous; q_lens, kv_lens int32 [b].  ws may be None when
     kvec_prefill_workspace_size(cfg) is 0."""
-    import torch
-    dt = _torch_dtype(cfg.dtype)
-    rows = (cfg.batch, cfg.n_q_heads, cfg.q_len, cfg.head_dim)
-    keys = (cfg.batch, cfg.n_kv_heads, cfg.kv_len, cfg.head_dim)
-    qs, os_ = _rows(q, rows, dt, "q"), _rows(out, rows, dt, "out")
-    ks, vs = _rows(k, keys, dt, "k"), _rows(v, keys, dt, "v")
-    ls = None if lse is None else _rows(lse, rows[:3], torch.float32, "lse")
-    ql = _dense(q_lens, (cfg.batch,), torch.int32, "q_lens")
-    kl = _dense(kv_lens, (cfg.batch,), torch.int32, "kv_lens")
-    lib, c, (wp, wn) = load(), cfg.c(), _ws(ws)
-    _on_device(q, (k, v, out, ws, lse, q_lens, kv_lens), stream, lambda st: lib.kvec_prefill_attention(
-        ctypes.byref(c), _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, ql, kl, _ptr(out), os_, _ptr(lse), ls, wp,
-        wn, st), "kvec_prefill_attention")
+    dt, f32, i32 = _types(cfg)
+    qs, os_ = _rows3(q, cfg.q_shape, dt, "q"), _rows3(out, cfg.q_shape, dt, "out")
+    ks, vs = _rows3(k, cfg.k_shape, dt, "k"), _rows3(v, cfg.k_shape, dt, "v")
+    ls = None if lse is None else _rows2(lse, cfg.lse_shape, f32, "lse")
+    ql, kl = _dense(q_lens, cfg.len_shape, i32, "q_lens"), _dense(kv_lens, cfg.len_shape, i32, "kv_lens")
+    wp, wn = _ws(ws)
+    _call("kvec_prefill_attention", stream, (q, k, v, out, ws, lse, q_lens, kv_lens), cfg.ref, q.data_ptr(), qs,
+          k.data_ptr(), ks, v.data_ptr(), vs, ql, kl, out.data_ptr(), os_, _ptr(lse), ls, wp, wn)
 
 
-def _pools(cfg: PagedConfig, k_pool, v_pool):
-    shape = (cfg.n_pages, cfg.n_kv_heads, cfg.page_size, cfg.head_dim)
-    dt = _torch_dtype(cfg.dtype)
-    ps = _rows(k_pool, shape, dt, "k_pool")
-    _rows(v_pool, shape, dt, "v_pool")
+def _pools(cfg: PagedConfig, dt, k_pool, v_pool):
+    ps = _rows3(k_pool, cfg.pool_shape, dt, "k_pool")
+    assert v_pool.shape == cfg.pool_shape and v_pool.dtype is dt, f"v_pool must be {cfg.pool_shape}, {dt}"
     assert k_pool.stride() == v_pool.stride(), "K and V pools share their strides"
     return ps
 
@@ -508,28 +533,31 @@ def kvec_paged_append(cfg: PagedConfig, q, k, v, positions, slots, q_out, k_pool
     [n_pages][H][page_size][d]; weights [d] (None: no norm); inv_freq float64 [rot_dim / 2]
     (None: no rotation); acc fp32 and pos int32 [n_pages][H][page_size]."""
     import torch
-    dt, n, d = _torch_dtype(cfg.dtype), q.shape[0], cfg.head_dim
-    qs, os_ = _rows(q, (n, cfg.n_q_heads, d), dt, "q"), _rows(q_out, (n, cfg.n_q_heads, d), dt, "q_out")
-    ks, vs = _rows(k, (n, cfg.n_kv_heads, d), dt, "k"), _rows(v, (n, cfg.n_kv_heads, d), dt, "v")
-    ps = _pools(cfg, k_pool, v_pool)
-    meta = (cfg.n_pages, cfg.n_kv_heads, cfg.page_size)
-    at, sl = _dense(positions, (n,), torch.int32, "positions"), _dense(slots, (n,), torch.int64, "slots")
+    dt, f32, i32 = _types(cfg)
+    n, d = q.shape[0], cfg.head_dim
+    queries, keys = (n, cfg.n_q_heads, d), (n, cfg.n_kv_heads, d)
+    qs, os_ = _rows2(q, queries, dt, "q"), _rows2(q_out, queries, dt, "q_out")
+    ks, vs = _rows2(k, keys, dt, "k"), _rows2(v, keys, dt, "v")
+    ps = _pools(cfg, dt, k_pool, v_pool)
+    at, sl = _dense(positions, (n,), i32, "positions"), _dense(slots, (n,), torch.int64, "slots")
     wq, wk = _dense(q_weight, (d,), dt, "q_weight"), _dense(k_weight, (d,), dt, "k_weight")
-    ac, po = _dense(acc, meta, torch.float32, "acc"), _dense(pos, meta, torch.int32, "pos")
-    rot = 0 if inv_freq is None else 2 * inv_freq.shape[0]
-    fr = None if inv_freq is None else _dense(inv_freq, (rot // 2,), torch.float64, "inv_freq")
-    lib, c = load(), cfg.c()
-    _on_device(k_pool, (q, k, v, positions, slots, q_out, v_pool, q_weight, k_weight, inv_freq, acc, pos),
-               stream, lambda st: lib.kvec_paged_append(
-        ctypes.byref(c), n, _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, wq, wk, eps, at, fr, rot, sl, _ptr(q_out),
-        os_, _ptr(k_pool), _ptr(v_pool), ps, ac, po, st), "kvec_paged_append")
+    ac, po = _dense(acc, cfg.meta_shape, f32, "acc"), _dense(pos, cfg.meta_shape, i32, "pos")
+    half = 0 if inv_freq is None else inv_freq.shape[0]
+    fr = _dense(inv_freq, (half,), torch.float64, "inv_freq")
+    _call("kvec_paged_append", stream, (k_pool, q, k, v, positions, slots, q_out, v_pool, q_weight, k_weight,
+                                        inv_freq, acc, pos),
+          cfg.ref, n, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, wq, wk, eps, at, fr, 2 * half, sl,
+          q_out.data_ptr(), os_, k_pool.data_ptr(), v_pool.data_ptr(), ps, ac, po)
+
+
+def _max_len(cfg: PagedConfig, max_len) -> int:
+    return cfg.max_pages * cfg.page_size if max_len is None else max_len
 
 
 def kvec_paged_decode_workspace_size(cfg: PagedConfig, max_len: int | None = None,
                                      with_acc: bool = False) -> int:
     out = ctypes.c_size_t(0)
-    n = cfg.max_pages * cfg.page_size if max_len is None else max_len
-    _check(load().kvec_paged_decode_workspace_size(ctypes.byref(cfg.c()), n, int(with_acc),
+    _check(load().kvec_paged_decode_workspace_size(cfg.ref, _max_len(cfg, max_len), int(with_acc),
                                                    ctypes.byref(out)), "kvec_paged_decode_workspace_size")
     return out.value
 
@@ -538,26 +566,21 @@ def kvec_paged_decode(cfg: PagedConfig, q, k_pool, v_pool, page_table, lens, out
                       window=0, n_sinks=0, lse=None, acc=None, stream=None) -> None:
     """q [b][HQ][d]; pools [n_pages][H][page_size][d] (K and V with the same strides);
     page_table int32 [b][max_pages]; lens int32 [b]; out fp32 [b][HQ][d]; lse fp32
-    [b][HQ]; acc fp32 [n_pages][H][page_size]."""
-    import torch
-    b, HQ, d = cfg.batch, cfg.n_q_heads, cfg.head_dim
-    qs, ps = _rows(q, (b, HQ, d), _torch_dtype(cfg.dtype), "q"), _pools(cfg, k_pool, v_pool)
-    tb = _dense(page_table, (b, cfg.max_pages), torch.int32, "page_table")
-    ln, op = _dense(lens, (b,), torch.int32, "lens"), _dense(out, (b, HQ, d), torch.float32, "out")
-    lp = _dense(lse, (b, HQ), torch.float32, "lse")
-    ac = _dense(acc, (cfg.n_pages, cfg.n_kv_heads, cfg.page_size), torch.float32, "acc")
-    n = cfg.max_pages * cfg.page_size if max_len is None else max_len
-    lib, c, (wp, wn) = load(), cfg.c(), _ws(ws)
-    _on_device(q, (k_pool, v_pool, page_table, lens, out, ws, lse, acc), stream,
-               lambda st: lib.kvec_paged_decode(ctypes.byref(c), _ptr(q), qs, _ptr(k_pool), _ptr(v_pool), ps,
-                                                tb, ln, n, window, n_sinks, op, lp, ac, wp, wn, st),
-               "kvec_paged_decode")
+    [b][HQ]; acc fp32 [n_pages][H][page_size].  max_len None: every slot of the table."""
+    dt, f32, i32 = _types(cfg)
+    qs, ps = _rows2(q, cfg.q_shape, dt, "q"), _pools(cfg, dt, k_pool, v_pool)
+    tb, ln = _dense(page_table, cfg.table_shape, i32, "page_table"), _dense(lens, cfg.len_shape, i32, "lens")
+    op, lp = _dense(out, cfg.q_shape, f32, "out"), _dense(lse, cfg.lse_shape, f32, "lse")
+    ac = _dense(acc, cfg.meta_shape, f32, "acc")
+    wp, wn = _ws(ws)
+    _call("kvec_paged_decode", stream, (q, k_pool, v_pool, page_table, lens, out, ws, lse, acc), cfg.ref,
+          q.data_ptr(), qs, k_pool.data_ptr(), v_pool.data_ptr(), ps, tb, ln, _max_len(cfg, max_len), window,
+          n_sinks, op, lp, ac, wp, wn)
 
 
 def kvec_paged_evict_workspace_size(cfg: PagedConfig, max_len: int | None, budget: int) -> int:
     out = ctypes.c_size_t(0)
-    n = cfg.max_pages * cfg.page_size if max_len is None else max_len
-    _check(load().kvec_paged_evict_workspace_size(ctypes.byref(cfg.c()), n, budget, ctypes.byref(out)),
+    _check(load().kvec_paged_evict_workspace_size(cfg.ref, _max_len(cfg, max_len), budget, ctypes.byref(out)),
            "kvec_paged_evict_workspace_size")
     return out.value
 
@@ -567,16 +590,13 @@ def kvec_paged_evict(cfg: PagedConfig, budget: int, k_pool, v_pool, page_table, 
     """Pools and tables as in kvec_paged_decode; acc fp32 and pos int32
     [n_pages][H][page_size]; lens, n_seen, lens_out int32 [b] (lens_out may be lens);
     kept int32 [b][H][budget]."""
-    import torch
-    b, H = cfg.batch, cfg.n_kv_heads
-    ps, meta = _pools(cfg, k_pool, v_pool), (cfg.n_pages, H, cfg.page_size)
-    tb = _dense(page_table, (b, cfg.max_pages), torch.int32, "page_table")
-    ln, ns = _dense(lens, (b,), torch.int32, "lens"), _dense(n_seen, (b,), torch.int32, "n_seen")
-    lo, ac = _dense(lens_out, (b,), torch.int32, "lens_out"), _dense(acc, meta, torch.float32, "acc")
-    po, kp = _dense(pos, meta, torch.int32, "pos"), _dense(kept, (b, H, budget), torch.int32, "kept")
-    n = cfg.max_pages * cfg.page_size if max_len is None else max_len
-    lib, c, (wp, wn) = load(), cfg.c(), _ws(ws)
-    _on_device(k_pool, (v_pool, page_table, lens, n_seen, acc, pos, lens_out, ws, kept), stream,
-               lambda st: lib.kvec_paged_evict(ctypes.byref(c), budget, window, n_sinks, _ptr(k_pool),
-                                               _ptr(v_pool), ps, tb, ln, ns, n, ac, po, kp, lo, wp, wn, st),
-               "kvec_paged_evict")
+    dt, f32, i32 = _types(cfg)
+    ps = _pools(cfg, dt, k_pool, v_pool)
+    tb, ln = _dense(page_table, cfg.table_shape, i32, "page_table"), _dense(lens, cfg.len_shape, i32, "lens")
+    ns, lo = _dense(n_seen, cfg.len_shape, i32, "n_seen"), _dense(lens_out, cfg.len_shape, i32, "lens_out")
+    ac, po = _dense(acc, cfg.meta_shape, f32, "acc"), _dense(pos, cfg.meta_shape, i32, "pos")
+    kp = _dense(kept, (cfg.batch, cfg.n_kv_heads, budget), i32, "kept")
+    wp, wn = _ws(ws)
+    _call("kvec_paged_evict", stream, (k_pool, v_pool, page_table, lens, n_seen, acc, pos, lens_out, ws, kept),
+          cfg.ref, budget, window, n_sinks, k_pool.data_ptr(), v_pool.data_ptr(), ps, tb, ln, ns,
+          _max_len(cfg, max_len), ac, po, kp, lo, wp, wn)
