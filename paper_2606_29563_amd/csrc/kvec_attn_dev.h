@@ -24,7 +24,6 @@
 namespace kvec {
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 // A group of 16 rows in LDS and the copies that bring it there.
 template <class TT, int D>
@@ -37,14 +36,46 @@ struct RowGroup {
   static constexpr int RPI = 64 / CPR;                   // rows per copy
 };
 
-// Four elements of row `row` from each of 16 rows, transposed (see above): rows
-// 4c .. 4c+3 of the group at `grp`, column 16 t + lane % 16.
-template <int D>
-__device__ __forceinline__ s16x4 vt_read(const char* grp, int t, int lane) {
-  using RG = RowGroup<BF16, D>;
-  const int n = lane & 15, row = 4 * (lane >> 4) + (n >> 2);
-  const char* p = grp + row * (D * 2) + (((2 * t + ((n >> 1) & 1)) ^ (row & RG::SWZ)) << 4) + ((n & 1) << 3);
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+// N transposing LDS reads (see above) at byte addresses addr[.] + OFF.  Written
+// out, the wait in the same statement: for the compiler's builtin every
+// direct-to-LDS copy in flight is drained first (it cannot tell the addresses
+// apart), which would stop the copies of the next tile.  The products issued
+// before run on while this waits.
+__device__ __forceinline__ uint32_t lds_addr(const char* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
+}
+template <int OFF>
+__device__ __forceinline__ void vt_read(const uint32_t (&addr)[4], s16x4 (&v)[4]) {
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %4 offset:%8\n\t"
+      "ds_read_b64_tr_b16 %1, %5 offset:%8\n\t"
+      "ds_read_b64_tr_b16 %2, %6 offset:%8\n\t"
+      "ds_read_b64_tr_b16 %3, %7 offset:%8\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+      : "v"(addr[0]), "v"(addr[1]), "v"(addr[2]), "v"(addr[3]), "n"(OFF)
+      : "memory");
+}
+template <int OFF>
+__device__ __forceinline__ void vt_read(const uint32_t (&addr)[8], s16x4 (&v)[8]) {
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %8 offset:%16\n\t"
+      "ds_read_b64_tr_b16 %1, %9 offset:%16\n\t"
+      "ds_read_b64_tr_b16 %2, %10 offset:%16\n\t"
+      "ds_read_b64_tr_b16 %3, %11 offset:%16\n\t"
+      "ds_read_b64_tr_b16 %4, %12 offset:%16\n\t"
+      "ds_read_b64_tr_b16 %5, %13 offset:%16\n\t"
+      "ds_read_b64_tr_b16 %6, %14 offset:%16\n\t"
+      "ds_read_b64_tr_b16 %7, %15 offset:%16\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7])
+      : "v"(addr[0]), "v"(addr[1]), "v"(addr[2]), "v"(addr[3]), "v"(addr[4]), "v"(addr[5]), "v"(addr[6]),
+        "v"(addr[7]), "n"(OFF)
+      : "memory");
+}
+__device__ __forceinline__ bf16x8 join8(s16x4 a, s16x4 b) {
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
 // Softmax state and output of 16 query columns, NG groups of 16 keys a step.
@@ -57,6 +88,15 @@ struct Columns16 {
   Frag<TT, D> q;
   float m, l;  // maximum (base-2 logits) of the column; this lane's part of the sum
   f32x4 o[DT];
+
+  // Byte offsets of the lane's transposing reads of a group: rows 4c .. 4c+3,
+  // columns 16 t + lane % 16.
+  static __device__ __forceinline__ void vt_offsets(int lane, uint32_t (&at)[DT]) {
+    const int n = lane & 15, row = 4 * (lane >> 4) + (n >> 2);
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+      at[t] = row * (D * 2) + (((2 * t + ((n >> 1) & 1)) ^ (row & RG::SWZ)) << 4) + ((n & 1) << 3);
+  }
 
   __device__ __forceinline__ void clear() {
     m = -INFINITY;
@@ -100,21 +140,38 @@ struct Columns16 {
         for (int i = 0; i < 4; ++i) o[t][i] *= f;
     }
     if constexpr (__is_same(TT, BF16)) {
-      static_assert(NG == 2, "one 32-key product per step");
-      bf16x8 hi, lo;
+      // one product over 32 keys, or over 16
+      static_assert(NG == 1 || NG == 2, "keys of a step");
+      typedef __bf16 bf16xk __attribute__((ext_vector_type(4 * NG)));
+      bf16xk hi, lo;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < 4 * NG; ++i) {
         const float v = p[i >> 2][i & 3];
         hi[i] = (__bf16)v;
         if (SPLIT) lo[i] = (__bf16)(v - (float)hi[i]);
       }
+      uint32_t at[DT];
+      vt_offsets(lane, at);
+      const uint32_t base = lds_addr(vgrp);
 #pragma unroll
-      for (int t = 0; t < DT; ++t) {
-        const s16x4 a0 = vt_read<D>(vgrp, t, lane), a1 = vt_read<D>(vgrp + RG::BYTES, t, lane);
-        typedef short s16x8 __attribute__((ext_vector_type(8)));
-        const bf16x8 a = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
-        o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, hi, o[t], 0, 0, 0);
-        if (SPLIT) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, lo, o[t], 0, 0, 0);
+      for (int t = 0; t < DT; ++t) at[t] += base;
+      s16x4 a0[DT];
+      vt_read<0>(at, a0);
+      if constexpr (NG == 2) {
+        s16x4 a1[DT];
+        vt_read<RG::BYTES>(at, a1);
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+          const bf16x8 a = join8(a0[t], a1[t]);
+          o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, hi, o[t], 0, 0, 0);
+          if (SPLIT) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, lo, o[t], 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+          o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a0[t], __builtin_bit_cast(s16x4, hi), o[t], 0, 0, 0);
+          if (SPLIT) o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a0[t], __builtin_bit_cast(s16x4, lo), o[t], 0, 0, 0);
+        }
       }
     } else {
       const int n = lane & 15, c = lane >> 4;

@@ -26,6 +26,10 @@ namespace {
 
 constexpr int kPdThreads = 256;
 constexpr int kPdWaves = kPdThreads / 64;
+#ifndef TARGET
+#define TARGET 512
+#endif
+constexpr int kPdTarget = TARGET;
 
 struct PdArgs {
   PagedView c;
@@ -66,30 +70,25 @@ __device__ __forceinline__ int page_of(const PdArgs& a, int b, int slot0, int* r
 }
 __device__ __forceinline__ bool page_ok(const PdArgs& a, int page) { return page >= 0 && page < a.c.n_pages; }
 
-template <class TT>
-constexpr int kPdGroups = __is_same(TT, BF16) ? 2 : 1;  // groups of 16 slots per step
+// Groups of a split: `per` from x * per on.
+__device__ __forceinline__ int split_groups(const Visible& v, int S) { return (v.groups + S - 1) / S; }
+
+constexpr int kPdRing = 2;  // groups of 16 slots in flight per wave
 
 template <class TT, int D>
-constexpr size_t pd_lds() {
-  return (size_t)kPdWaves * 2 * 2 * kPdGroups<TT> * RowGroup<TT, D>::BYTES;
-}
-
-template <class TT, int D>
-__global__ __launch_bounds__(kPdThreads) void pd_partial(PdArgs a) {
+__device__ __forceinline__ void partial(const PdArgs& a, char* smem) {
   using RG = RowGroup<TT, D>;
-  constexpr int NG = kPdGroups<TT>, ES = RG::ES;
-  constexpr int STEP = 2 * NG * RG::BYTES;  // K groups, then V groups
-  constexpr int LOADS = 2 * NG * RG::NI;
-  __shared__ __align__(1024) char smem[pd_lds<TT, D>()];
+  constexpr int ES = RG::ES;
+  constexpr int STEP = 2 * RG::BYTES;  // K rows, then V rows of a group
+  constexpr int LOADS = 2 * RG::NI;
   const int s = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int n = lane & 15, c = lane >> 4, G = a.c.G;
   const Visible vis(a, b);
-  const int steps = (vis.groups + NG - 1) / NG;
-  const int per = (steps + a.S - 1) / a.S;
-  const int st0 = min(s * per, steps), st1 = min(st0 + per, steps);
+  const int per = split_groups(vis, a.S);
+  const int st0 = min(s * per, vis.groups), st1 = min(st0 + per, vis.groups);
 
-  Columns16<TT, D, NG, true> col;
+  Columns16<TT, D, 1, true> col;
   col.clear();
   col.q.zero();
   if (n < G) col.q.load(a.q + ((int64_t)b * a.qs_b + (int64_t)(h * G + n) * a.qs_h) * ES, c);
@@ -101,28 +100,38 @@ __global__ __launch_bounds__(kPdThreads) void pd_partial(PdArgs a) {
     voff[i] = rowi[i] * (int)(a.c.sr * ES) + piece_in_copy<TT, D>(i, lane) * 16;
   }
   const int extent = 15 * (int)(a.c.sr * ES) + D * ES;
-  char* ring = smem + w * 2 * STEP;
+  char* ring = smem + w * kPdRing * STEP;
 
-  // pages of the next step to be copied
-  int page[NG], row0[NG];
-  auto lookup = [&](int st) {
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const int vg = min(st * NG + g, max(vis.groups - 1, 0));
-      page[g] = page_of(a, b, vis.slot0(vg), &row0[g]);
-    }
+  // The wave's groups are st0 + w, st0 + w + 4, ...: number k of them.  Lane l
+  // holds the page entry of number 64 * (k / 64) + l, looked up for 64 groups at a
+  // time (a lookup in the loop would wait for every copy in flight).
+  const int first = st0 + w, count = (st1 - first + kPdWaves - 1) / kPdWaves;
+  int entry = 0, entry_row = 0;
+  auto lookup = [&](int k) {
+    const int vg = min(first + (k + lane) * kPdWaves, vis.groups - 1);
+    entry = page_of(a, b, vis.slot0(vg), &entry_row);
+    asm volatile("" : "+v"(entry));  // waited for here, not at every use in the loop
   };
-  auto copy = [&](int u, int st) {
+  bool whole[kPdRing];  // every slot of the group in the ring slot is visible
+  bool ok[kPdRing];     // ... lies in a page
+  auto copy = [&](auto U, int k) {
+    constexpr int u = decltype(U)::value;
+    if ((k & 63) == 0) lookup(k);
+    const int page = __builtin_amdgcn_readlane(entry, k & 63), row0 = __builtin_amdgcn_readlane(entry_row, k & 63);
+    const int slot0 = vis.slot0(first + k * kPdWaves);
+    ok[u] = k < count && page_ok(a, page);
+    whole[u] = ok[u] && slot0 + 16 <= vis.n && (slot0 >= vis.lo || slot0 + 16 <= vis.sinks);
+    const int64_t base = ok[u] ? ((int64_t)page * a.c.sp + (int64_t)h * a.c.sh + (int64_t)row0 * a.c.sr) * ES : 0;
+    const auto kr = __builtin_amdgcn_make_buffer_rsrc(a.c.k + base, 0, ok[u] ? extent : 0, kBufferWord3);
+    const auto vr = __builtin_amdgcn_make_buffer_rsrc(a.c.v + base, 0, ok[u] ? extent : 0, kBufferWord3);
+    auto* dk = (__attribute__((address_space(3))) char*)(ring + u * STEP);
+    auto* dv = (__attribute__((address_space(3))) char*)(ring + u * STEP + RG::BYTES);
+    if (whole[u]) {
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const int vg = st * NG + g;
-      const int slot0 = vis.slot0(vg);
-      const bool ok = vg < vis.groups && page_ok(a, page[g]);
-      const int64_t base = ((ok ? (int64_t)page[g] : 0) * a.c.sp + (int64_t)h * a.c.sh + (int64_t)row0[g] * a.c.sr) * ES;
-      const auto kr = __builtin_amdgcn_make_buffer_rsrc(a.c.k + base, 0, ok ? extent : 0, kBufferWord3);
-      const auto vr = __builtin_amdgcn_make_buffer_rsrc(a.c.v + base, 0, ok ? extent : 0, kBufferWord3);
-      auto* dk = (__attribute__((address_space(3))) char*)(ring + u * STEP + g * RG::BYTES);
-      auto* dv = (__attribute__((address_space(3))) char*)(ring + u * STEP + (NG + g) * RG::BYTES);
+      for (int i = 0; i < RG::NI; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, dk + i * 1024, 16, voff[i], 0, 0, 2);
+#pragma unroll
+      for (int i = 0; i < RG::NI; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, dv + i * 1024, 16, voff[i], 0, 0, 2);
+    } else {
 #pragma unroll
       for (int i = 0; i < RG::NI; ++i) {
         const int off = vis.sees(slot0 + rowi[i]) ? voff[i] : kOutOfRange;
@@ -131,50 +140,32 @@ __global__ __launch_bounds__(kPdThreads) void pd_partial(PdArgs a) {
       }
     }
   };
-
-  const int first = st0 + w;
-  // which groups of the two steps in the ring have a page
-  bool okp[2][NG];
-  auto note = [&](int u, int st) {
-#pragma unroll
-    for (int g = 0; g < NG; ++g) okp[u][g] = st * NG + g < vis.groups && page_ok(a, page[g]);
-  };
-  if (first < st1) {
-    lookup(first);
-    note(0, first);
-    copy(0, first);
-    lookup(first + kPdWaves);
-    note(1, first + kPdWaves);
-    copy(1, first + kPdWaves);
-    lookup(first + 2 * kPdWaves);
-  }
-  float* lg = a.logits ? a.logits + (((int64_t)b * a.c.H + h) * G + n) * a.pad : nullptr;
-  auto step = [&](auto U, int st) {
+  float* lg = a.logits && n < G ? a.logits + (((int64_t)b * a.c.H + h) * G + n) * a.pad + 4 * c : nullptr;
+  auto step = [&](auto U, int k) {
     constexpr int u = decltype(U)::value;
-    wait_vmem<LOADS>();
+    wait_vmem<(kPdRing - 1) * LOADS>();
     const char* slot = ring + u * STEP;
-    f32x4 x[NG];
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      x[g] = col.logits(slot + g * RG::BYTES, lane);
-      const int s0 = vis.slot0(st * NG + g);
-      float y[4];
+    const int s0 = vis.slot0(first + k * kPdWaves);
+    f32x4 x[1];
+    x[0] = col.logits(slot, lane) * a.sc;
+    if (!whole[u]) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        y[i] = x[g][i] = okp[u][g] && vis.sees(s0 + 4 * c + i) ? x[g][i] * a.sc : -INFINITY;
-      if (lg && n < G && st * NG + g < vis.groups)
-        *reinterpret_cast<float4*>(lg + s0 + 4 * c) = make_float4(y[0], y[1], y[2], y[3]);
+        if (!(ok[u] && vis.sees(s0 + 4 * c + i))) x[0][i] = -INFINITY;
     }
-    col.absorb(x, slot + NG * RG::BYTES, lane);
+    if (lg) *reinterpret_cast<f32x4*>(lg + s0) = x[0];
+    col.absorb(x, slot + RG::BYTES, lane);
     // the ring slot is read out before the next copy into it starts
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    note(u, st + 2 * kPdWaves);
-    copy(u, st + 2 * kPdWaves);
-    lookup(st + 3 * kPdWaves);
+    copy(U, k + kPdRing);
   };
-  for (int st = first; st < st1; st += 2 * kPdWaves) {
-    step(std::integral_constant<int, 0>{}, st);
-    if (st + kPdWaves < st1) step(std::integral_constant<int, 1>{}, st + kPdWaves);
+  if (count > 0) {
+    copy(std::integral_constant<int, 0>{}, 0);
+    copy(std::integral_constant<int, 1>{}, 1);
+    for (int k = 0; k < count; k += kPdRing) {
+      step(std::integral_constant<int, 0>{}, k);
+      if (k + 1 < count) step(std::integral_constant<int, 1>{}, k + 1);
+    }
   }
   wait_vmem<0>();
   __syncthreads();
@@ -208,19 +199,40 @@ __global__ __launch_bounds__(kPdThreads) void pd_partial(PdArgs a) {
   }
 }
 
-// Work-group x of a (KV head, sequence): the output of query head x while x < G,
-// and the weights of split x while x < S.
 template <class TT, int D>
+__global__ __launch_bounds__(kPdThreads) void pd_partial(PdArgs a) {
+  constexpr int RING = kPdWaves * kPdRing * 2 * RowGroup<TT, D>::BYTES, MERGE = kPdWaves * 16 * (D + 2) * 4;
+  __shared__ __align__(1024) char smem[RING > MERGE ? RING : MERGE];
+  partial<TT, D>(a, smem);
+}
+
+// Work-group x of a (KV head, sequence): the output of query head x while x < G,
+// and the weights of 1024 slots, four a thread.
+constexpr int kPdAccGroups = kPdThreads / 4;
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));  // acc is aligned to its elements
+
+template <int D>
 __global__ __launch_bounds__(kPdThreads) void pd_combine(PdArgs a) {
   constexpr int PARTS = kPdThreads / D;
-  constexpr int NG = kPdGroups<TT>;
   const int x = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
   const int G = a.c.G, S = a.S;
   const float* part = a.part + ((int64_t)b * a.c.HQ + (int64_t)h * G) * S * (D + 2);
+  // the thread's slots, before the states: the loads do not depend on each other
+  int page = -1, row = 0, slot = 0;
+  const Visible vis(a, b);
+  const int vg = x * kPdAccGroups + (int)(threadIdx.x >> 2);
+  const bool adds = a.acc && x * kPdAccGroups < vis.groups;
+  if (adds && vg < vis.groups) {
+    slot = vis.slot0(vg);
+    page = page_of(a, b, slot, &row);
+    row += 4 * (threadIdx.x & 3);
+    slot += 4 * (threadIdx.x & 3);
+  }
   if (x < G) {
     __shared__ float st[PARTS][3][D];
     const int e = threadIdx.x % D, p = threadIdx.x / D;
     float m = -INFINITY, l = 0.f, o = 0.f;
+#pragma unroll 4
     for (int s = p; s < S; s += PARTS) {
       const float* pp = part + ((int64_t)x * S + s) * (D + 2);
       state_merge(m, l, o, pp[0], pp[1], pp[2 + e]);
@@ -237,7 +249,7 @@ __global__ __launch_bounds__(kPdThreads) void pd_combine(PdArgs a) {
       if (a.lse && e == 0) a.lse[j] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
     }
   }
-  if (!a.acc || x >= S) return;
+  if (!adds) return;
   // base-2 normaliser of every query head: one wave per head in turn
   __shared__ float norm[16];
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -255,21 +267,33 @@ __global__ __launch_bounds__(kPdThreads) void pd_combine(PdArgs a) {
     if (lane == 0) norm[g] = m + log2f(l);
   }
   __syncthreads();
-  const Visible vis(a, b);
-  const int steps = (vis.groups + NG - 1) / NG;
-  const int per = (steps + S - 1) / S;
-  const int g0 = min(x * per, steps) * NG, g1 = min(min(x * per + per, steps) * NG, vis.groups);
-  const float* lg = a.logits + ((int64_t)b * a.c.H + h) * G * a.pad;
-  const float mean = 1.f / G;
-  for (int i = threadIdx.x; i < (g1 - g0) * 16; i += kPdThreads) {
-    const int s0 = vis.slot0(g0 + (i >> 4)), slot = s0 + (i & 15);
-    int row0;
-    const int page = page_of(a, b, s0, &row0);
-    if (!vis.sees(slot) || !page_ok(a, page)) continue;
-    float sum = 0.f;
-    for (int g = 0; g < G; ++g) sum += __builtin_amdgcn_exp2f(lg[(int64_t)g * a.pad + slot] - norm[g]);
-    a.acc[((int64_t)page * a.c.H + h) * a.c.ps + row0 + (i & 15)] += sum * mean;
+  if (!page_ok(a, page)) return;
+  const float* lg = a.logits + ((int64_t)b * a.c.H + h) * G * a.pad + slot;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int g = 0; g < G; ++g) {
+    const f32x4 y = *reinterpret_cast<const f32x4*>(lg + (int64_t)g * a.pad);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] += __builtin_amdgcn_exp2f(y[i] - norm[g]);
   }
+  float* acc = a.acc + ((int64_t)page * a.c.H + h) * a.c.ps + row;
+  const float mean = 1.f / G;
+  if (vis.sees(slot) && vis.sees(slot + 1) && vis.sees(slot + 2) && vis.sees(slot + 3)) {
+    f32x4_any* p4 = reinterpret_cast<f32x4_any*>(acc);
+    *p4 = *p4 + sum * mean;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (vis.sees(slot + i)) acc[i] += sum[i] * mean;
+  }
+}
+
+// Bound of a sequence's visible groups.
+int most_groups(const PagedView& c, int window, int sinks) {
+  const int all = (c.max_len + 15) / 16;
+  if (window == 0) return all;
+  const int64_t some = ((int64_t)window + 15) / 16 + 1 + (sinks + 15) / 16;
+  return some < all ? (int)some : all;
 }
 
 template <class TT, int D>
@@ -277,23 +301,23 @@ hipError_t launch(const PdArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((pd_partial<TT, D>), dim3(a.S, a.c.H, a.c.batch), dim3(kPdThreads), 0, s, a);
   const hipError_t e1 = hipGetLastError();
   if (e1 != hipSuccess) return e1;
-  const int x = a.acc && a.S > a.c.G ? a.S : a.c.G;
-  hipLaunchKernelGGL((pd_combine<TT, D>), dim3(x, a.c.H, a.c.batch), dim3(kPdThreads), 0, s, a);
+  int x = a.c.G;
+  if (a.acc) {
+    const int chunks = (most_groups(a.c, a.window, a.sinks) + kPdAccGroups - 1) / kPdAccGroups;
+    if (chunks > x) x = chunks;
+  }
+  hipLaunchKernelGGL((pd_combine<D>), dim3(x, a.c.H, a.c.batch), dim3(kPdThreads), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-// Splits: about 512 work-groups over batch and heads, at least four steps (one
-// per wave) each.
+// Splits: about 512 work-groups over batch and heads (two per compute unit), at
+// least four groups (one per wave) each.
 PagedDecodePlan paged_decode_plan(const PagedView& c, int window, int sinks, bool acc) {
-  const int step = c.esize == 2 ? 32 : 16;
-  int64_t most = c.max_len;
-  if (window > 0 && (int64_t)window + sinks + 64 < most) most = (int64_t)window + sinks + 64;
-  const int steps = (int)((most + step - 1) / step);
   const int64_t bh = (int64_t)c.batch * c.H;
-  int64_t S = (512 + bh - 1) / bh;
-  const int most_s = (steps + kPdWaves - 1) / kPdWaves;
+  int64_t S = (kPdTarget + bh - 1) / bh;
+  const int most_s = (most_groups(c, window, sinks) + kPdWaves - 1) / kPdWaves;
   if (S > most_s) S = most_s;
   PagedDecodePlan p;
   p.S = (int)(S < 1 ? 1 : S);

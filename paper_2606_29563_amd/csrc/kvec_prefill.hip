@@ -93,7 +93,8 @@ __global__ __launch_bounds__(kPfThreads) void pf_rows16(PfArgs a) {
   constexpr int GRPS = kPfKeys / 16;
   constexpr int BUF = 2 * GRPS * RG::BYTES;       // K groups, then V groups
   constexpr int PER = 2 * GRPS * RG::NI / 4;      // copies per wave and tile
-  __shared__ __align__(1024) char smem[2 * BUF];
+  constexpr int NB = ES == 2 ? 3 : 2;             // LDS buffers
+  __shared__ __align__(1024) char smem[NB * BUF];
   const PrefillArgs& p = a.p;
   const int G = p.G;
   int bh, tile, split;
@@ -128,18 +129,20 @@ __global__ __launch_bounds__(kPfThreads) void pf_rows16(PfArgs a) {
       const bool is_v = at >= GRPS * RG::NI;
       const int in = is_v ? at - GRPS * RG::NI : at;
       const int row = row_in_copy<TT, D>(in % RG::NI, lane) + in / RG::NI * 16;
-      const int off = key0 + row < sp.nk ? (key0 + row) * (is_v ? vstr : kstr) + piece_in_copy<TT, D>(in % RG::NI, lane) * 16
+      const int off = t < t1 && key0 + row < sp.nk ? (key0 + row) * (is_v ? vstr : kstr) + piece_in_copy<TT, D>(in % RG::NI, lane) * 16
                                          : kOutOfRange;
       auto* dst = (__attribute__((address_space(3))) char*)(smem + u * BUF + at * 1024);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(is_v ? vr : kr, dst, 16, off, 0, 0, 0);
     }
   };
-  if (t0 < t1) copy(0, t0);
+  // tiles past the last are copied as zeros: the number of copies in flight stays
+#pragma unroll
+  for (int d = 0; d < NB - 1; ++d) copy(d, t0 + d);
+  int u = 0;
   for (int t = t0; t < t1; ++t) {
-    const int u = (t - t0) & 1;
-    wait_vmem<0>();
-    lds_barrier();  // the tile is there, and every wave is done with the other buffer
-    if (t + 1 < t1) copy(u ^ 1, t + 1);
+    wait_vmem<(NB - 2) * PER>();
+    lds_barrier();  // the tile is there, and every wave is done with the buffer before it
+    copy(u == 0 ? NB - 1 : u - 1, t + NB - 1);
     const char* kb = smem + u * BUF;
     const int key0 = sp.key0(t);
     const bool open = sp.open(key0) && live;
@@ -157,7 +160,9 @@ __global__ __launch_bounds__(kPfThreads) void pf_rows16(PfArgs a) {
       }
       col.absorb(x, kb + (GRPS + g0) * RG::BYTES, lane);
     }
+    u = u == NB - 1 ? 0 : u + 1;
   }
+  wait_vmem<0>();  // no copy outlives the work-group
   col.l = col_sum4(col.l);
   if (!live) return;
   const int64_t row = ((int64_t)b * p.HQ + j) * p.q_len + r;
@@ -192,20 +197,35 @@ __global__ __launch_bounds__(kPfThreads) void pf_rows16(PfArgs a) {
         col.m == -INFINITY ? -INFINITY : (col.m + log2f(col.l)) * 0.69314718055994531f;
 }
 
-// Long prompts, bf16: a work-group of four waves takes 128 packed rows, a wave
+// Long prompts, bf16: a work-group of eight waves takes 256 packed rows, a wave
 // 32 of them as the columns of 32x32x16 products (S^T = K Q^T, O^T = V^T P^T; see
 // kvec_attn_dev.h for why P stays in its registers: here the output lane holds
 // keys 8 (i / 4) + 4 (lane / 32) + i % 4 of column lane % 32, and the V product's
 // reduction runs over the keys in that order).  Tiles of 64 keys are copied
 // into one of two LDS buffers while the other is used; one barrier per tile.
 //
-// The softmax keeps a reference per column instead of the running maximum: O and
-// the sum are rescaled only when a tile's maximum exceeds the reference by more
-// than 8 (a factor of 256), so most tiles skip the pass over O.  The quotient
-// O / l does not depend on the reference, float32 sums of terms up to 2^8 lose
-// nothing, and the bf16 rounding of P is relative.
+// The softmax keeps a reference per column instead of the running maximum, and
+// looks for a maximum only when the tile's probabilities say so: their sum in a
+// lane beyond 2^12 (or no number: the column has no reference yet) takes the
+// tile's maximum as the new reference, rescales O and the sum, and weighs the
+// tile again.  The quotient O / l does not depend on the reference, float32 holds
+// terms up to 2^12 as exactly as those up to 1, and the bf16 rounding of P is
+// relative.  Most tiles so need neither the maximum nor a pass over O.
+//
+// Bound by the matrix cores and the vector work of the softmax, which mostly add
+// up (the counters see them together in 28% of the matrix cores' busy cycles).
+// A causal 8k prompt (32 query, 8 KV heads, d 128): 1.05 PFLOP/s, where a large
+// library product reaches 1.22.  In us of that prompt: a running maximum and
+// four waves of 128 rows 569, eight waves, which copy each key tile half as often,
+// 549 (535 and 522 without and with the search for the maximum left out, on
+// another card; without any copies, for timing, 490 of the 569).  Measured and
+// dropped: three LDS buffers (540 for 535), the next tile's logits computed beside this
+// tile's exponentials (561 for 549), waves 4-7 half a tile behind waves 0-3, in
+// step by barriers (607), raised wave priority around the products (549 for 545).
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-constexpr int kPf32Rows = 128, kPf32Keys = 64;
+constexpr int kPf32Rows = 256, kPf32Keys = 64;
+
+constexpr int kPf32Threads = 512;
 
 // 16-byte piece p of row r is stored at position p ^ swizzle(r) of the row, so
 // that the 16 lanes of a fragment read (16 rows, one piece) and the 32 lanes of a
@@ -222,7 +242,7 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
   constexpr int ES = elem_bytes<TT>();
   constexpr int CPR = D / 8, RPI = 64 / CPR;  // pieces per row, rows per copy
   constexpr int HALF = kPf32Keys * D * 2;     // bytes of the K (or V) rows of a tile
-  constexpr int PER = HALF / 1024 / 4;        // copies per wave of each
+  constexpr int PER = HALF / 1024 / 8;        // copies per wave of each
   constexpr int KS = D / 16, DT = D / 32;
   __shared__ __align__(1024) char smem[2 * 2 * HALF];
   const PrefillArgs& p = a.p;
@@ -321,17 +341,28 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
         for (int e = 0; e < 16; ++e)
           if (!sp.sees(key0 + 32 * g + 8 * (e >> 2) + 4 * hh + (e & 3), pos)) x[g][e] = -INFINITY;
     }
-    float mx = fmaxf(x[0][0], x[1][0]);
+    // probabilities against the reference, and their sum in this lane
+    bf16x8 pf[4];
+    float sum;
+    auto weigh = [&](float ref) {
+      sum = 0.f;
 #pragma unroll
-    for (int e = 1; e < 16; ++e) mx = fmaxf(fmaxf(mx, x[0][e]), x[1][e]);
-    {
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float v = __builtin_amdgcn_exp2f(fmaf(x[g][e], a.sc, -ref));
+          sum += v;
+          pf[2 * g + (e >> 3)][e & 7] = (__bf16)v;
+        }
+    };
+    weigh(m);
+    if (__any(!(sum <= 4096.f))) {  // inf or NaN: exponentials against -inf
+      float mx = fmaxf(x[0][0], x[1][0]);
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mx = fmaxf(fmaxf(mx, x[0][e]), x[1][e]);
       float a0 = mx, b0 = mx;
       lane_swap32(a0, b0);
-      mx = fmaxf(a0, b0) * a.sc;
-    }
-    // a column without a visible key so far keeps the reference -inf, used as 0
-    if (__any(mx > m + 8.f || (m == -INFINITY && mx != -INFINITY))) {
-      const float mm = fmaxf(m, mx), ref = mm == -INFINITY ? 0.f : mm;
+      const float mm = fmaxf(m, fmaxf(a0, b0) * a.sc), ref = mm == -INFINITY ? 0.f : mm;
       const float f = __builtin_amdgcn_exp2f(m - ref);
       m = mm;
       l *= f;
@@ -339,24 +370,16 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[dt][e] *= f;
+      weigh(ref);
     }
-    const float ref = m == -INFINITY ? 0.f : m;
-    bf16x8 pf[4];
-#pragma unroll
-    for (int g = 0; g < 2; ++g)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float v = __builtin_amdgcn_exp2f(fmaf(x[g][e], a.sc, -ref));
-        l += v;
-        pf[2 * g + (e >> 3)][e & 7] = (__bf16)v;
-      }
+    l += sum;
 #pragma unroll
     for (int ss = 0; ss < 4; ++ss)
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         const char* vs = vb + ss * 16 * D * 2;
-        const s16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + voff[dt][0]));
-        const s16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + voff[dt][1]));
+        const s16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vs + voff[dt][0]));
+        const s16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vs + voff[dt][1]));
         typedef short s16x8 __attribute__((ext_vector_type(8)));
         const bf16x8 vf = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
         o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[ss], o[dt], 0, 0, 0);
@@ -397,18 +420,40 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
 }
 
 template <class TT, int D>
-__global__ __launch_bounds__(kPfThreads, 2) void pf_rows32(PfArgs a) { rows32<TT, D>(a); }
+__global__ __launch_bounds__(kPf32Threads, 2) void pf_rows32(PfArgs a) { rows32<TT, D>(a); }
 
-// Join the splits of one row: grid (q_len, HQ, batch), one thread per element.
+// Join the splits of one row: grid (q_len, HQ, batch), 256 / D threads per element,
+// each with the states of a batch of splits in flight at once (they come from
+// other XCDs: every batch is one memory round trip).
 template <class T, int D>
-__global__ __launch_bounds__(D) void pf_join(PfArgs a) {
+__global__ __launch_bounds__(256) void pf_join(PfArgs a) {
+  constexpr int PARTS = 256 / D, BATCH = 8;
+  __shared__ float st[PARTS][3][D];
   const PrefillArgs& p = a.p;
-  const int r = blockIdx.x, j = blockIdx.y, b = blockIdx.z, e = threadIdx.x;
+  const int r = blockIdx.x, j = blockIdx.y, b = blockIdx.z, e = threadIdx.x % D, part = threadIdx.x / D;
   const int nq = p.q_lens ? min(max(p.q_lens[b], 0), p.q_len) : p.q_len;
   if (r >= nq) return;
   const float* pp = a.part + (((int64_t)b * p.HQ + j) * p.q_len + r) * a.S * (D + 2);
   float m = -INFINITY, l = 0.f, o = 0.f;
-  for (int s = 0; s < a.S; ++s, pp += D + 2) state_merge(m, l, o, pp[0], pp[1], pp[2 + e]);
+  for (int s0 = part * BATCH; s0 < a.S; s0 += PARTS * BATCH) {
+    float ms[BATCH], ls[BATCH], os[BATCH];
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const float* q = pp + (int64_t)min(s0 + i, a.S - 1) * (D + 2);
+      ms[i] = s0 + i < a.S ? q[0] : -INFINITY;
+      ls[i] = q[1];
+      os[i] = q[2 + e];
+    }
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) state_merge(m, l, o, ms[i], ls[i], os[i]);
+  }
+  st[part][0][e] = m;
+  st[part][1][e] = l;
+  st[part][2][e] = o;
+  __syncthreads();
+  if (part) return;
+#pragma unroll
+  for (int i = 1; i < PARTS; ++i) state_merge(m, l, o, st[i][0][e], st[i][1][e], st[i][2][e]);
   T* dst = reinterpret_cast<T*>(p.out) + (int64_t)b * p.os[0] + (int64_t)j * p.os[1] + (int64_t)r * p.os[2];
   dst[e] = (T)(m == -INFINITY ? 0.f : o / l);
   if (p.lse && e == 0)
@@ -421,8 +466,9 @@ struct PfPlan {
   size_t bytes;
 };
 
-// Kernel and splits over the keys: where the row tiles are fewer than 512
-// work-groups, as many splits as that takes, of at least 256 keys each.
+// Kernel and splits over the keys: as many splits as fill the chip once (one
+// work-group of pf_rows32 or two of pf_rows16 per compute unit), of at least 128
+// keys each.
 PfPlan pf_plan(const PrefillArgs& a) {
   PfPlan pl;
   const int64_t packed = (int64_t)a.q_len * a.G;
@@ -435,8 +481,8 @@ PfPlan pf_plan(const PrefillArgs& a) {
     const int64_t most = (int64_t)a.window + a.sinks + rows;
     if (most < keys) keys = most;
   }
-  const int64_t most_s = keys / 256;
-  int64_t S = groups >= 512 ? 1 : (512 + groups - 1) / groups;
+  const int64_t most_s = keys / 128;
+  int64_t S = (pl.wide ? 256 : 512) / groups;
   if (S > most_s) S = most_s;
   if (S > 64) S = 64;
   pl.S = S < 1 ? 1 : (int)S;
@@ -458,8 +504,8 @@ hipError_t run_prefill(const PrefillArgs& p, char* ws, hipStream_t s) {
   a.sc = (float)(1.4426950408889634 / sqrt((double)p.D));
   const dim3 grid(pf_grid(a));
   if (pl.wide) {
-    if (p.D == 64) hipLaunchKernelGGL((pf_rows32<BF16, 64>), grid, dim3(kPfThreads), 0, s, a);
-    else hipLaunchKernelGGL((pf_rows32<BF16, 128>), grid, dim3(kPfThreads), 0, s, a);
+    if (p.D == 64) hipLaunchKernelGGL((pf_rows32<BF16, 64>), grid, dim3(kPf32Threads), 0, s, a);
+    else hipLaunchKernelGGL((pf_rows32<BF16, 128>), grid, dim3(kPf32Threads), 0, s, a);
   } else if (p.esize == 2) {
     if (p.D == 64) hipLaunchKernelGGL((pf_rows16<BF16, 64>), grid, dim3(kPfThreads), 0, s, a);
     else hipLaunchKernelGGL((pf_rows16<BF16, 128>), grid, dim3(kPfThreads), 0, s, a);
@@ -471,11 +517,11 @@ hipError_t run_prefill(const PrefillArgs& p, char* ws, hipStream_t s) {
   if (e != hipSuccess || pl.S == 1) return e;
   const dim3 jgrid(p.q_len, p.HQ, p.batch);
   if (p.esize == 2) {
-    if (p.D == 64) hipLaunchKernelGGL((pf_join<__bf16, 64>), jgrid, dim3(64), 0, s, a);
-    else hipLaunchKernelGGL((pf_join<__bf16, 128>), jgrid, dim3(128), 0, s, a);
+    if (p.D == 64) hipLaunchKernelGGL((pf_join<__bf16, 64>), jgrid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((pf_join<__bf16, 128>), jgrid, dim3(256), 0, s, a);
   } else {
-    if (p.D == 64) hipLaunchKernelGGL((pf_join<float, 64>), jgrid, dim3(64), 0, s, a);
-    else hipLaunchKernelGGL((pf_join<float, 128>), jgrid, dim3(128), 0, s, a);
+    if (p.D == 64) hipLaunchKernelGGL((pf_join<float, 64>), jgrid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((pf_join<float, 128>), jgrid, dim3(256), 0, s, a);
   }
   return hipGetLastError();
 }
