@@ -26,10 +26,6 @@ namespace {
 
 constexpr int kPdThreads = 256;
 constexpr int kPdWaves = kPdThreads / 64;
-#ifndef TARGET
-#define TARGET 512
-#endif
-constexpr int kPdTarget = TARGET;
 
 struct PdArgs {
   PagedView c;
@@ -312,12 +308,20 @@ hipError_t launch(const PdArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// Splits: about 512 work-groups over batch and heads (two per compute unit), at
-// least four groups (one per wave) each.
+// Splits: 1024 work-groups over batch and heads as long as each has 1024 slots
+// (16 groups a wave), more of fewer slots only to give every compute unit one,
+// down to one group a wave.  us of both launches with 512 / 1024 / 4096
+// work-groups, 16 sequences of 8k to 16k slots (8 heads, d 128): 169 / 163 / 170;
+// with 256 / 1024 slots at least, one sequence of 32k: 35.2 / 27.5, 32 of 1k to 2k:
+// 48.6 / 50.3.
 PagedDecodePlan paged_decode_plan(const PagedView& c, int window, int sinks, bool acc) {
   const int64_t bh = (int64_t)c.batch * c.H;
-  int64_t S = (kPdTarget + bh - 1) / bh;
-  const int most_s = (most_groups(c, window, sinks) + kPdWaves - 1) / kPdWaves;
+  const int groups = most_groups(c, window, sinks);
+  auto per_bh = [&](int64_t work_groups) { return (work_groups + bh - 1) / bh; };
+  int64_t S = per_bh(1024);
+  if (S > groups / 64) S = groups / 64;
+  if (S < per_bh(256)) S = per_bh(256);
+  const int most_s = (groups + kPdWaves - 1) / kPdWaves;
   if (S > most_s) S = most_s;
   PagedDecodePlan p;
   p.S = (int)(S < 1 ? 1 : S);

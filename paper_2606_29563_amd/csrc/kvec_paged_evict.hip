@@ -8,14 +8,10 @@
 //           the weight's bits, order preserving, with protected slots on top
 //           and NaN at the bottom.  A radix select over 11, 11 and 10 bits
 //           finds the B-th largest key; of the slots that have it, the lowest are
-//           kept.  Wave w holds the w-th sixteenth of the slots, 64 at a time
-//           in slot order, so ranks are ballots within a wave and one sum over
-//           the waves before it.  Kept slots behind B and evicted ones below it
-//           go to two lists in ascending order.
+//           kept.  Kept slots behind B and evicted ones below it go to two lists
+//           in ascending order: a thread counts both over a run of neighbouring
+//           slots, one sum over the threads gives its places in the lists.
 //   move    pairs of the lists: K, V, acc and pos.
-// Bound by the latency of the select: five passes over the keys, which stay in
-// registers up to 32768 slots (longer sequences read them again), and by the
-// bytes of the moved rows when many move.
 #include "kvec_attn_dev.h"
 #include "kvec_serve.h"
 
@@ -40,19 +36,21 @@ struct EvArgs {
   int32_t* dst;
 };
 
-__device__ __forceinline__ int ev_page(const EvArgs& a, int b, int slot, int* row) {
-  const int g = slot >> 4;
-  const int pg = (int)(((uint64_t)(uint32_t)g * a.c.gdiv.magic) >> 32);
-  *row = slot - pg * a.c.ps;
-  const int page = a.c.table[(int64_t)b * a.c.max_pages + pg];
+// Index of a slot's page in the table, and the page (-1: not one of the pool's).
+__device__ __forceinline__ int ev_page_index(const EvArgs& a, int slot) {
+  return (int)(((uint64_t)(uint32_t)(slot >> 4) * a.c.gdiv.magic) >> 32);
+}
+__device__ __forceinline__ int ev_page(const EvArgs& a, int b, int slot) {
+  const int page = a.c.table[(int64_t)b * a.c.max_pages + ev_page_index(a, slot)];
   return page >= 0 && page < a.c.n_pages ? page : -1;
 }
 
-// Exclusive prefix over the waves and the total of one value per wave.
-__device__ __forceinline__ int waves_before(int v, int* tmp, int& total) {
-  const int w = threadIdx.x >> 6;
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) tmp[w] = v;
+// Exclusive prefix of v over the work-group and its total.  Barriers: one; tmp may be
+// written again behind the caller's next one.
+__device__ __forceinline__ int scan_before(int v, int* tmp, int& total) {
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int incl = wave_incl_scan(v);
+  if (lane == 63) tmp[w] = incl;
   __syncthreads();
   int before = 0;
   total = 0;
@@ -62,60 +60,69 @@ __device__ __forceinline__ int waves_before(int v, int* tmp, int& total) {
     before += i < w ? x : 0;
     total += x;
   }
-  return before;
+  return before + incl - v;
 }
 
-// R: 64-slot rows of keys that a wave holds in registers; 0: read again.
-template <int R>
+// The keys of a tile of CAP slots are made in LDS, EB loads of a thread in flight at
+// once; sequences of one tile make them once, longer ones in every pass.
+template <int CAP, int EB>
 __global__ __launch_bounds__(kEvThreads) void ev_select(EvArgs a) {
-  __shared__ uint32_t hist[kEvBins];
-  __shared__ int tmp[kEvWaves];
-  __shared__ uint32_t found[2];
-  const int h = blockIdx.x, b = blockIdx.y, H = a.c.H, B = a.B;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  static_assert(CAP < 1 << 16, "two counts of a tile share a word");
+  __shared__ uint32_t keys[CAP];
+  __shared__ uint32_t hist[2][kEvBins];
+  __shared__ int tmp[2][kEvWaves];
+  __shared__ uint32_t found[3][2];
+  const int h = blockIdx.x, b = blockIdx.y, H = a.c.H, B = a.B, tid = threadIdx.x;
   const int n = min(max(a.c.lens[b], 0), a.c.max_len);
   const int64_t bh = (int64_t)b * H + h;
-  int32_t* kept = a.kept ? a.kept + bh * B : nullptr;
-  if (threadIdx.x == 0 && h == 0) a.new_len[b] = min(n, B);
+  if (tid == 0 && h == 0) a.new_len[b] = min(n, B);
+  // what is kept below the budget stays there; the moves fill in the others
+  if (a.kept)
+    for (int s = tid; s < B; s += kEvThreads) a.kept[bh * B + s] = s < n ? s : -1;
   if (n <= B) {
-    if (threadIdx.x == 0) a.count[bh] = 0;
-    if (kept)
-      for (int s = threadIdx.x; s < B; s += kEvThreads) kept[s] = s < n ? s : -1;
+    if (tid == 0) a.count[bh] = 0;
     return;
   }
   const int64_t recent = a.window > 0 ? (int64_t)a.n_seen[b] - a.window : INT64_MAX;
-  const int rows = (n + kEvWaves * 64 - 1) / (kEvWaves * 64);  // 64-slot rows per wave
-  const int base = w * rows * 64 + lane;
+  for (int i = tid; i < 2 * kEvBins; i += kEvThreads) (&hist[0][0])[i] = 0;
 
-  auto read_key = [&](int i) -> uint32_t {
-    const int s = base + 64 * i;
-    uint32_t key = 0;
-    if (s < n) {
-      int row;
-      const int page = ev_page(a, b, s, &row);
-      if (page >= 0) {
-        const int64_t at = ((int64_t)page * H + h) * a.c.ps + row;
-        const float x = a.acc[at];
-        const int p = a.pos[at];
+  auto make_keys = [&](int t0, int m) {
+    for (int i0 = 0; i0 < m; i0 += EB * kEvThreads) {
+      int page[EB], row[EB];
+#pragma unroll
+      for (int i = 0; i < EB; ++i) {  // slots behind the tile read its last one
+        const int s = t0 + min(i0 + i * kEvThreads + tid, m - 1);
+        page[i] = ev_page(a, b, s);
+        row[i] = s - ev_page_index(a, s) * a.c.ps;
+      }
+      float x[EB];
+      int p[EB];
+#pragma unroll
+      for (int i = 0; i < EB; ++i) {
+        const int64_t at = ((int64_t)max(page[i], 0) * H + h) * a.c.ps + row[i];
+        x[i] = a.acc[at];
+        p[i] = a.pos[at];
+      }
+#pragma unroll
+      for (int i = 0; i < EB; ++i) {
+        const bool safe = p[i] < a.sinks || p[i] >= recent;
         // + 0: the two zeros are equal
-        key = p < a.sinks || p >= recent ? 0xffffffffu : x != x ? 0u : float_key(x + 0.f);
+        const uint32_t key = page[i] < 0 ? 0u : safe ? 0xffffffffu : x[i] != x[i] ? 0u : float_key(x[i] + 0.f);
+        if (i0 + i * kEvThreads + tid < m) keys[i0 + i * kEvThreads + tid] = key;
       }
     }
-    return key;
   };
-  uint32_t held[R > 0 ? R : 1];
-  if constexpr (R > 0) {
-#pragma unroll
-    for (int i = 0; i < R; ++i) held[i] = i < rows ? read_key(i) : 0;
-  }
-  // f(i, key, slot exists) for the wave's rows in slot order
-  auto each = [&](auto f) {
-    if constexpr (R > 0) {
-#pragma unroll
-      for (int i = 0; i < R; ++i)
-        if (i < rows) f(i, held[i], base + 64 * i < n);
-    } else {
-      for (int i = 0; i < rows; ++i) f(i, read_key(i), base + 64 * i < n);
+  const int tiles = (n + CAP - 1) / CAP;
+  // f(tile, first slot, slots of the tile) with the tile's keys in LDS
+  auto each_tile = [&](bool fresh, auto f) {
+    for (int t = 0; t < tiles; ++t) {
+      const int t0 = t * CAP, m = min(CAP, n - t0);
+      if (fresh || tiles > 1) {
+        __syncthreads();
+        make_keys(t0, m);
+        __syncthreads();
+      }
+      f(t0, m);
     }
   };
 
@@ -126,67 +133,71 @@ __global__ __launch_bounds__(kEvThreads) void ev_select(EvArgs a) {
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
     const uint32_t digits = pass == 2 ? 1023u : 2047u;
-    for (int i = threadIdx.x; i < kEvBins; i += kEvThreads) hist[i] = 0;
-    __syncthreads();
-    each([&](int, uint32_t k, bool in) {
-      if (in && (k & mask) == prefix) atomicAdd(&hist[(k >> shift) & digits], 1u);
+    uint32_t* hp = hist[pass & 1];
+    each_tile(pass == 0, [&](int, int m) {
+#pragma unroll 4
+      for (int i = tid; i < m; i += kEvThreads) {
+        const uint32_t k = keys[i];
+        if ((k & mask) == prefix) atomicAdd(&hp[(k >> shift) & digits], 1u);
+      }
     });
     __syncthreads();
     // thread t: bins 2047 - 2t and 2046 - 2t, from the largest digit down
-    const int top = kEvBins - 1 - 2 * (int)threadIdx.x;
-    const int c0 = (int)hist[top], c1 = (int)hist[top - 1];
+    const int top = kEvBins - 1 - 2 * tid;
+    const int c0 = (int)hp[top], c1 = (int)hp[top - 1];
+    if (pass == 0) hp[top] = hp[top - 1] = 0;  // the third pass uses it again
     int total;
-    const int incl = wave_incl_scan(c0 + c1);
-    const int in_wave = __builtin_amdgcn_readlane(incl, 63);
-    const int before = waves_before(in_wave, tmp, total) + incl - c0 - c1;
+    const int before = scan_before(c0 + c1, tmp[pass & 1], total);
     if (before < need && need <= before + c0 + c1) {
-      const bool first = need <= before + c0;
-      found[0] = (uint32_t)(first ? top : top - 1);
-      found[1] = (uint32_t)(need - before - (first ? 0 : c0));
+      const bool upper = need <= before + c0;
+      found[pass][0] = (uint32_t)(upper ? top : top - 1);
+      found[pass][1] = (uint32_t)(need - before - (upper ? 0 : c0));
     }
     __syncthreads();
-    prefix |= found[0] << shift;
+    prefix |= found[pass][0] << shift;
     mask |= digits << shift;
-    need = (int)found[1];
+    need = (int)found[pass][1];
   }
-  const uint32_t cut = prefix;  // the B-th largest key; `need` slots that have it are kept
+  const uint32_t cut = prefix;  // the B-th largest key; the `need` lowest slots that have it are kept
 
-  int ties = 0;
-  each([&](int, uint32_t k, bool in) { ties += __popcll(__ballot(in && k == cut)); });
-  int total;
-  const int tie0 = waves_before(ties, tmp, total);
-  const uint64_t below = ((uint64_t)1 << lane) - 1;
-  int tie = tie0, late = 0, holes = 0;
-  auto keeps = [&](uint32_t k, bool in) {
-    const uint64_t same = __ballot(in && k == cut);
-    const bool keep = in && (k > cut || (k == cut && tie + __popcll(same & below) < need));
-    tie += __popcll(same);
-    return keep;
-  };
-  each([&](int i, uint32_t k, bool in) {
-    const int s = base + 64 * i;
-    const bool keep = keeps(k, in);
-    late += __popcll(__ballot(keep && s >= B));
-    holes += __popcll(__ballot(in && !keep && s < B));
-  });
-  int n_late, n_holes;
-  int at_late = waves_before(late, tmp, n_late), at_hole = waves_before(holes, tmp, n_holes);
+  // Thread t goes over the t-th run of a tile's slots; an odd run length, so that the
+  // threads' reads fall in distinct banks.
   int32_t* src = a.src + bh * a.cap;
   int32_t* dst = a.dst + bh * a.cap;
-  tie = tie0;
-  each([&](int i, uint32_t k, bool in) {
-    const int s = base + 64 * i;
-    const bool keep = keeps(k, in);
-    const bool is_late = keep && s >= B, hole = in && !keep && s < B;
-    const uint64_t ml = __ballot(is_late), mh = __ballot(hole);
-    if (is_late) src[at_late + __popcll(ml & below)] = s;
-    if (hole) dst[at_hole + __popcll(mh & below)] = s;
-    if (kept && keep && s < B) kept[s] = s;
-    at_late += __popcll(ml);
-    at_hole += __popcll(mh);
+  int late0 = 0, hole0 = 0;
+  each_tile(false, [&](int t0, int m) {
+    const int run = ((m + kEvThreads - 1) / kEvThreads) | 1;
+    const int i0 = min(tid * run, m), i1 = min(i0 + run, m);
+    int ties = 0, total;
+#pragma unroll 4
+    for (int i = i0; i < i1; ++i) ties += keys[i] == cut;
+    const int tie0 = need - scan_before(ties, tmp[0], total);  // ties wanted from this run on
+    need -= total;
+    int tie = tie0, counts = 0;  // kept behind B, and evicted below it in the upper half
+#pragma unroll 4
+    for (int i = i0; i < i1; ++i) {
+      const uint32_t k = keys[i];
+      const bool keep = k > cut || (k == cut && tie > 0), low = t0 + i < B;
+      tie -= k == cut;
+      counts += keep ? (low ? 0 : 1) : (low ? 1 << 16 : 0);
+    }
+    const int before = scan_before(counts, tmp[1], total);
+    int at_late = late0 + (before & 0xffff), at_hole = hole0 + (int)((uint32_t)before >> 16);
+    late0 += total & 0xffff;
+    hole0 += (int)((uint32_t)total >> 16);
+    tie = tie0;
+#pragma unroll 4
+    for (int i = i0; i < i1; ++i) {
+      const uint32_t k = keys[i];
+      const bool keep = k > cut || (k == cut && tie > 0), low = t0 + i < B;
+      tie -= k == cut;
+      if (keep && !low) src[at_late++] = t0 + i;
+      if (!keep && low) dst[at_hole++] = t0 + i;
+    }
+    __syncthreads();  // tmp, before the next tile
   });
   // B slots are kept, so as many are kept behind B as are evicted below it
-  if (threadIdx.x == 0) a.count[bh] = n_late;
+  if (tid == 0) a.count[bh] = late0;
 }
 
 constexpr int kMvThreads = 256;
@@ -197,14 +208,16 @@ __global__ __launch_bounds__(kMvThreads) void ev_move(EvArgs a) {
   const int h = blockIdx.y, b = blockIdx.z, H = a.c.H;
   const int64_t bh = (int64_t)b * H + h;
   if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0) a.lens_out[b] = a.new_len[b];
-  const int count = a.count[bh];
+  const int count = min(a.count[bh], a.cap);
   const int p = threadIdx.x % LPR;
   const int32_t* src = a.src + bh * a.cap;
   const int32_t* dst = a.dst + bh * a.cap;
   for (int i = blockIdx.x * (kMvThreads / LPR) + threadIdx.x / LPR; i < count; i += gridDim.x * (kMvThreads / LPR)) {
     const int s = src[i], d = dst[i];
-    int rs, rd;
-    const int ps = ev_page(a, b, s, &rs), pd = ev_page(a, b, d, &rd);
+    // the lists lie in the caller's workspace: nothing outside the cache is followed
+    if ((uint32_t)s >= (uint32_t)a.c.max_len || (uint32_t)d >= (uint32_t)min(a.B, a.c.max_len)) continue;
+    const int ps = ev_page(a, b, s), pd = ev_page(a, b, d);
+    const int rs = s - ev_page_index(a, s) * a.c.ps, rd = d - ev_page_index(a, d) * a.c.ps;
     if (p == 0 && a.kept) a.kept[bh * a.B + d] = s;
     if (ps < 0 || pd < 0) continue;
     const int64_t es = a.c.esize;
@@ -256,9 +269,8 @@ hipError_t run_paged_evict(const PagedView& c, int budget, int window, int sinks
   a.src = reinterpret_cast<int32_t*>(ws);
   a.dst = reinterpret_cast<int32_t*>(ws + up256(bh * a.cap * 4));
   const dim3 grid(c.H, c.batch);
-  if (c.max_len <= 4 * kEvThreads) hipLaunchKernelGGL(ev_select<4>, grid, dim3(kEvThreads), 0, s, a);
-  else if (c.max_len <= 32 * kEvThreads) hipLaunchKernelGGL(ev_select<32>, grid, dim3(kEvThreads), 0, s, a);
-  else hipLaunchKernelGGL(ev_select<0>, grid, dim3(kEvThreads), 0, s, a);
+  if (c.max_len <= 4096) hipLaunchKernelGGL((ev_select<4096, 4>), grid, dim3(kEvThreads), 0, s, a);
+  else hipLaunchKernelGGL((ev_select<32768, 8>), grid, dim3(kEvThreads), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int row = c.D * c.esize, per = kMvThreads / (row / 16);

@@ -308,10 +308,11 @@ def _check_evict(c, before, kept, out, budget, window, sinks, seen, max_len=None
             want, m = ref.evict(before[2].cpu().numpy()[p, h, r], before[3].cpu().numpy()[p, h, r], ok, n, budget, window, sinks, seen[i])
             assert np.array_equal(kept[i, h], want), (i, h)
             assert out[i] == m
-            for d, s in enumerate(want[:m]):
-                if d != s and ok[d] and ok[s]:
-                    for t, o in ((k0, before[0]), (v0, before[1]), (acc0, before[2]), (pos0, before[3])):
-                        t[p[d], h, r[d]] = o[p[s], h, r[s]].cpu()
+            d = np.arange(m)
+            d = d[(want[:m] != d) & ok[:m]]
+            d = d[ok[want[d]]]
+            for t, o in ((k0, before[0]), (v0, before[1]), (acc0, before[2]), (pos0, before[3])):
+                t[p[d], h, r[d]] = o.cpu()[p[want[d]], h, r[want[d]]]
     for got, want in ((c.k, k0), (c.v, v0), (c.acc, acc0), (c.pos, pos0)):
         got = got.cpu()
         bits = torch.int16 if got.element_size() == 2 else torch.int32
@@ -361,6 +362,19 @@ def test_evict_ties_and_special_weights(gpu_lib, kind):
     seen = torch.tensor([1990, 1700], dtype=torch.int32, device="cuda")
     kept, out = _evict(c, 500, 300, 100, seen)
     _check_evict(c, before, kept, out, 500, 300, 100, seen)
+
+
+@pytest.mark.parametrize("lens,budget", [([32768, 32769, 40000], 20000), ([65537], 33000), ([4096, 4097], 1500)])
+def test_evict_few_values_at_the_ends_of_key_tiles(gpu_lib, lens, budget):
+    """Ties, kept and evicted slots on both sides of the 4096 and 32768 keys held at a time."""
+    import torch
+    c = Cache(gpu_lib, lens, 1, 1, 64, 256, "bf16", seed=15)
+    c.acc.copy_(torch.randint(0, 4, c.acc.shape, generator=c.gen).float())
+    c.cuda()
+    before = [t.clone() for t in (c.k, c.v, c.acc, c.pos)]
+    seen = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    kept, out = _evict(c, budget, 700, 5, seen)
+    _check_evict(c, before, kept, out, budget, 700, 5, seen)
 
 
 def test_evict_in_place_lengths_bad_pages_and_clamped_lengths(gpu_lib):
