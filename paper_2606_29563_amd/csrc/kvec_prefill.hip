@@ -86,15 +86,18 @@ constexpr int kPfThreads = 256;
 constexpr int kPfRows = 64;  // packed rows per work-group, 16 per wave
 constexpr int kPfKeys = 32;
 
-template <class TT, int D>
+// float32: a work-group of four waves takes 64 packed rows, 16 a wave (Columns16), on
+// the 16x16x4 f32 product; tiles of 32 keys in two LDS buffers.  Bound by that
+// product's rate (a sixteenth of the bf16 one's).
+template <int D>
 __global__ __launch_bounds__(kPfThreads) void pf_rows16(PfArgs a) {
+  using TT = F32;
   using RG = RowGroup<TT, D>;
-  constexpr int NG = __is_same(TT, BF16) ? 2 : 1, ES = RG::ES;
+  constexpr int NG = 1, ES = RG::ES;
   constexpr int GRPS = kPfKeys / 16;
   constexpr int BUF = 2 * GRPS * RG::BYTES;       // K groups, then V groups
   constexpr int PER = 2 * GRPS * RG::NI / 4;      // copies per wave and tile
-  constexpr int NB = ES == 2 ? 3 : 2;             // LDS buffers
-  __shared__ __align__(1024) char smem[NB * BUF];
+  __shared__ __align__(1024) char smem[2 * BUF];
   const PrefillArgs& p = a.p;
   const int G = p.G;
   int bh, tile, split;
@@ -129,20 +132,18 @@ __global__ __launch_bounds__(kPfThreads) void pf_rows16(PfArgs a) {
       const bool is_v = at >= GRPS * RG::NI;
       const int in = is_v ? at - GRPS * RG::NI : at;
       const int row = row_in_copy<TT, D>(in % RG::NI, lane) + in / RG::NI * 16;
-      const int off = t < t1 && key0 + row < sp.nk ? (key0 + row) * (is_v ? vstr : kstr) + piece_in_copy<TT, D>(in % RG::NI, lane) * 16
+      const int off = key0 + row < sp.nk ? (key0 + row) * (is_v ? vstr : kstr) + piece_in_copy<TT, D>(in % RG::NI, lane) * 16
                                          : kOutOfRange;
       auto* dst = (__attribute__((address_space(3))) char*)(smem + u * BUF + at * 1024);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(is_v ? vr : kr, dst, 16, off, 0, 0, 0);
     }
   };
-  // tiles past the last are copied as zeros: the number of copies in flight stays
-#pragma unroll
-  for (int d = 0; d < NB - 1; ++d) copy(d, t0 + d);
-  int u = 0;
+  if (t0 < t1) copy(0, t0);
   for (int t = t0; t < t1; ++t) {
-    wait_vmem<(NB - 2) * PER>();
-    lds_barrier();  // the tile is there, and every wave is done with the buffer before it
-    copy(u == 0 ? NB - 1 : u - 1, t + NB - 1);
+    const int u = (t - t0) & 1;
+    wait_vmem<0>();
+    lds_barrier();  // the tile is there, and every wave is done with the other buffer
+    if (t + 1 < t1) copy(u ^ 1, t + 1);
     const char* kb = smem + u * BUF;
     const int key0 = sp.key0(t);
     const bool open = sp.open(key0) && live;
@@ -160,9 +161,7 @@ __global__ __launch_bounds__(kPfThreads) void pf_rows16(PfArgs a) {
       }
       col.absorb(x, kb + (GRPS + g0) * RG::BYTES, lane);
     }
-    u = u == NB - 1 ? 0 : u + 1;
   }
-  wait_vmem<0>();  // no copy outlives the work-group
   col.l = col_sum4(col.l);
   if (!live) return;
   const int64_t row = ((int64_t)b * p.HQ + j) * p.q_len + r;
@@ -182,50 +181,26 @@ __global__ __launch_bounds__(kPfThreads) void pf_rows16(PfArgs a) {
   char* dst = p.out + ((int64_t)b * p.os[0] + (int64_t)j * p.os[1] + (int64_t)r * p.os[2]) * ES;
 #pragma unroll
   for (int t = 0; t < D / 16; ++t) {
-    if constexpr (ES == 2) {
-      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-      bf16x4 v;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = (__bf16)(col.o[t][e] * inv);
-      *reinterpret_cast<bf16x4*>(dst + (16 * t + 4 * c) * 2) = v;
-    } else {
-      *reinterpret_cast<f32x4*>(dst + (16 * t + 4 * c) * 4) = col.o[t] * inv;
-    }
+    *reinterpret_cast<f32x4*>(dst + (16 * t + 4 * c) * 4) = col.o[t] * inv;
   }
   if (p.lse && c == 0)
     p.lse[(int64_t)b * p.ls[0] + (int64_t)j * p.ls[1] + r] =
         col.m == -INFINITY ? -INFINITY : (col.m + log2f(col.l)) * 0.69314718055994531f;
 }
 
-// Long prompts, bf16: a work-group of eight waves takes 256 packed rows, a wave
-// 32 of them as the columns of 32x32x16 products (S^T = K Q^T, O^T = V^T P^T; see
-// kvec_attn_dev.h for why P stays in its registers: here the output lane holds
-// keys 8 (i / 4) + 4 (lane / 32) + i % 4 of column lane % 32, and the V product's
-// reduction runs over the keys in that order).  Tiles of 64 keys are copied
-// into one of two LDS buffers while the other is used; one barrier per tile.
+// bf16: 32 packed rows are the columns of 32x32x16 products (S^T = K Q^T, O^T = V^T
+// P^T; see kvec_attn_dev.h for why P stays in its registers: here the output lane
+// holds keys 8 (i / 4) + 4 (lane / 32) + i % 4 of column lane % 32, and the V
+// product's reduction runs over the keys in that order).
 //
 // The softmax keeps a reference per column instead of the running maximum, and
-// looks for a maximum only when the tile's probabilities say so: their sum in a
+// looks for a maximum only when a tile's probabilities say so: their sum in a
 // lane beyond 2^12 (or no number: the column has no reference yet) takes the
 // tile's maximum as the new reference, rescales O and the sum, and weighs the
 // tile again.  The quotient O / l does not depend on the reference, float32 holds
 // terms up to 2^12 as exactly as those up to 1, and the bf16 rounding of P is
 // relative.  Most tiles so need neither the maximum nor a pass over O.
-//
-// Bound by the matrix cores and the vector work of the softmax, which mostly add
-// up (the counters see them together in 28% of the matrix cores' busy cycles).
-// A causal 8k prompt (32 query, 8 KV heads, d 128): 1.05 PFLOP/s, where a large
-// library product reaches 1.22.  In us of that prompt: a running maximum and
-// four waves of 128 rows 569, eight waves, which copy each key tile half as often,
-// 549 (535 and 522 without and with the search for the maximum left out, on
-// another card; without any copies, for timing, 490 of the 569).  Measured and
-// dropped: three LDS buffers (540 for 535), the next tile's logits computed beside this
-// tile's exponentials (561 for 549), waves 4-7 half a tile behind waves 0-3, in
-// step by barriers (607), raised wave priority around the products (549 for 545).
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-constexpr int kPf32Rows = 256, kPf32Keys = 64;
-
-constexpr int kPf32Threads = 512;
 
 // 16-byte piece p of row r is stored at position p ^ swizzle(r) of the row, so
 // that the 16 lanes of a fragment read (16 rows, one piece) and the 32 lanes of a
@@ -237,13 +212,172 @@ __device__ __forceinline__ int v_swizzle(int r) {
   return D == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
 }
 
+// A wave's 32 columns.
+template <class TT, int D>
+struct Columns32 {
+  static constexpr int KS = D / 16, DT = D / 32;
+  bf16x8 q[KS];
+  f32x16 o[DT];
+  float m, l;  // reference (base-2 logits); this lane's part of the sum
+  int n, hh;   // column of the lane, which half of the keys it holds
+  int koff[KS];          // bytes of the lane's K fragments in a block of 32 rows
+  uint32_t voff[2 * DT];  // ... of its V reads in 16 rows: of the first (2 dt) and the last four of eight
+
+  __device__ __forceinline__ void init(int lane, const char* row, bool live) {
+    n = lane & 31;
+    hh = lane >> 5;
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      q[ks] = __builtin_bit_cast(bf16x8, live ? reinterpret_cast<const uint4*>(row)[2 * ks + hh] : make_uint4(0, 0, 0, 0));
+      koff[ks] = n * D * 2 + ((2 * ks + hh) ^ k_swizzle<D>(n)) * 16;
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = 8 * e + 4 * hh + ((lane & 15) >> 2), piece = 4 * dt + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+        voff[2 * dt + e] = r * D * 2 + (piece ^ v_swizzle<D>(r)) * 16 + (lane & 1) * 8;
+      }
+    }
+  }
+
+  // Logits of NB blocks of 32 keys at `kb`.
+  template <int NB>
+  __device__ __forceinline__ void logits(f32x16 (&x)[NB], const char* kb) const {
+#pragma unroll
+    for (int g = 0; g < NB; ++g)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[g][e] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int g = 0; g < NB; ++g) {
+        const bf16x8 kf = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(kb + g * 32 * D * 2 + koff[ks]));
+        x[g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[ks], x[g], 0, 0, 0);
+      }
+  }
+  // Key of element e of block g, from the tile's first.
+  __device__ __forceinline__ int key(int g, int e) const { return 32 * g + 8 * (e >> 2) + 4 * hh + (e & 3); }
+
+  // Probabilities of a tile's logits, -inf where masked, as 16-key steps of the V product.
+  template <int NB>
+  __device__ __forceinline__ void weigh(const f32x16 (&x)[NB], float sc, bf16x8 (&pf)[2 * NB]) {
+    float sum;
+    auto against = [&](float ref) {
+      sum = 0.f;
+#pragma unroll
+      for (int g = 0; g < NB; ++g)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float v = __builtin_amdgcn_exp2f(fmaf(x[g][e], sc, -ref));
+          sum += v;
+          pf[2 * g + (e >> 3)][e & 7] = (__bf16)v;
+        }
+    };
+    against(m);
+    if (__any(!(sum <= 4096.f))) {  // inf or NaN: exponentials against -inf
+      float mx = x[0][0];
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+#pragma unroll
+        for (int g = 0; g < NB; ++g) mx = fmaxf(mx, x[g][e]);
+      float a0 = mx, b0 = mx;
+      lane_swap32(a0, b0);
+      const float mm = fmaxf(m, fmaxf(a0, b0) * sc), ref = mm == -INFINITY ? 0.f : mm;
+      const float f = __builtin_amdgcn_exp2f(m - ref);
+      m = mm;
+      l *= f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[dt][e] *= f;
+      against(ref);
+    }
+    l += sum;
+  }
+
+  // The sum over the column, in both of its lanes.
+  __device__ __forceinline__ void close() {
+    float a0 = l, b0 = l;
+    lane_swap32(a0, b0);
+    l = a0 + b0;
+  }
+  // Element of the head dimension that o[dt][e] holds.
+  __device__ __forceinline__ int dim(int dt, int e) const { return 32 * dt + 8 * (e >> 2) + 4 * hh + (e & 3); }
+};
+
+// Copies of a block of rows by direct global-to-LDS loads: row and byte (K's and V's
+// order of the pieces) of the lane in copy i.
+template <int D>
+struct RowCopy {
+  static constexpr int CPR = D / 8, RPI = 64 / CPR;  // pieces per row, rows per copy
+  int row, kb, vb;
+  __device__ __forceinline__ void init(int i, int lane) {
+    row = i * RPI + lane / CPR;
+    kb = ((lane % CPR) ^ k_swizzle<D>(row)) * 16;
+    vb = ((lane % CPR) ^ v_swizzle<D>(row)) * 16;
+  }
+};
+
+// One column's result, or its partial state.
+template <class TT, int D>
+__device__ __forceinline__ void store_column(const PfArgs& a, const Columns32<TT, D>& col, int b, int j, int r, int split) {
+  const PrefillArgs& p = a.p;
+  if (a.S > 1) {
+    float* pp = a.part + ((((int64_t)b * p.HQ + j) * p.q_len + r) * a.S + split) * (D + 2);
+    if (col.hh == 0) {
+      pp[0] = col.m;
+      pp[1] = col.l;
+    }
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) pp[2 + col.dim(dt, e)] = col.o[dt][e];
+    return;
+  }
+  const float inv = col.m == -INFINITY ? 0.f : 1.f / col.l;
+  char* dst = p.out + ((int64_t)b * p.os[0] + (int64_t)j * p.os[1] + (int64_t)r * p.os[2]) * 2;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+      bf16x4 v;
+#pragma unroll
+      for (int f = 0; f < 4; ++f) v[f] = (__bf16)(col.o[dt][e + f] * inv);
+      *reinterpret_cast<bf16x4*>(dst + col.dim(dt, e) * 2) = v;
+    }
+  if (p.lse && col.hh == 0)
+    p.lse[(int64_t)b * p.ls[0] + (int64_t)j * p.ls[1] + r] =
+        col.m == -INFINITY ? -INFINITY : (col.m + log2f(col.l)) * 0.69314718055994531f;
+}
+
+// Many rows: a work-group of eight waves takes 256 packed rows, 32 a wave.  Tiles of
+// 64 keys are copied into one of two LDS buffers while the other is used; one
+// barrier per tile.
+//
+// Bound by the matrix cores and the vector work of the softmax, which mostly add
+// up (the counters see them together in 28% of the matrix cores' busy cycles).
+// A causal 8k prompt (32 query, 8 KV heads, d 128): 1.05 PFLOP/s, where a large
+// library product reaches 1.22.  In us of that prompt: a running maximum and
+// four waves of 128 rows 569, eight waves, which copy each key tile half as often,
+// 549 (535 and 522 without and with the search for the maximum left out, on
+// another card; without any copies, for timing, 490 of the 569).  Measured and
+// dropped: three LDS buffers (540 for 535), the next tile's logits computed beside this
+// tile's exponentials (561 for 549), waves 4-7 half a tile behind waves 0-3, in
+// step by barriers (607), raised wave priority around the products (549 for 545).
+constexpr int kPf32Threads = 512, kPf32Rows = 256, kPf32Keys = 64;
+
 template <class TT, int D>
 __device__ __forceinline__ void rows32(const PfArgs& a) {
   constexpr int ES = elem_bytes<TT>();
-  constexpr int CPR = D / 8, RPI = 64 / CPR;  // pieces per row, rows per copy
   constexpr int HALF = kPf32Keys * D * 2;     // bytes of the K (or V) rows of a tile
   constexpr int PER = HALF / 1024 / 8;        // copies per wave of each
-  constexpr int KS = D / 16, DT = D / 32;
+  constexpr int DT = D / 32;
   __shared__ __align__(1024) char smem[2 * 2 * HALF];
   const PrefillArgs& p = a.p;
   const int G = p.G;
@@ -251,68 +385,37 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
   if (!pf_item(a, &bh, &tile, &split)) return;
   const int b = bh / p.H, h = bh % p.H;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int n = lane & 31, hh = lane >> 5;
   const Span<kPf32Keys> sp(p, b, tile * kPf32Rows, kPf32Rows);
   if (!sp.any) return;
-  const int i = tile * kPf32Rows + w * 32 + n, r = i / G, j = h * G + i % G;
+  const int i = tile * kPf32Rows + w * 32 + (lane & 31), r = i / G, j = h * G + i % G;
   const bool live = r < sp.nq;
   const int pos = live ? sp.shift + r : -1;
   const int per = (sp.n + a.S - 1) / a.S;
   const int t0 = min(split * per, sp.n), t1 = min(t0 + per, sp.n);
 
-  bf16x8 qf[KS];
-  {
-    const char* q = p.q + ((int64_t)b * p.qs[0] + (int64_t)j * p.qs[1] + (int64_t)r * p.qs[2]) * ES;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-      qf[ks] = __builtin_bit_cast(bf16x8, live ? reinterpret_cast<const uint4*>(q)[2 * ks + hh] : make_uint4(0, 0, 0, 0));
-  }
+  Columns32<TT, D> col;
+  col.init(lane, p.q + ((int64_t)b * p.qs[0] + (int64_t)j * p.qs[1] + (int64_t)r * p.qs[2]) * ES, live);
   const int kstr = (int)(p.ks[2] * ES), vstr = (int)(p.vs[2] * ES);
   const int last = max(sp.nk - 1, 0);
   const auto kr = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<char*>(p.k) + ((int64_t)b * p.ks[0] + (int64_t)h * p.ks[1]) * ES, 0, last * kstr + D * ES, kBufferWord3);
   const auto vr = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<char*>(p.v) + ((int64_t)b * p.vs[0] + (int64_t)h * p.vs[1]) * ES, 0, last * vstr + D * ES, kBufferWord3);
-  int krow[PER], kpc[PER], vpc[PER];
+  RowCopy<D> rc[PER];
 #pragma unroll
-  for (int q = 0; q < PER; ++q) {
-    krow[q] = (w * PER + q) * RPI + lane / CPR;
-    kpc[q] = ((lane % CPR) ^ k_swizzle<D>(krow[q])) * 16;
-    vpc[q] = ((lane % CPR) ^ v_swizzle<D>(krow[q])) * 16;
-  }
+  for (int q = 0; q < PER; ++q) rc[q].init(w * PER + q, lane);
   auto copy = [&](int u, int t) {
     const int key0 = sp.key0(t);
 #pragma unroll
     for (int q = 0; q < PER; ++q) {
       auto* dk = (__attribute__((address_space(3))) char*)(smem + u * 2 * HALF + (w * PER + q) * 1024);
       auto* dv = (__attribute__((address_space(3))) char*)(smem + u * 2 * HALF + HALF + (w * PER + q) * 1024);
-      const bool in = key0 + krow[q] < sp.nk;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, dk, 16, in ? (key0 + krow[q]) * kstr + kpc[q] : kOutOfRange, 0, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, dv, 16, in ? (key0 + krow[q]) * vstr + vpc[q] : kOutOfRange, 0, 0, 0);
+      const int key = key0 + rc[q].row;
+      const bool in = key < sp.nk;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, dk, 16, in ? key * kstr + rc[q].kb : kOutOfRange, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, dv, 16, in ? key * vstr + rc[q].vb : kOutOfRange, 0, 0, 0);
     }
   };
-
-  // lane part of the LDS addresses: fragments of K, transposed reads of V
-  int koff[KS];
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) koff[ks] = n * D * 2 + ((2 * ks + hh) ^ k_swizzle<D>(n)) * 16;
-  const int vrow = 4 * hh + ((lane & 15) >> 2);  // row of the lane in a step's first four and last four
-  int voff[DT][2];
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int row = vrow + 8 * e, piece = 4 * dt + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
-      voff[dt][e] = row * D * 2 + (piece ^ v_swizzle<D>(row)) * 16 + (lane & 1) * 8;
-    }
-
-  f32x16 o[DT];
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
-  float m = -INFINITY, l = 0.f;  // reference (base-2 logits); this lane's part of the sum
-
   if (t0 < t1) copy(0, t0);
   for (int t = t0; t < t1; ++t) {
     const int u = (t - t0) & 1;
@@ -322,105 +425,149 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
     const char* kb = smem + u * 2 * HALF;
     const char* vb = kb + HALF;
     f32x16 x[2];
-#pragma unroll
-    for (int g = 0; g < 2; ++g)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) x[g][e] = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        const bf16x8 kf = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(kb + g * 32 * D * 2 + koff[ks]));
-        x[g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], x[g], 0, 0, 0);
-      }
+    col.logits(x, kb);
     const int key0 = sp.key0(t);
     if (!sp.open(key0)) {
 #pragma unroll
       for (int g = 0; g < 2; ++g)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (!sp.sees(key0 + 32 * g + 8 * (e >> 2) + 4 * hh + (e & 3), pos)) x[g][e] = -INFINITY;
+          if (!sp.sees(key0 + col.key(g, e), pos)) x[g][e] = -INFINITY;
     }
-    // probabilities against the reference, and their sum in this lane
     bf16x8 pf[4];
-    float sum;
-    auto weigh = [&](float ref) {
-      sum = 0.f;
-#pragma unroll
-      for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float v = __builtin_amdgcn_exp2f(fmaf(x[g][e], a.sc, -ref));
-          sum += v;
-          pf[2 * g + (e >> 3)][e & 7] = (__bf16)v;
-        }
-    };
-    weigh(m);
-    if (__any(!(sum <= 4096.f))) {  // inf or NaN: exponentials against -inf
-      float mx = fmaxf(x[0][0], x[1][0]);
-#pragma unroll
-      for (int e = 1; e < 16; ++e) mx = fmaxf(fmaxf(mx, x[0][e]), x[1][e]);
-      float a0 = mx, b0 = mx;
-      lane_swap32(a0, b0);
-      const float mm = fmaxf(m, fmaxf(a0, b0) * a.sc), ref = mm == -INFINITY ? 0.f : mm;
-      const float f = __builtin_amdgcn_exp2f(m - ref);
-      m = mm;
-      l *= f;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[dt][e] *= f;
-      weigh(ref);
-    }
-    l += sum;
+    col.weigh(x, a.sc, pf);
+    // (the compiler's transposing read waits for the copies in flight, which were
+    // issued half a tile before; written out with waits of its own it was slower, 566
+    // us for 545, because then the products cannot be scheduled between the reads)
 #pragma unroll
     for (int ss = 0; ss < 4; ++ss)
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
         const char* vs = vb + ss * 16 * D * 2;
-        const s16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vs + voff[dt][0]));
-        const s16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vs + voff[dt][1]));
-        typedef short s16x8 __attribute__((ext_vector_type(8)));
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
-        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[ss], o[dt], 0, 0, 0);
+        const s16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + col.voff[2 * dt]));
+        const s16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + col.voff[2 * dt + 1]));
+        col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(join8(a0, a1), pf[ss], col.o[dt], 0, 0, 0);
       }
   }
-  {
-    float a0 = l, b0 = l;
-    lane_swap32(a0, b0);
-    l = a0 + b0;
-  }
-  if (!live) return;
-  if (a.S > 1) {
-    float* pp = a.part + ((((int64_t)b * p.HQ + j) * p.q_len + r) * a.S + split) * (D + 2);
-    if (hh == 0) {
-      pp[0] = m;
-      pp[1] = l;
-    }
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) pp[2 + 32 * dt + 8 * (e >> 2) + 4 * hh + (e & 3)] = o[dt][e];
-    return;
-  }
-  const float inv = m == -INFINITY ? 0.f : 1.f / l;
-  char* dst = p.out + ((int64_t)b * p.os[0] + (int64_t)j * p.os[1] + (int64_t)r * p.os[2]) * ES;
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int e = 0; e < 16; e += 4) {
-      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-      bf16x4 v;
-#pragma unroll
-      for (int f = 0; f < 4; ++f) v[f] = (__bf16)(o[dt][e + f] * inv);
-      *reinterpret_cast<bf16x4*>(dst + (32 * dt + 2 * e + 4 * hh) * 2) = v;
-    }
-  if (p.lse && hh == 0)
-    p.lse[(int64_t)b * p.ls[0] + (int64_t)j * p.ls[1] + r] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+  col.close();
+  if (live) store_column(a, col, b, j, r, split);
 }
 
 template <class TT, int D>
 __global__ __launch_bounds__(kPf32Threads, 2) void pf_rows32(PfArgs a) { rows32<TT, D>(a); }
+
+// Few rows, bf16: a work-group of two waves takes 32 packed rows, both waves the
+// same ones.  The waves go over the 32-key steps of the work-group's split in
+// turn, each with an LDS ring of two steps of its own and no barrier before the
+// end, where their states are joined: what bounds it is the reading of K and V.
+constexpr int kPfFewThreads = 128, kPfFewRows = 32, kPfFewKeys = 32;
+
+template <class TT, int D>
+__device__ __forceinline__ void few(const PfArgs& a) {
+  constexpr int ES = elem_bytes<TT>(), DT = D / 32, WAVES = kPfFewThreads / 64;
+  constexpr int HALF = kPfFewKeys * D * 2, STEP = 2 * HALF, PER = HALF / 1024;
+  constexpr int MERGE = WAVES * 32 * (D + 2) * 4;
+  __shared__ __align__(1024) char smem[WAVES * 2 * STEP > MERGE ? WAVES * 2 * STEP : MERGE];
+  const PrefillArgs& p = a.p;
+  const int G = p.G;
+  int bh, tile, split;
+  if (!pf_item(a, &bh, &tile, &split)) return;
+  const int b = bh / p.H, h = bh % p.H;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const Span<kPfFewKeys> sp(p, b, tile * kPfFewRows, kPfFewRows);
+  if (!sp.any) return;
+  const int i = tile * kPfFewRows + (lane & 31), r = i / G, j = h * G + i % G;
+  const bool live = r < sp.nq;
+  const int pos = live ? sp.shift + r : -1;
+  const int per = (sp.n + a.S - 1) / a.S;
+  const int t0 = min(split * per, sp.n), t1 = min(t0 + per, sp.n);
+
+  Columns32<TT, D> col;
+  col.init(lane, p.q + ((int64_t)b * p.qs[0] + (int64_t)j * p.qs[1] + (int64_t)r * p.qs[2]) * ES, live);
+  const int kstr = (int)(p.ks[2] * ES), vstr = (int)(p.vs[2] * ES);
+  const int last = max(sp.nk - 1, 0);
+  const auto kr = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<char*>(p.k) + ((int64_t)b * p.ks[0] + (int64_t)h * p.ks[1]) * ES, 0, last * kstr + D * ES, kBufferWord3);
+  const auto vr = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<char*>(p.v) + ((int64_t)b * p.vs[0] + (int64_t)h * p.vs[1]) * ES, 0, last * vstr + D * ES, kBufferWord3);
+  char* ring = smem + w * 2 * STEP;
+  RowCopy<D> rc[PER];
+#pragma unroll
+  for (int q = 0; q < PER; ++q) rc[q].init(q, lane);
+  // steps behind the split's last are copied as zeros: the number in flight stays
+  auto copy = [&](int u, int t) {
+    const int key0 = sp.key0(t);
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      auto* dk = (__attribute__((address_space(3))) char*)(ring + u * STEP + q * 1024);
+      auto* dv = (__attribute__((address_space(3))) char*)(ring + u * STEP + HALF + q * 1024);
+      const int key = key0 + rc[q].row;
+      const bool in = t < t1 && key < sp.nk;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, dk, 16, in ? key * kstr + rc[q].kb : kOutOfRange, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, dv, 16, in ? key * vstr + rc[q].vb : kOutOfRange, 0, 0, 0);
+    }
+  };
+  copy(0, t0 + w);
+  copy(1, t0 + w + WAVES);
+  int u = 0;
+  for (int t = t0 + w; t < t1; t += WAVES) {
+    wait_vmem<2 * PER>();
+    const char* kb = ring + u * STEP;
+    f32x16 x[1];
+    col.logits(x, kb);
+    const int key0 = sp.key0(t);
+    if (!sp.open(key0)) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (!sp.sees(key0 + col.key(0, e), pos)) x[0][e] = -INFINITY;
+    }
+    bf16x8 pf[2];
+    col.weigh(x, a.sc, pf);
+    uint32_t at[2 * DT];
+#pragma unroll
+    for (int e = 0; e < 2 * DT; ++e) at[e] = lds_addr(kb) + HALF + col.voff[e];
+    s16x4 v0[2 * DT], v1[2 * DT];
+    vt_read<0>(at, v0);
+    vt_read<16 * D * 2>(at, v1);
+    // the ring slot is read out (the last statement waited): the next copy may start
+    copy(u, t + 2 * WAVES);
+    u ^= 1;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(join8(v0[2 * dt], v0[2 * dt + 1]), pf[0], col.o[dt], 0, 0, 0);
+      col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(join8(v1[2 * dt], v1[2 * dt + 1]), pf[1], col.o[dt], 0, 0, 0);
+    }
+  }
+  wait_vmem<0>();
+  col.close();
+  __syncthreads();
+  // wave 1 hands its state to wave 0
+  float* sm = reinterpret_cast<float*>(smem);  // [column][D + 2]
+  float* mine = sm + col.n * (D + 2);
+  if (w == 1) {
+    mine[0] = col.m;
+    mine[1] = col.l;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mine[2 + col.dim(dt, e)] = col.o[dt][e];
+  }
+  __syncthreads();
+  if (w == 1 || !live) return;
+  const float m2 = mine[0], mm = fmaxf(col.m, m2), ref = mm == -INFINITY ? 0.f : mm;
+  const float f1 = __builtin_amdgcn_exp2f(col.m - ref), f2 = __builtin_amdgcn_exp2f(m2 - ref);
+  col.m = mm;
+  col.l = col.l * f1 + mine[1] * f2;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) col.o[dt][e] = col.o[dt][e] * f1 + mine[2 + col.dim(dt, e)] * f2;
+  store_column(a, col, b, j, r, split);
+}
+
+template <class TT, int D>
+__global__ __launch_bounds__(kPfFewThreads, 1) void pf_few(PfArgs a) { few<TT, D>(a); }
 
 // Join the splits of one row: grid (q_len, HQ, batch), 256 / D threads per element,
 // each with the states of a batch of splits in flight at once (they come from
@@ -460,20 +607,22 @@ __global__ __launch_bounds__(256) void pf_join(PfArgs a) {
     p.lse[(int64_t)b * p.ls[0] + (int64_t)j * p.ls[1] + r] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
 
+enum PfKernel { kRows16, kRows32, kFew };
+
 struct PfPlan {
-  bool wide;  // pf_rows32 instead of pf_rows16
+  PfKernel kernel;
   int S, tiles;
   size_t bytes;
 };
 
-// Kernel and splits over the keys: as many splits as fill the chip once (one
-// work-group of pf_rows32 or two of pf_rows16 per compute unit), of at least 128
-// keys each.
+// Kernel and splits over the keys.  float32: pf_rows16.  bf16: pf_few up to 64 packed
+// rows, else pf_rows32.  As many splits as fill the chip once (one work-group of
+// pf_rows32, two of the others per compute unit), of at least 128 keys each.
 PfPlan pf_plan(const PrefillArgs& a) {
   PfPlan pl;
   const int64_t packed = (int64_t)a.q_len * a.G;
-  pl.wide = a.esize == 2 && packed > kPfRows;
-  const int rows = pl.wide ? kPf32Rows : kPfRows;
+  pl.kernel = a.esize == 4 ? kRows16 : packed > 2 * kPfFewRows ? kRows32 : kFew;
+  const int rows = pl.kernel == kRows32 ? kPf32Rows : pl.kernel == kFew ? kPfFewRows : kPfRows;
   pl.tiles = (int)((packed + rows - 1) / rows);
   const int64_t groups = (int64_t)pl.tiles * a.batch * a.H;
   int64_t keys = a.kv_len;
@@ -482,7 +631,7 @@ PfPlan pf_plan(const PrefillArgs& a) {
     if (most < keys) keys = most;
   }
   const int64_t most_s = keys / 128;
-  int64_t S = (pl.wide ? 256 : 512) / groups;
+  int64_t S = (pl.kernel == kRows32 ? 256 : 512) / groups;
   if (S > most_s) S = most_s;
   if (S > 64) S = 64;
   pl.S = S < 1 ? 1 : (int)S;
@@ -503,15 +652,16 @@ hipError_t run_prefill(const PrefillArgs& p, char* ws, hipStream_t s) {
   a.part = reinterpret_cast<float*>(ws);
   a.sc = (float)(1.4426950408889634 / sqrt((double)p.D));
   const dim3 grid(pf_grid(a));
-  if (pl.wide) {
-    if (p.D == 64) hipLaunchKernelGGL((pf_rows32<BF16, 64>), grid, dim3(kPf32Threads), 0, s, a);
+  const bool d64 = p.D == 64;
+  if (pl.kernel == kRows32) {
+    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64>), grid, dim3(kPf32Threads), 0, s, a);
     else hipLaunchKernelGGL((pf_rows32<BF16, 128>), grid, dim3(kPf32Threads), 0, s, a);
-  } else if (p.esize == 2) {
-    if (p.D == 64) hipLaunchKernelGGL((pf_rows16<BF16, 64>), grid, dim3(kPfThreads), 0, s, a);
-    else hipLaunchKernelGGL((pf_rows16<BF16, 128>), grid, dim3(kPfThreads), 0, s, a);
+  } else if (pl.kernel == kFew) {
+    if (d64) hipLaunchKernelGGL((pf_few<BF16, 64>), grid, dim3(kPfFewThreads), 0, s, a);
+    else hipLaunchKernelGGL((pf_few<BF16, 128>), grid, dim3(kPfFewThreads), 0, s, a);
   } else {
-    if (p.D == 64) hipLaunchKernelGGL((pf_rows16<F32, 64>), grid, dim3(kPfThreads), 0, s, a);
-    else hipLaunchKernelGGL((pf_rows16<F32, 128>), grid, dim3(kPfThreads), 0, s, a);
+    if (d64) hipLaunchKernelGGL(pf_rows16<64>, grid, dim3(kPfThreads), 0, s, a);
+    else hipLaunchKernelGGL(pf_rows16<128>, grid, dim3(kPfThreads), 0, s, a);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || pl.S == 1) return e;

@@ -142,8 +142,11 @@ class PagedConfig:
 
 
 def _fix(cfg, c, **more) -> None:
-    """Keeps the C view of a frozen configuration, a reference to it and the shapes it implies."""
-    for name, value in dict(_c=c, ref=ctypes.byref(c), **more).items():
+    """Keeps the C view of a frozen configuration, a reference to it, the types (of elements, float32,
+    int32) and the shapes it implies."""
+    import torch
+    types = (torch.bfloat16 if cfg.dtype == KVEC_BF16 else torch.float32, torch.float32, torch.int32)
+    for name, value in dict(_c=c, ref=ctypes.byref(c), types=types, **more).items():
         object.__setattr__(cfg, name, value)
 
 
@@ -481,17 +484,16 @@ def _call(name: str, stream, tensors, *args) -> None:
     assert dev >= 0, f"{name}: the tensors must be on a GPU"
     for t in tensors:
         assert t is None or t.get_device() == dev, f"{name}: the tensors must share a device"
-    if dev == torch.cuda.current_device():
-        _check(getattr(load(), name)(*args, _stream(stream)), name)
+    fn = getattr(_lib or load(), name)
+    # the current stream's handle, without a Stream object around it
+    st = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if dev == torch._C._cuda_getDevice():
+        status = fn(*args, st)
     else:
         with torch.cuda.device(dev):
-            _check(getattr(load(), name)(*args, _stream(stream)), name)
-
-
-def _types(cfg):
-    """(element type, float32, int32) of a configuration's tensors."""
-    import torch
-    return torch.bfloat16 if cfg.dtype == KVEC_BF16 else torch.float32, torch.float32, torch.int32
+            status = fn(*args, st)
+    if status:
+        _check(status, name)
 
 
 def _ws(ws):
@@ -509,7 +511,7 @@ def kvec_prefill_attention(cfg: AttentionConfig, q, k, v, out, ws=None, lse=None
     """q, out [b][HQ][q_len][d]; k, v [b][H][kv_len][d] (any leading strides); lse fp32
     [b][HQ][q_len], rows contiguous; q_lens, kv_lens int32 [b].  ws may be None when
     kvec_prefill_workspace_size(cfg) is 0."""
-    dt, f32, i32 = _types(cfg)
+    dt, f32, i32 = cfg.types
     qs, os_ = _rows3(q, cfg.q_shape, dt, "q"), _rows3(out, cfg.q_shape, dt, "out")
     ks, vs = _rows3(k, cfg.k_shape, dt, "k"), _rows3(v, cfg.k_shape, dt, "v")
     ls = None if lse is None else _rows2(lse, cfg.lse_shape, f32, "lse")
@@ -533,7 +535,7 @@ def kvec_paged_append(cfg: PagedConfig, q, k, v, positions, slots, q_out, k_pool
     [n_pages][H][page_size][d]; weights [d] (None: no norm); inv_freq float64 [rot_dim / 2]
     (None: no rotation); acc fp32 and pos int32 [n_pages][H][page_size]."""
     import torch
-    dt, f32, i32 = _types(cfg)
+    dt, f32, i32 = cfg.types
     n, d = q.shape[0], cfg.head_dim
     queries, keys = (n, cfg.n_q_heads, d), (n, cfg.n_kv_heads, d)
     qs, os_ = _rows2(q, queries, dt, "q"), _rows2(q_out, queries, dt, "q_out")
@@ -567,7 +569,7 @@ def kvec_paged_decode(cfg: PagedConfig, q, k_pool, v_pool, page_table, lens, out
     """q [b][HQ][d]; pools [n_pages][H][page_size][d] (K and V with the same strides);
     page_table int32 [b][max_pages]; lens int32 [b]; out fp32 [b][HQ][d]; lse fp32
     [b][HQ]; acc fp32 [n_pages][H][page_size].  max_len None: every slot of the table."""
-    dt, f32, i32 = _types(cfg)
+    dt, f32, i32 = cfg.types
     qs, ps = _rows2(q, cfg.q_shape, dt, "q"), _pools(cfg, dt, k_pool, v_pool)
     tb, ln = _dense(page_table, cfg.table_shape, i32, "page_table"), _dense(lens, cfg.len_shape, i32, "lens")
     op, lp = _dense(out, cfg.q_shape, f32, "out"), _dense(lse, cfg.lse_shape, f32, "lse")
@@ -590,7 +592,7 @@ def kvec_paged_evict(cfg: PagedConfig, budget: int, k_pool, v_pool, page_table, 
     """Pools and tables as in kvec_paged_decode; acc fp32 and pos int32
     [n_pages][H][page_size]; lens, n_seen, lens_out int32 [b] (lens_out may be lens);
     kept int32 [b][H][budget]."""
-    dt, f32, i32 = _types(cfg)
+    dt, f32, i32 = cfg.types
     ps = _pools(cfg, dt, k_pool, v_pool)
     tb, ln = _dense(page_table, cfg.table_shape, i32, "page_table"), _dense(lens, cfg.len_shape, i32, "lens")
     ns, lo = _dense(n_seen, cfg.len_shape, i32, "n_seen"), _dense(lens_out, cfg.len_shape, i32, "lens_out")
