@@ -112,6 +112,21 @@ struct Columns16 {
     return mma(k, q, f32x4{0.f, 0.f, 0.f, 0.f});
   }
 
+  // ... with the NG groups at `grp`, the products of the groups interleaved (two
+  // accumulation chains).
+  __device__ __forceinline__ void logits(f32x4 (&x)[NG], const char* grp, int lane) const {
+    Frag<TT, D> k[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      k[g].load_lds(reinterpret_cast<const uint4*>(grp + g * RG::BYTES), lane & 15, lane >> 4, RG::SWZ);
+      x[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll
+    for (int j = 0; j < Frag<TT, D>::KS; ++j)
+#pragma unroll
+      for (int g = 0; g < NG; ++g) x[g] = mma1(k[g], q, x[g], j);
+  }
+
   // One step of the online softmax: x are base-2 logits, -inf where masked.
   // A column that has seen no key keeps m = -inf, and the exponentials use 0
   // for it: 2^(-inf - 0) = 0 instead of 2^(-inf + inf).

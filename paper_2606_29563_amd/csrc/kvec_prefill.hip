@@ -93,8 +93,7 @@ template <int D>
 __global__ __launch_bounds__(kPfThreads) void pf_rows16(PfArgs a) {
   using TT = F32;
   using RG = RowGroup<TT, D>;
-  constexpr int NG = 1, ES = RG::ES;
-  constexpr int GRPS = kPfKeys / 16;
+  constexpr int ES = RG::ES, GRPS = kPfKeys / 16;
   constexpr int BUF = 2 * GRPS * RG::BYTES;       // K groups, then V groups
   constexpr int PER = 2 * GRPS * RG::NI / 4;      // copies per wave and tile
   __shared__ __align__(1024) char smem[2 * BUF];
@@ -113,7 +112,7 @@ __global__ __launch_bounds__(kPfThreads) void pf_rows16(PfArgs a) {
   const int per = (sp.n + a.S - 1) / a.S;
   const int t0 = min(split * per, sp.n), t1 = min(t0 + per, sp.n);
 
-  Columns16<TT, D, NG, false> col;
+  Columns16<TT, D, GRPS, false> col;
   col.clear();
   col.q.zero();
   if (live) col.q.load(p.q + ((int64_t)b * p.qs[0] + (int64_t)j * p.qs[1] + (int64_t)r * p.qs[2]) * ES, c);
@@ -147,20 +146,14 @@ __global__ __launch_bounds__(kPfThreads) void pf_rows16(PfArgs a) {
     const char* kb = smem + u * BUF;
     const int key0 = sp.key0(t);
     const bool open = sp.open(key0) && live;
+    f32x4 x[GRPS];
+    col.logits(x, kb, lane);
 #pragma unroll
-    for (int g0 = 0; g0 < GRPS; g0 += NG) {
-      f32x4 x[NG];
+    for (int g = 0; g < GRPS; ++g)
 #pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        x[g] = col.logits(kb + (g0 + g) * RG::BYTES, lane);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int key = key0 + 16 * (g0 + g) + 4 * c + e;
-          x[g][e] = open || sp.sees(key, pos) ? x[g][e] * a.sc : -INFINITY;
-        }
-      }
-      col.absorb(x, kb + (GRPS + g0) * RG::BYTES, lane);
-    }
+      for (int e = 0; e < 4; ++e)
+        x[g][e] = open || sp.sees(key0 + 16 * g + 4 * c + e, pos) ? x[g][e] * a.sc : -INFINITY;
+    col.absorb(x, kb + GRPS * RG::BYTES, lane);
   }
   col.l = col_sum4(col.l);
   if (!live) return;
@@ -569,42 +562,56 @@ __device__ __forceinline__ void few(const PfArgs& a) {
 template <class TT, int D>
 __global__ __launch_bounds__(kPfFewThreads, 1) void pf_few(PfArgs a) { few<TT, D>(a); }
 
-// Join the splits of one row: grid (q_len, HQ, batch), 256 / D threads per element,
-// each with the states of a batch of splits in flight at once (they come from
-// other XCDs: every batch is one memory round trip).
-template <class T, int D>
+// Join the splits of the rows: grid (row groups, HQ, batch).  The 256 / D threads of an
+// element take a row each (ROWS; few splits), or share one row's splits.  A batch of
+// states is in flight at once (they come from other XCDs: one memory round trip).
+constexpr int kJoinBatch = 8;
+
+template <class T, int D, bool ROWS>
 __global__ __launch_bounds__(256) void pf_join(PfArgs a) {
-  constexpr int PARTS = 256 / D, BATCH = 8;
-  __shared__ float st[PARTS][3][D];
+  constexpr int PARTS = 256 / D;
+  __shared__ float st[ROWS ? 1 : PARTS][3][ROWS ? 1 : D];
   const PrefillArgs& p = a.p;
-  const int r = blockIdx.x, j = blockIdx.y, b = blockIdx.z, e = threadIdx.x % D, part = threadIdx.x / D;
+  const int e = threadIdx.x % D, part = threadIdx.x / D;
+  const int r = ROWS ? blockIdx.x * PARTS + part : blockIdx.x, j = blockIdx.y, b = blockIdx.z;
   const int nq = p.q_lens ? min(max(p.q_lens[b], 0), p.q_len) : p.q_len;
   if (r >= nq) return;
   const float* pp = a.part + (((int64_t)b * p.HQ + j) * p.q_len + r) * a.S * (D + 2);
   float m = -INFINITY, l = 0.f, o = 0.f;
-  for (int s0 = part * BATCH; s0 < a.S; s0 += PARTS * BATCH) {
-    float ms[BATCH], ls[BATCH], os[BATCH];
+  for (int s0 = ROWS ? 0 : part * kJoinBatch; s0 < a.S; s0 += (ROWS ? 1 : PARTS) * kJoinBatch) {
+    float ms[kJoinBatch], ls[kJoinBatch], os[kJoinBatch];
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i) {
+    for (int i = 0; i < kJoinBatch; ++i) {
       const float* q = pp + (int64_t)min(s0 + i, a.S - 1) * (D + 2);
       ms[i] = s0 + i < a.S ? q[0] : -INFINITY;
       ls[i] = q[1];
       os[i] = q[2 + e];
     }
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i) state_merge(m, l, o, ms[i], ls[i], os[i]);
+    for (int i = 0; i < kJoinBatch; ++i) state_merge(m, l, o, ms[i], ls[i], os[i]);
   }
-  st[part][0][e] = m;
-  st[part][1][e] = l;
-  st[part][2][e] = o;
-  __syncthreads();
-  if (part) return;
+  if constexpr (!ROWS) {
+    st[part][0][e] = m;
+    st[part][1][e] = l;
+    st[part][2][e] = o;
+    __syncthreads();
+    if (part) return;
 #pragma unroll
-  for (int i = 1; i < PARTS; ++i) state_merge(m, l, o, st[i][0][e], st[i][1][e], st[i][2][e]);
+    for (int i = 1; i < PARTS; ++i) state_merge(m, l, o, st[i][0][e], st[i][1][e], st[i][2][e]);
+  }
   T* dst = reinterpret_cast<T*>(p.out) + (int64_t)b * p.os[0] + (int64_t)j * p.os[1] + (int64_t)r * p.os[2];
   dst[e] = (T)(m == -INFINITY ? 0.f : o / l);
   if (p.lse && e == 0)
     p.lse[(int64_t)b * p.ls[0] + (int64_t)j * p.ls[1] + r] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+
+template <class T, int D>
+void launch_join(const PfArgs& a, hipStream_t s) {
+  const PrefillArgs& p = a.p;
+  if (a.S <= kJoinBatch)
+    hipLaunchKernelGGL((pf_join<T, D, true>), dim3((p.q_len + 256 / D - 1) / (256 / D), p.HQ, p.batch), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((pf_join<T, D, false>), dim3(p.q_len, p.HQ, p.batch), dim3(256), 0, s, a);
 }
 
 enum PfKernel { kRows16, kRows32, kFew };
@@ -615,28 +622,52 @@ struct PfPlan {
   size_t bytes;
 };
 
-// Kernel and splits over the keys.  float32: pf_rows16.  bf16: pf_few up to 64 packed
-// rows, else pf_rows32.  As many splits as fill the chip once (one work-group of
-// pf_rows32, two of the others per compute unit), of at least 128 keys each.
+// Kernel and splits over the keys: the pair with the least estimated time
+//   max(key tiles of the longest work-group * us a tile,
+//       key tiles of all / work-groups at a time * us a tile,
+//       K and V at 4.5 TB/s) + what the join costs.
+// A tile of pf_rows32 (256 rows, 64 keys, one work-group per compute unit) takes
+// 1.95 us, of pf_few (32 rows, two waves with 32 keys each, two work-groups) 1.3, of
+// pf_rows16 (64 rows, 32 keys, two) 2.6; the join a launch (4 us), a round
+// trip per 16 splits and the partial states there and back at 4 TB/s.  us measured, pf_few / pf_rows32 unsplit or split /
+// estimates, Llama heads: 250 rows 10 / 16 / 9 and 8, 1000 rows 31 / 44 (two splits)
+// / 21 and 31 (unsplit), the Qwen heads' 2000 rows 78 / 62 / 69 and 62, 100 rows over
+// 5000 keys 32 (four splits) / 29 (16) / 31 and 27.
 PfPlan pf_plan(const PrefillArgs& a) {
-  PfPlan pl;
-  const int64_t packed = (int64_t)a.q_len * a.G;
-  pl.kernel = a.esize == 4 ? kRows16 : packed > 2 * kPfFewRows ? kRows32 : kFew;
-  const int rows = pl.kernel == kRows32 ? kPf32Rows : pl.kernel == kFew ? kPfFewRows : kPfRows;
-  pl.tiles = (int)((packed + rows - 1) / rows);
-  const int64_t groups = (int64_t)pl.tiles * a.batch * a.H;
-  int64_t keys = a.kv_len;
-  if (a.window > 0) {
-    const int64_t most = (int64_t)a.window + a.sinks + rows;
-    if (most < keys) keys = most;
+  const int64_t packed = (int64_t)a.q_len * a.G, heads = (int64_t)a.batch * a.H;
+  PfPlan best = {};
+  double least = 0;
+  auto consider = [&](PfKernel kernel, int rows, int keys, int at_a_time, double us) {
+    const int64_t tiles = (packed + rows - 1) / rows, groups = tiles * heads;
+    // keys that a row tile sees at most, and on average
+    double most = a.kv_len, mean = a.kv_len - 0.5 * (a.q_len < a.kv_len ? a.q_len : a.kv_len);
+    const double span = (double)a.window + a.sinks + (double)rows / a.G;
+    if (a.window > 0 && span < most) most = span;
+    if (mean > most) mean = most;
+    const double state = 2.0 * a.batch * a.HQ * a.q_len * (a.D + 2) * 4 / 4e6;  // us per split
+    const double all = groups * (mean / keys) / at_a_time * us;
+    const double read = heads * most * 2 * a.D * a.esize / 4.5e6;
+    const double floor = all > read ? all : read;
+    for (int S = 1; S <= 64 && (S == 1 || most / S >= 64); ++S) {
+      const double longest = ((double)(int64_t)((most / keys + S - 0.001) / S) + 1) * us;
+      const double t = (longest > floor ? longest : floor) + (S > 1 ? 4.0 + 0.7 * ((S + 15) / 16) + S * state : 0.0);
+      if (best.S == 0 || t < least) {
+        least = t;
+        best.kernel = kernel;
+        best.S = S;
+        best.tiles = (int)tiles;
+      }
+      if (longest <= floor) break;  // more splits only add states
+    }
+  };
+  if (a.esize == 4) {
+    consider(kRows16, kPfRows, kPfKeys, 512, 2.6);
+  } else {
+    consider(kRows32, kPf32Rows, kPf32Keys, 256, 1.95);
+    consider(kFew, kPfFewRows, 2 * kPfFewKeys, 512, 1.3);
   }
-  const int64_t most_s = keys / 128;
-  int64_t S = (pl.kernel == kRows32 ? 256 : 512) / groups;
-  if (S > most_s) S = most_s;
-  if (S > 64) S = 64;
-  pl.S = S < 1 ? 1 : (int)S;
-  pl.bytes = pl.S > 1 ? (size_t)a.batch * a.HQ * a.q_len * pl.S * (a.D + 2) * 4 : 0;
-  return pl;
+  best.bytes = best.S > 1 ? (size_t)a.batch * a.HQ * a.q_len * best.S * (a.D + 2) * 4 : 0;
+  return best;
 }
 
 }  // namespace
@@ -665,13 +696,12 @@ hipError_t run_prefill(const PrefillArgs& p, char* ws, hipStream_t s) {
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || pl.S == 1) return e;
-  const dim3 jgrid(p.q_len, p.HQ, p.batch);
   if (p.esize == 2) {
-    if (p.D == 64) hipLaunchKernelGGL((pf_join<__bf16, 64>), jgrid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((pf_join<__bf16, 128>), jgrid, dim3(256), 0, s, a);
+    if (d64) launch_join<__bf16, 64>(a, s);
+    else launch_join<__bf16, 128>(a, s);
   } else {
-    if (p.D == 64) hipLaunchKernelGGL((pf_join<float, 64>), jgrid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((pf_join<float, 128>), jgrid, dim3(256), 0, s, a);
+    if (d64) launch_join<float, 64>(a, s);
+    else launch_join<float, 128>(a, s);
   }
   return hipGetLastError();
 }
