@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from dataclasses import dataclass
+from dataclasses import dataclass, fields
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libkvec.so")
@@ -116,6 +116,9 @@ class AttentionConfig:
     def c(self) -> kvec_attention_config:
         return self._c
 
+    def __reduce__(self):
+        return _rebuild(self)
+
 
 @dataclass(frozen=True)
 class PagedConfig:
@@ -139,6 +142,14 @@ class PagedConfig:
 
     def c(self) -> kvec_paged_config:
         return self._c
+
+    def __reduce__(self):
+        return _rebuild(self)
+
+
+def _rebuild(cfg):
+    """Copies and pickles of a frozen configuration are made from its fields."""
+    return type(cfg), tuple(getattr(cfg, f.name) for f in fields(cfg))
 
 
 def _fix(cfg, c, **more) -> None:

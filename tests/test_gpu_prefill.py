@@ -101,25 +101,45 @@ def test_prefill(gpu_lib, b, H, G, d, nq, nk, dt, window, sinks, q_lens, kv_lens
     assert o2.equal(out)
 
 
-@pytest.mark.parametrize("dt,window,sinks", [("bf16", 0, 0), ("bf16", 500, 20), ("f32", 0, 0)])
-def test_prefill_long(gpu_lib, dt, window, sinks):
-    """Many tiles and work-groups, some rows checked."""
-    q, k, v = _tensors(1, 2, 4, 128, 1300, 2500, dt, seed=5)
-    out, lse = _run(gpu_lib, q, k, v, window, sinks)
-    _check(q, k, v, out, lse, window, sinks, rows=[0, 1, 63, 64, 127, 640, 1023, 1298, 1299])
+LONG = [  # b, H, G, d, q rows, keys, dtype, window, sinks, q_lens, kv_lens
+    (1, 2, 4, 128, 1300, 2500, "bf16", 0, 0, None, None),
+    (1, 2, 4, 128, 1300, 2500, "bf16", 500, 20, None, None),
+    (1, 2, 4, 128, 1300, 2500, "f32", 0, 0, None, None),
+    # more row tiles than compute units
+    (1, 8, 4, 128, 2100, 2100, "bf16", 0, 0, None, None),
+    (2, 8, 2, 64, 4200, 4300, "bf16", 0, 0, [4200, 4111], [4300, 4000]),
+    (3, 4, 7, 128, 1999, 2400, "bf16", 700, 100, [1999, 50, 1500], [2400, 2400, 1200]),
+    (1, 8, 16, 64, 1100, 1100, "bf16", 300, 0, None, None),
+    (1, 5, 5, 128, 2300, 2300, "bf16", 0, 0, None, None),
+    # ... split over the keys
+    (1, 8, 4, 128, 100, 5000, "bf16", 0, 0, None, None),
+    (1, 8, 4, 64, 200, 9000, "bf16", 4000, 65, None, None),
+]
+
+
+@pytest.mark.parametrize("b,H,G,d,nq,nk,dt,window,sinks,q_lens,kv_lens", LONG)
+def test_prefill_long(gpu_lib, b, H, G, d, nq, nk, dt, window, sinks, q_lens, kv_lens):
+    """Many tiles and work-groups, some rows checked: the first and last of tiles."""
+    q, k, v = _tensors(b, H, G, d, nq, nk, dt, seed=5)
+    out, lse = _run(gpu_lib, q, k, v, window, sinks, q_lens, kv_lens)
+    rows = sorted({r for r in (0, 1, 15, 16, 49, 63, 64, 99, 127, 255, 640, 1023, nq // 2, nq - 2, nq - 1) if r < nq})
+    _check(q, k, v, out, lse, window, sinks, q_lens, kv_lens, rows=rows)
 
 
 def test_prefill_extreme_logits(gpu_lib):
     """Logits of thousands that grow along the keys, fall along them, and are all equal."""
     import torch
-    for kind in ("grow", "fall", "equal"):
-        q, k, v = _tensors(1, 1, 2, 64, 300, 300, "bf16", seed=6)
-        ramp = torch.arange(300, device="cuda")[:, None].float()
-        u = torch.ones(64, device="cuda")
-        k.copy_((u * (ramp / 4 if kind == "grow" else -ramp / 4 if kind == "fall" else 0 * ramp + 1)).to(k.dtype))
-        q.copy_(q.abs())
-        out, lse = _run(gpu_lib, q, k, v)
-        _check(q, k, v, out, lse, rows=list(range(0, 300, 7)))
+    for n, H, every in ((300, 1, 7), (2100, 16, 211)):  # few and many row tiles
+        for kind in ("grow", "fall", "equal", "one"):
+            q, k, v = _tensors(1, H, 2, 64, n, n, "bf16", seed=6)
+            ramp = torch.arange(n, device="cuda")[:, None].float()
+            u = torch.ones(64, device="cuda")
+            k.copy_((u * (ramp / 4 if kind == "grow" else -ramp / 4 if kind == "fall" else 0 * ramp + 1)).to(k.dtype))
+            if kind == "one":  # a single key far above the others, behind many
+                k[:, :, n // 2] *= 50
+            q.copy_(q.abs())
+            out, lse = _run(gpu_lib, q, k, v)
+            _check(q[:, :2], k[:, :1], v[:, :1], out[:, :2], lse[:, :2], rows=list(range(0, n, every)))
 
 
 def test_prefill_strides_of_outputs_and_shared_keys(gpu_lib):

@@ -145,3 +145,15 @@ def test_binding_checks_tensors():
                 dict(q=q.transpose(1, 2).contiguous().transpose(1, 2)), {}):  # the last: nothing is on a GPU
         with pytest.raises(AssertionError):
             kvec.kvec_paged_decode(c, **{**good, **bad})
+
+
+@pytest.mark.parametrize("cfg", [_paged(), _attn(window=7)])
+def test_configurations_copy(cfg):
+    import copy
+    import dataclasses
+    import pickle
+    for other in (copy.deepcopy(cfg), pickle.loads(pickle.dumps(cfg)), dataclasses.replace(cfg)):
+        assert other == cfg and bytes(other.c()) == bytes(cfg.c())
+    assert dataclasses.replace(cfg, batch=7).c().batch == 7
+    with pytest.raises(dataclasses.FrozenInstanceError):
+        cfg.batch = 3
