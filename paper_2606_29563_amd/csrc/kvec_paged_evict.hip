@@ -63,12 +63,18 @@ __device__ __forceinline__ int scan_before(int v, int* tmp, int& total) {
   return before + incl - v;
 }
 
-// The keys of a tile of CAP slots are made in LDS, EB loads of a thread in flight at
-// once; sequences of one tile make them once, longer ones in every pass.
+// acc and pos are aligned to their elements
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+
+// The keys of a tile of CAP slots are made in LDS, the loads of EB quads of slots of a
+// thread in flight at once (one round trip for the page entries and one for weights
+// and positions; slot by slot, three of each for 24k slots, the selection of 4 x 24k
+// slots took 26 us instead of 24); sequences of one tile make them once, longer ones in every pass.
 template <int CAP, int EB>
 __global__ __launch_bounds__(kEvThreads) void ev_select(EvArgs a) {
   static_assert(CAP < 1 << 16, "two counts of a tile share a word");
-  __shared__ uint32_t keys[CAP];
+  __shared__ __align__(16) uint32_t keys[CAP];
   __shared__ uint32_t hist[2][kEvBins];
   __shared__ int tmp[2][kEvWaves];
   __shared__ uint32_t found[3][2];
@@ -86,29 +92,36 @@ __global__ __launch_bounds__(kEvThreads) void ev_select(EvArgs a) {
   const int64_t recent = a.window > 0 ? (int64_t)a.n_seen[b] - a.window : INT64_MAX;
   for (int i = tid; i < 2 * kEvBins; i += kEvThreads) (&hist[0][0])[i] = 0;
 
+  // four neighbouring slots a load (they share a page)
   auto make_keys = [&](int t0, int m) {
-    for (int i0 = 0; i0 < m; i0 += EB * kEvThreads) {
+    const int quads = (m + 3) / 4;
+    for (int q0 = 0; q0 < quads; q0 += EB * kEvThreads) {
       int page[EB], row[EB];
 #pragma unroll
-      for (int i = 0; i < EB; ++i) {  // slots behind the tile read its last one
-        const int s = t0 + min(i0 + i * kEvThreads + tid, m - 1);
+      for (int i = 0; i < EB; ++i) {  // quads behind the tile read its last one
+        const int s = t0 + 4 * min(q0 + i * kEvThreads + tid, quads - 1);
         page[i] = ev_page(a, b, s);
         row[i] = s - ev_page_index(a, s) * a.c.ps;
       }
-      float x[EB];
-      int p[EB];
+      f32x4_any x[EB];
+      i32x4_any p[EB];
 #pragma unroll
       for (int i = 0; i < EB; ++i) {
         const int64_t at = ((int64_t)max(page[i], 0) * H + h) * a.c.ps + row[i];
-        x[i] = a.acc[at];
-        p[i] = a.pos[at];
+        x[i] = *reinterpret_cast<const f32x4_any*>(a.acc + at);
+        p[i] = *reinterpret_cast<const i32x4_any*>(a.pos + at);
       }
 #pragma unroll
       for (int i = 0; i < EB; ++i) {
-        const bool safe = p[i] < a.sinks || p[i] >= recent;
-        // + 0: the two zeros are equal
-        const uint32_t key = page[i] < 0 ? 0u : safe ? 0xffffffffu : x[i] != x[i] ? 0u : float_key(x[i] + 0.f);
-        if (i0 + i * kEvThreads + tid < m) keys[i0 + i * kEvThreads + tid] = key;
+        uint32_t key[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool safe = p[i][e] < a.sinks || p[i][e] >= recent;
+          // + 0: the two zeros are equal
+          key[e] = page[i] < 0 ? 0u : safe ? 0xffffffffu : x[i][e] != x[i][e] ? 0u : float_key(x[i][e] + 0.f);
+        }
+        const int q = q0 + i * kEvThreads + tid;
+        if (q < quads) *reinterpret_cast<uint4*>(keys + 4 * q) = make_uint4(key[0], key[1], key[2], key[3]);
       }
     }
   };
@@ -173,27 +186,29 @@ __global__ __launch_bounds__(kEvThreads) void ev_select(EvArgs a) {
     for (int i = i0; i < i1; ++i) ties += keys[i] == cut;
     const int tie0 = need - scan_before(ties, tmp[0], total);  // ties wanted from this run on
     need -= total;
-    int tie = tie0, counts = 0;  // kept behind B, and evicted below it in the upper half
+    // the run as two masks: kept behind B, evicted below it
+    static_assert(((CAP + kEvThreads - 1) / kEvThreads | 1) <= 64, "a run's slots are bits of a word");
+    uint64_t late = 0, holes = 0;
+    int tie = tie0;
 #pragma unroll 4
     for (int i = i0; i < i1; ++i) {
       const uint32_t k = keys[i];
       const bool keep = k > cut || (k == cut && tie > 0), low = t0 + i < B;
       tie -= k == cut;
-      counts += keep ? (low ? 0 : 1) : (low ? 1 << 16 : 0);
+      late |= (uint64_t)(keep && !low) << (i - i0);
+      holes |= (uint64_t)(!keep && low) << (i - i0);
     }
-    const int before = scan_before(counts, tmp[1], total);
-    int at_late = late0 + (before & 0xffff), at_hole = hole0 + (int)((uint32_t)before >> 16);
-    late0 += total & 0xffff;
-    hole0 += (int)((uint32_t)total >> 16);
-    tie = tie0;
-#pragma unroll 4
-    for (int i = i0; i < i1; ++i) {
-      const uint32_t k = keys[i];
-      const bool keep = k > cut || (k == cut && tie > 0), low = t0 + i < B;
-      tie -= k == cut;
-      if (keep && !low) src[at_late++] = t0 + i;
-      if (!keep && low) dst[at_hole++] = t0 + i;
-    }
+    const int before = scan_before((int)__popcll(late) | (int)__popcll(holes) << 16, tmp[1], total);
+    // (every thread is done with the keys:) the tile's lists, in LDS, then in whole lines
+    const int n_late = total & 0xffff, n_holes = (int)((uint32_t)total >> 16);
+    int at_late = before & 0xffff, at_hole = n_late + (int)((uint32_t)before >> 16);
+    for (; late; late &= late - 1) keys[at_late++] = t0 + i0 + __builtin_ctzll(late);
+    for (; holes; holes &= holes - 1) keys[at_hole++] = t0 + i0 + __builtin_ctzll(holes);
+    __syncthreads();
+    for (int i = tid; i < n_late; i += kEvThreads) src[late0 + i] = (int)keys[i];
+    for (int i = tid; i < n_holes; i += kEvThreads) dst[hole0 + i] = (int)keys[n_late + i];
+    late0 += n_late;
+    hole0 += n_holes;
     __syncthreads();  // tmp, before the next tile
   });
   // B slots are kept, so as many are kept behind B as are evicted below it
@@ -269,8 +284,8 @@ hipError_t run_paged_evict(const PagedView& c, int budget, int window, int sinks
   a.src = reinterpret_cast<int32_t*>(ws);
   a.dst = reinterpret_cast<int32_t*>(ws + up256(bh * a.cap * 4));
   const dim3 grid(c.H, c.batch);
-  if (c.max_len <= 4096) hipLaunchKernelGGL((ev_select<4096, 4>), grid, dim3(kEvThreads), 0, s, a);
-  else hipLaunchKernelGGL((ev_select<32768, 8>), grid, dim3(kEvThreads), 0, s, a);
+  if (c.max_len <= 4096) hipLaunchKernelGGL((ev_select<4096, 1>), grid, dim3(kEvThreads), 0, s, a);
+  else hipLaunchKernelGGL((ev_select<32768, 3>), grid, dim3(kEvThreads), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int row = c.D * c.esize, per = kMvThreads / (row / 16);
