@@ -256,9 +256,10 @@ struct Columns32 {
   // Key of element e of block g, from the tile's first.
   __device__ __forceinline__ int key(int g, int e) const { return 32 * g + 8 * (e >> 2) + 4 * hh + (e & 3); }
 
-  // Probabilities of a tile's logits, -inf where masked, as 16-key steps of the V product.
-  template <int NB>
-  __device__ __forceinline__ void weigh(const f32x16 (&x)[NB], float sc, bf16x8 (&pf)[2 * NB]) {
+  // Probabilities of a tile's logits, -inf where masked, as 16-key steps of the V product;
+  // lo: what their rounding to bf16 leaves, rounded again (SPLIT).
+  template <int NB, bool SPLIT>
+  __device__ __forceinline__ void weigh(const f32x16 (&x)[NB], float sc, bf16x8 (&pf)[2 * NB], bf16x8 (&lo)[2 * NB]) {
     float sum;
     auto against = [&](float ref) {
       sum = 0.f;
@@ -268,7 +269,9 @@ struct Columns32 {
         for (int e = 0; e < 16; ++e) {
           const float v = __builtin_amdgcn_exp2f(fmaf(x[g][e], sc, -ref));
           sum += v;
-          pf[2 * g + (e >> 3)][e & 7] = (__bf16)v;
+          const __bf16 top = (__bf16)v;
+          pf[2 * g + (e >> 3)][e & 7] = top;
+          if constexpr (SPLIT) lo[2 * g + (e >> 3)][e & 7] = (__bf16)(v - (float)top);
         }
     };
     against(m);
@@ -428,7 +431,7 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
           if (!sp.sees(key0 + col.key(g, e), pos)) x[g][e] = -INFINITY;
     }
     bf16x8 pf[4];
-    col.weigh(x, a.sc, pf);
+    col.template weigh<2, false>(x, a.sc, pf, pf);
     // (the compiler's transposing read waits for the copies in flight, which were
     // issued half a tile before; written out with waits of its own it was slower, 566
     // us for 545, because then the products cannot be scheduled between the reads)
@@ -453,7 +456,9 @@ __global__ __launch_bounds__(kPf32Threads, 2) void pf_rows32(PfArgs a) { rows32<
 // Few rows, bf16: a work-group of two waves takes 32 packed rows, both waves the
 // same ones.  The waves go over the 32-key steps of the work-group's split in
 // turn, each with an LDS ring of two steps of its own and no barrier before the
-// end, where their states are joined: what bounds it is the reading of K and V.
+// end, where their states are joined.  What bounds it is the latency and the reading
+// of K and V (8 rows of 32 heads over 16k keys: 18 us, 3.7 TB/s), so the probabilities
+// go into the product as two bf16 terms.
 constexpr int kPfFewThreads = 128, kPfFewRows = 32, kPfFewKeys = 32;
 
 template <class TT, int D>
@@ -515,8 +520,8 @@ __device__ __forceinline__ void few(const PfArgs& a) {
       for (int e = 0; e < 16; ++e)
         if (!sp.sees(key0 + col.key(0, e), pos)) x[0][e] = -INFINITY;
     }
-    bf16x8 pf[2];
-    col.weigh(x, a.sc, pf);
+    bf16x8 pf[2], lo[2];
+    col.template weigh<1, true>(x, a.sc, pf, lo);
     uint32_t at[2 * DT];
 #pragma unroll
     for (int e = 0; e < 2 * DT; ++e) at[e] = lds_addr(kb) + HALF + col.voff[e];
@@ -528,8 +533,11 @@ __device__ __forceinline__ void few(const PfArgs& a) {
     u ^= 1;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(join8(v0[2 * dt], v0[2 * dt + 1]), pf[0], col.o[dt], 0, 0, 0);
-      col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(join8(v1[2 * dt], v1[2 * dt + 1]), pf[1], col.o[dt], 0, 0, 0);
+      const bf16x8 a0 = join8(v0[2 * dt], v0[2 * dt + 1]), a1 = join8(v1[2 * dt], v1[2 * dt + 1]);
+      col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a0, pf[0], col.o[dt], 0, 0, 0);
+      col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1, pf[1], col.o[dt], 0, 0, 0);
+      col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a0, lo[0], col.o[dt], 0, 0, 0);
+      col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1, lo[1], col.o[dt], 0, 0, 0);
     }
   }
   wait_vmem<0>();
