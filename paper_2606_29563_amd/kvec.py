@@ -157,6 +157,7 @@ def _fix(cfg, c, **more) -> None:
     int32) and the shapes it implies."""
     import torch
     types = (torch.bfloat16 if cfg.dtype == KVEC_BF16 else torch.float32, torch.float32, torch.int32)
+    more["long_types"] = (torch.float64, torch.int64)
     for name, value in dict(_c=c, ref=ctypes.byref(c), types=types, **more).items():
         object.__setattr__(cfg, name, value)
 
@@ -459,43 +460,30 @@ def kvec_decode_attention_noalloc(cfg: Config, q, k_cache, v_cache, out, idx=Non
            "kvec_decode_attention_noalloc")
 
 
+# The calls below are made once per layer and token, where the launch is as short as
+# the marshalling: each checks its tensors in one expression, and only a failure goes
+# through them again for the message.
+
 _I64x2, _I64x3 = ctypes.c_int64 * 2, ctypes.c_int64 * 3
 
 
-def _rows2(t, shape, dtype, what: str):
-    """Checks a tensor [.][.][d] of rows, its last dimension contiguous; its leading strides."""
-    st = t.stride()
-    assert t.shape == shape, f"{what} must be {shape}, not {tuple(t.shape)}"
-    assert t.dtype is dtype and st[2] == 1, f"{what} must be {dtype}, its last dimension contiguous"
-    return _I64x2(st[0], st[1])
+def _refuse(name: str, *tensors) -> None:
+    """Raises for the first of (what, tensor, shape, dtype, contiguous) that is not what it says."""
+    first = tensors[0][1]
+    for what, t, shape, dtype, dense in tensors:
+        if t is None:
+            continue
+        assert tuple(t.shape) == tuple(shape), f"{name}: {what} must be {tuple(shape)}, not {tuple(t.shape)}"
+        assert t.dtype == dtype, f"{name}: {what} must be {dtype}, not {t.dtype}"
+        assert t.is_contiguous() if dense else t.stride(-1) == 1, \
+            f"{name}: {what} must be contiguous" + ("" if dense else " in its last dimension")
+        assert t.is_cuda and t.device == first.device, f"{name}: {what} must be on the GPU of the other tensors"
+    raise AssertionError(f"{name}: K and V pools must have the same strides, and a workspace be on their GPU")
 
 
-def _rows3(t, shape, dtype, what: str):
-    """As _rows2 for [.][.][.][d]."""
-    st = t.stride()
-    assert t.shape == shape, f"{what} must be {shape}, not {tuple(t.shape)}"
-    assert t.dtype is dtype and st[3] == 1, f"{what} must be {dtype}, its last dimension contiguous"
-    return _I64x3(st[0], st[1], st[2])
-
-
-def _dense(t, shape, dtype, what: str) -> int | None:
-    """Checks a contiguous tensor (None passes); its address."""
-    if t is None:
-        return None
-    assert t.shape == shape and t.is_contiguous(), f"{what} must be contiguous {shape}, not {tuple(t.shape)}"
-    assert t.dtype is dtype, f"{what} must be {dtype}"
-    return t.data_ptr()
-
-
-def _call(name: str, stream, tensors, *args) -> None:
-    """The library's call `name` with the tensors' device current, on its current stream
-    unless one is given.  The tensors (None passes) must share one GPU."""
+def _launch(fn, dev: int, stream, args, name: str) -> None:
+    """fn(*args, stream handle) with device `dev` current, on its current stream unless one is given."""
     import torch
-    dev = tensors[0].get_device()
-    assert dev >= 0, f"{name}: the tensors must be on a GPU"
-    for t in tensors:
-        assert t is None or t.get_device() == dev, f"{name}: the tensors must share a device"
-    fn = getattr(_lib or load(), name)
     # the current stream's handle, without a Stream object around it
     st = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
     if dev == torch._C._cuda_getDevice():
@@ -505,10 +493,6 @@ def _call(name: str, stream, tensors, *args) -> None:
             status = fn(*args, st)
     if status:
         _check(status, name)
-
-
-def _ws(ws):
-    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
 
 
 def kvec_prefill_workspace_size(cfg: AttentionConfig) -> int:
@@ -523,20 +507,31 @@ def kvec_prefill_attention(cfg: AttentionConfig, q, k, v, out, ws=None, lse=None
     [b][HQ][q_len], rows contiguous; q_lens, kv_lens int32 [b].  ws may be None when
     kvec_prefill_workspace_size(cfg) is 0."""
     dt, f32, i32 = cfg.types
-    qs, os_ = _rows3(q, cfg.q_shape, dt, "q"), _rows3(out, cfg.q_shape, dt, "out")
-    ks, vs = _rows3(k, cfg.k_shape, dt, "k"), _rows3(v, cfg.k_shape, dt, "v")
-    ls = None if lse is None else _rows2(lse, cfg.lse_shape, f32, "lse")
-    ql, kl = _dense(q_lens, cfg.len_shape, i32, "q_lens"), _dense(kv_lens, cfg.len_shape, i32, "kv_lens")
-    wp, wn = _ws(ws)
-    _call("kvec_prefill_attention", stream, (q, k, v, out, ws, lse, q_lens, kv_lens), cfg.ref, q.data_ptr(), qs,
-          k.data_ptr(), ks, v.data_ptr(), vs, ql, kl, out.data_ptr(), os_, _ptr(lse), ls, wp, wn)
-
-
-def _pools(cfg: PagedConfig, dt, k_pool, v_pool):
-    ps = _rows3(k_pool, cfg.pool_shape, dt, "k_pool")
-    assert v_pool.shape == cfg.pool_shape and v_pool.dtype is dt, f"v_pool must be {cfg.pool_shape}, {dt}"
-    assert k_pool.stride() == v_pool.stride(), "K and V pools share their strides"
-    return ps
+    dev, qs, ks, vs, os_ = q.get_device(), q.stride(), k.stride(), v.stride(), out.stride()
+    if not (q.shape == cfg.q_shape and out.shape == cfg.q_shape and k.shape == cfg.k_shape and v.shape == cfg.k_shape
+            and q.dtype is dt and out.dtype is dt and k.dtype is dt and v.dtype is dt
+            and qs[3] == 1 and os_[3] == 1 and ks[3] == 1 and vs[3] == 1
+            and dev >= 0 and k.get_device() == dev and v.get_device() == dev and out.get_device() == dev
+            and (ws is None or ws.get_device() == dev)
+            and (lse is None or lse.shape == cfg.lse_shape and lse.dtype is f32 and lse.stride(2) == 1
+                 and lse.get_device() == dev)
+            and (q_lens is None or q_lens.shape == cfg.len_shape and q_lens.dtype is i32
+                 and q_lens.is_contiguous() and q_lens.get_device() == dev)
+            and (kv_lens is None or kv_lens.shape == cfg.len_shape and kv_lens.dtype is i32
+                 and kv_lens.is_contiguous() and kv_lens.get_device() == dev)):
+        _refuse("kvec_prefill_attention", ("q", q, cfg.q_shape, dt, False), ("out", out, cfg.q_shape, dt, False),
+                ("k", k, cfg.k_shape, dt, False), ("v", v, cfg.k_shape, dt, False),
+                ("lse", lse, cfg.lse_shape, f32, False), ("q_lens", q_lens, cfg.len_shape, i32, True),
+                ("kv_lens", kv_lens, cfg.len_shape, i32, True))
+    ls = None
+    if lse is not None:
+        st = lse.stride()
+        ls = _I64x2(st[0], st[1])
+    _launch((_lib or load()).kvec_prefill_attention, dev, stream, (
+        cfg.ref, q.data_ptr(), _I64x3(qs[0], qs[1], qs[2]), k.data_ptr(), _I64x3(ks[0], ks[1], ks[2]),
+        v.data_ptr(), _I64x3(vs[0], vs[1], vs[2]), _ptr(q_lens), _ptr(kv_lens), out.data_ptr(),
+        _I64x3(os_[0], os_[1], os_[2]), _ptr(lse), ls, _ptr(ws), 0 if ws is None else ws.nbytes),
+        "kvec_prefill_attention")
 
 
 def kvec_paged_append(cfg: PagedConfig, q, k, v, positions, slots, q_out, k_pool, v_pool, q_weight=None,
@@ -545,22 +540,42 @@ def kvec_paged_append(cfg: PagedConfig, q, k, v, positions, slots, q_out, k_pool
     [n], slots int64 [n] (page * page_size + row; -1: not stored), pools
     [n_pages][H][page_size][d]; weights [d] (None: no norm); inv_freq float64 [rot_dim / 2]
     (None: no rotation); acc fp32 and pos int32 [n_pages][H][page_size]."""
-    import torch
     dt, f32, i32 = cfg.types
-    n, d = q.shape[0], cfg.head_dim
+    n, d, meta, f64, i64 = q.shape[0], cfg.head_dim, cfg.meta_shape, *cfg.long_types
     queries, keys = (n, cfg.n_q_heads, d), (n, cfg.n_kv_heads, d)
-    qs, os_ = _rows2(q, queries, dt, "q"), _rows2(q_out, queries, dt, "q_out")
-    ks, vs = _rows2(k, keys, dt, "k"), _rows2(v, keys, dt, "v")
-    ps = _pools(cfg, dt, k_pool, v_pool)
-    at, sl = _dense(positions, (n,), i32, "positions"), _dense(slots, (n,), torch.int64, "slots")
-    wq, wk = _dense(q_weight, (d,), dt, "q_weight"), _dense(k_weight, (d,), dt, "k_weight")
-    ac, po = _dense(acc, cfg.meta_shape, f32, "acc"), _dense(pos, cfg.meta_shape, i32, "pos")
+    dev, qs, ks, vs, os_, ps = k_pool.get_device(), q.stride(), k.stride(), v.stride(), q_out.stride(), k_pool.stride()
     half = 0 if inv_freq is None else inv_freq.shape[0]
-    fr = _dense(inv_freq, (half,), torch.float64, "inv_freq")
-    _call("kvec_paged_append", stream, (k_pool, q, k, v, positions, slots, q_out, v_pool, q_weight, k_weight,
-                                        inv_freq, acc, pos),
-          cfg.ref, n, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, wq, wk, eps, at, fr, 2 * half, sl,
-          q_out.data_ptr(), os_, k_pool.data_ptr(), v_pool.data_ptr(), ps, ac, po)
+    if not (q.shape == queries and q_out.shape == queries and k.shape == keys and v.shape == keys
+            and k_pool.shape == cfg.pool_shape and v_pool.shape == cfg.pool_shape and v_pool.stride() == ps
+            and q.dtype is dt and q_out.dtype is dt and k.dtype is dt and v.dtype is dt and k_pool.dtype is dt
+            and v_pool.dtype is dt and qs[2] == 1 and os_[2] == 1 and ks[2] == 1 and vs[2] == 1 and ps[3] == 1
+            and positions.shape == (n,) and positions.dtype is i32 and positions.is_contiguous()
+            and slots.shape == (n,) and slots.dtype is i64 and slots.is_contiguous()
+            and dev >= 0 and q.get_device() == dev and k.get_device() == dev and v.get_device() == dev
+            and q_out.get_device() == dev and v_pool.get_device() == dev and positions.get_device() == dev
+            and slots.get_device() == dev
+            and (q_weight is None or q_weight.shape == (d,) and q_weight.dtype is dt and q_weight.is_contiguous()
+                 and q_weight.get_device() == dev)
+            and (k_weight is None or k_weight.shape == (d,) and k_weight.dtype is dt and k_weight.is_contiguous()
+                 and k_weight.get_device() == dev)
+            and (inv_freq is None or inv_freq.dtype is f64 and inv_freq.is_contiguous() and inv_freq.dim() == 1
+                 and inv_freq.get_device() == dev)
+            and (acc is None or acc.shape == meta and acc.dtype is f32 and acc.is_contiguous()
+                 and acc.get_device() == dev)
+            and (pos is None or pos.shape == meta and pos.dtype is i32 and pos.is_contiguous()
+                 and pos.get_device() == dev)):
+        _refuse("kvec_paged_append", ("k_pool", k_pool, cfg.pool_shape, dt, False),
+                ("v_pool", v_pool, cfg.pool_shape, dt, False), ("q", q, queries, dt, False),
+                ("q_out", q_out, queries, dt, False), ("k", k, keys, dt, False), ("v", v, keys, dt, False),
+                ("positions", positions, (n,), i32, True), ("slots", slots, (n,), i64, True),
+                ("q_weight", q_weight, (d,), dt, True), ("k_weight", k_weight, (d,), dt, True),
+                ("inv_freq", inv_freq, (half,), f64, True), ("acc", acc, meta, f32, True),
+                ("pos", pos, meta, i32, True))
+    _launch((_lib or load()).kvec_paged_append, dev, stream, (
+        cfg.ref, n, q.data_ptr(), _I64x2(qs[0], qs[1]), k.data_ptr(), _I64x2(ks[0], ks[1]), v.data_ptr(),
+        _I64x2(vs[0], vs[1]), _ptr(q_weight), _ptr(k_weight), eps, positions.data_ptr(), _ptr(inv_freq), 2 * half,
+        slots.data_ptr(), q_out.data_ptr(), _I64x2(os_[0], os_[1]), k_pool.data_ptr(), v_pool.data_ptr(),
+        _I64x3(ps[0], ps[1], ps[2]), _ptr(acc), _ptr(pos)), "kvec_paged_append")
 
 
 def _max_len(cfg: PagedConfig, max_len) -> int:
@@ -581,14 +596,28 @@ def kvec_paged_decode(cfg: PagedConfig, q, k_pool, v_pool, page_table, lens, out
     page_table int32 [b][max_pages]; lens int32 [b]; out fp32 [b][HQ][d]; lse fp32
     [b][HQ]; acc fp32 [n_pages][H][page_size].  max_len None: every slot of the table."""
     dt, f32, i32 = cfg.types
-    qs, ps = _rows2(q, cfg.q_shape, dt, "q"), _pools(cfg, dt, k_pool, v_pool)
-    tb, ln = _dense(page_table, cfg.table_shape, i32, "page_table"), _dense(lens, cfg.len_shape, i32, "lens")
-    op, lp = _dense(out, cfg.q_shape, f32, "out"), _dense(lse, cfg.lse_shape, f32, "lse")
-    ac = _dense(acc, cfg.meta_shape, f32, "acc")
-    wp, wn = _ws(ws)
-    _call("kvec_paged_decode", stream, (q, k_pool, v_pool, page_table, lens, out, ws, lse, acc), cfg.ref,
-          q.data_ptr(), qs, k_pool.data_ptr(), v_pool.data_ptr(), ps, tb, ln, _max_len(cfg, max_len), window,
-          n_sinks, op, lp, ac, wp, wn)
+    dev, qs, ps = q.get_device(), q.stride(), k_pool.stride()
+    if not (q.shape == cfg.q_shape and out.shape == cfg.q_shape and k_pool.shape == cfg.pool_shape
+            and v_pool.shape == cfg.pool_shape and v_pool.stride() == ps and q.dtype is dt and k_pool.dtype is dt
+            and v_pool.dtype is dt and out.dtype is f32 and qs[2] == 1 and ps[3] == 1 and out.is_contiguous()
+            and page_table.shape == cfg.table_shape and page_table.dtype is i32 and page_table.is_contiguous()
+            and lens.shape == cfg.len_shape and lens.dtype is i32 and lens.is_contiguous()
+            and dev >= 0 and k_pool.get_device() == dev and v_pool.get_device() == dev and out.get_device() == dev
+            and page_table.get_device() == dev and lens.get_device() == dev
+            and (ws is None or ws.get_device() == dev)
+            and (lse is None or lse.shape == cfg.lse_shape and lse.dtype is f32 and lse.is_contiguous()
+                 and lse.get_device() == dev)
+            and (acc is None or acc.shape == cfg.meta_shape and acc.dtype is f32 and acc.is_contiguous()
+                 and acc.get_device() == dev)):
+        _refuse("kvec_paged_decode", ("q", q, cfg.q_shape, dt, False), ("k_pool", k_pool, cfg.pool_shape, dt, False),
+                ("v_pool", v_pool, cfg.pool_shape, dt, False), ("page_table", page_table, cfg.table_shape, i32, True),
+                ("lens", lens, cfg.len_shape, i32, True), ("out", out, cfg.q_shape, f32, True),
+                ("lse", lse, cfg.lse_shape, f32, True), ("acc", acc, cfg.meta_shape, f32, True))
+    _launch((_lib or load()).kvec_paged_decode, dev, stream, (
+        cfg.ref, q.data_ptr(), _I64x2(qs[0], qs[1]), k_pool.data_ptr(), v_pool.data_ptr(),
+        _I64x3(ps[0], ps[1], ps[2]), page_table.data_ptr(), lens.data_ptr(), _max_len(cfg, max_len), window,
+        n_sinks, out.data_ptr(), _ptr(lse), _ptr(acc), _ptr(ws), 0 if ws is None else ws.nbytes),
+        "kvec_paged_decode")
 
 
 def kvec_paged_evict_workspace_size(cfg: PagedConfig, max_len: int | None, budget: int) -> int:
@@ -604,12 +633,28 @@ def kvec_paged_evict(cfg: PagedConfig, budget: int, k_pool, v_pool, page_table, 
     [n_pages][H][page_size]; lens, n_seen, lens_out int32 [b] (lens_out may be lens);
     kept int32 [b][H][budget]."""
     dt, f32, i32 = cfg.types
-    ps = _pools(cfg, dt, k_pool, v_pool)
-    tb, ln = _dense(page_table, cfg.table_shape, i32, "page_table"), _dense(lens, cfg.len_shape, i32, "lens")
-    ns, lo = _dense(n_seen, cfg.len_shape, i32, "n_seen"), _dense(lens_out, cfg.len_shape, i32, "lens_out")
-    ac, po = _dense(acc, cfg.meta_shape, f32, "acc"), _dense(pos, cfg.meta_shape, i32, "pos")
-    kp = _dense(kept, (cfg.batch, cfg.n_kv_heads, budget), i32, "kept")
-    wp, wn = _ws(ws)
-    _call("kvec_paged_evict", stream, (k_pool, v_pool, page_table, lens, n_seen, acc, pos, lens_out, ws, kept),
-          cfg.ref, budget, window, n_sinks, k_pool.data_ptr(), v_pool.data_ptr(), ps, tb, ln, ns,
-          _max_len(cfg, max_len), ac, po, kp, lo, wp, wn)
+    dev, ps, meta, one, kept_shape = k_pool.get_device(), k_pool.stride(), cfg.meta_shape, cfg.len_shape, \
+        (cfg.batch, cfg.n_kv_heads, budget)
+    if not (k_pool.shape == cfg.pool_shape and v_pool.shape == cfg.pool_shape and v_pool.stride() == ps
+            and k_pool.dtype is dt and v_pool.dtype is dt and ps[3] == 1
+            and page_table.shape == cfg.table_shape and page_table.dtype is i32 and page_table.is_contiguous()
+            and lens.shape == one and lens.dtype is i32 and lens.is_contiguous()
+            and n_seen.shape == one and n_seen.dtype is i32 and n_seen.is_contiguous()
+            and lens_out.shape == one and lens_out.dtype is i32 and lens_out.is_contiguous()
+            and acc.shape == meta and acc.dtype is f32 and acc.is_contiguous()
+            and pos.shape == meta and pos.dtype is i32 and pos.is_contiguous()
+            and dev >= 0 and v_pool.get_device() == dev and page_table.get_device() == dev
+            and lens.get_device() == dev and n_seen.get_device() == dev and lens_out.get_device() == dev
+            and acc.get_device() == dev and pos.get_device() == dev and (ws is None or ws.get_device() == dev)
+            and (kept is None or kept.shape == kept_shape and kept.dtype is i32 and kept.is_contiguous()
+                 and kept.get_device() == dev)):
+        _refuse("kvec_paged_evict", ("k_pool", k_pool, cfg.pool_shape, dt, False),
+                ("v_pool", v_pool, cfg.pool_shape, dt, False), ("page_table", page_table, cfg.table_shape, i32, True),
+                ("lens", lens, one, i32, True), ("n_seen", n_seen, one, i32, True),
+                ("lens_out", lens_out, one, i32, True), ("acc", acc, meta, f32, True), ("pos", pos, meta, i32, True),
+                ("kept", kept, kept_shape, i32, True))
+    _launch((_lib or load()).kvec_paged_evict, dev, stream, (
+        cfg.ref, budget, window, n_sinks, k_pool.data_ptr(), v_pool.data_ptr(), _I64x3(ps[0], ps[1], ps[2]),
+        page_table.data_ptr(), lens.data_ptr(), n_seen.data_ptr(), _max_len(cfg, max_len), acc.data_ptr(),
+        pos.data_ptr(), _ptr(kept), lens_out.data_ptr(), _ptr(ws), 0 if ws is None else ws.nbytes),
+        "kvec_paged_evict")
