@@ -14,10 +14,12 @@
 namespace kvec {
 namespace {
 
+constexpr int kStateHead = 4;  // floats before the output in a partial state (16-byte pieces)
+
 struct PfArgs {
   PrefillArgs p;
   int S, tiles;
-  float* part;  // [b][HQ][q_len][S][D + 2] when S > 1
+  float* part;  // [b][HQ][q_len][S][D + 4] when S > 1: maximum, sum, (two unused,) output
   float sc;
 };
 
@@ -159,15 +161,14 @@ __global__ __launch_bounds__(kPfThreads) void pf_rows16(PfArgs a) {
   if (!live) return;
   const int64_t row = ((int64_t)b * p.HQ + j) * p.q_len + r;
   if (a.S > 1) {
-    float* pp = a.part + (row * a.S + split) * (D + 2);
+    float* pp = a.part + (row * a.S + split) * (D + kStateHead);
     if (c == 0) {
       pp[0] = col.m;
       pp[1] = col.l;
     }
 #pragma unroll
     for (int t = 0; t < D / 16; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) pp[2 + 16 * t + 4 * c + e] = col.o[t][e];
+      *reinterpret_cast<f32x4*>(pp + kStateHead + 16 * t + 4 * c) = col.o[t];
     return;
   }
   const float inv = col.m == -INFINITY ? 0.f : 1.f / col.l;
@@ -324,7 +325,7 @@ template <class TT, int D>
 __device__ __forceinline__ void store_column(const PfArgs& a, const Columns32<TT, D>& col, int b, int j, int r, int split) {
   const PrefillArgs& p = a.p;
   if (a.S > 1) {
-    float* pp = a.part + ((((int64_t)b * p.HQ + j) * p.q_len + r) * a.S + split) * (D + 2);
+    float* pp = a.part + ((((int64_t)b * p.HQ + j) * p.q_len + r) * a.S + split) * (D + kStateHead);
     if (col.hh == 0) {
       pp[0] = col.m;
       pp[1] = col.l;
@@ -332,7 +333,9 @@ __device__ __forceinline__ void store_column(const PfArgs& a, const Columns32<TT
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) pp[2 + col.dim(dt, e)] = col.o[dt][e];
+      for (int e = 0; e < 16; e += 4)
+        *reinterpret_cast<f32x4*>(pp + kStateHead + col.dim(dt, e)) =
+            f32x4{col.o[dt][e], col.o[dt][e + 1], col.o[dt][e + 2], col.o[dt][e + 3]};
     return;
   }
   const float inv = col.m == -INFINITY ? 0.f : 1.f / col.l;
@@ -573,9 +576,7 @@ __global__ __launch_bounds__(kPfFewThreads, 1) void pf_few(PfArgs a) { few<TT, D
 // Join the splits of the rows: grid (row groups, HQ, batch).  The 256 / D threads of an
 // element take a row each (ROWS; few splits), or share one row's splits.  A batch of
 // states is in flight at once (they come from other XCDs: one memory round trip).
-constexpr int kJoinBatch = 8;
-
-template <class T, int D, bool ROWS>
+template <class T, int D, bool ROWS, int BATCH>
 __global__ __launch_bounds__(256) void pf_join(PfArgs a) {
   constexpr int PARTS = 256 / D;
   __shared__ float st[ROWS ? 1 : PARTS][3][ROWS ? 1 : D];
@@ -584,19 +585,19 @@ __global__ __launch_bounds__(256) void pf_join(PfArgs a) {
   const int r = ROWS ? blockIdx.x * PARTS + part : blockIdx.x, j = blockIdx.y, b = blockIdx.z;
   const int nq = p.q_lens ? min(max(p.q_lens[b], 0), p.q_len) : p.q_len;
   if (r >= nq) return;
-  const float* pp = a.part + (((int64_t)b * p.HQ + j) * p.q_len + r) * a.S * (D + 2);
+  const float* pp = a.part + (((int64_t)b * p.HQ + j) * p.q_len + r) * a.S * (D + kStateHead);
   float m = -INFINITY, l = 0.f, o = 0.f;
-  for (int s0 = ROWS ? 0 : part * kJoinBatch; s0 < a.S; s0 += (ROWS ? 1 : PARTS) * kJoinBatch) {
-    float ms[kJoinBatch], ls[kJoinBatch], os[kJoinBatch];
+  for (int s0 = ROWS ? 0 : part * BATCH; s0 < a.S; s0 += (ROWS ? 1 : PARTS) * BATCH) {
+    float ms[BATCH], ls[BATCH], os[BATCH];
 #pragma unroll
-    for (int i = 0; i < kJoinBatch; ++i) {
-      const float* q = pp + (int64_t)min(s0 + i, a.S - 1) * (D + 2);
+    for (int i = 0; i < BATCH; ++i) {
+      const float* q = pp + (int64_t)min(s0 + i, a.S - 1) * (D + kStateHead);
       ms[i] = s0 + i < a.S ? q[0] : -INFINITY;
       ls[i] = q[1];
-      os[i] = q[2 + e];
+      os[i] = q[kStateHead + e];
     }
 #pragma unroll
-    for (int i = 0; i < kJoinBatch; ++i) state_merge(m, l, o, ms[i], ls[i], os[i]);
+    for (int i = 0; i < BATCH; ++i) state_merge(m, l, o, ms[i], ls[i], os[i]);
   }
   if constexpr (!ROWS) {
     st[part][0][e] = m;
@@ -616,10 +617,11 @@ __global__ __launch_bounds__(256) void pf_join(PfArgs a) {
 template <class T, int D>
 void launch_join(const PfArgs& a, hipStream_t s) {
   const PrefillArgs& p = a.p;
-  if (a.S <= kJoinBatch)
-    hipLaunchKernelGGL((pf_join<T, D, true>), dim3((p.q_len + 256 / D - 1) / (256 / D), p.HQ, p.batch), dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL((pf_join<T, D, false>), dim3(p.q_len, p.HQ, p.batch), dim3(256), 0, s, a);
+  const dim3 rows((p.q_len + 256 / D - 1) / (256 / D), p.HQ, p.batch), one(p.q_len, p.HQ, p.batch);
+  if (a.S <= 2) hipLaunchKernelGGL((pf_join<T, D, true, 2>), rows, dim3(256), 0, s, a);
+  else if (a.S <= 4) hipLaunchKernelGGL((pf_join<T, D, true, 4>), rows, dim3(256), 0, s, a);
+  else if (a.S <= 8) hipLaunchKernelGGL((pf_join<T, D, true, 8>), rows, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((pf_join<T, D, false, 8>), one, dim3(256), 0, s, a);
 }
 
 enum PfKernel { kRows16, kRows32, kFew };
@@ -635,12 +637,13 @@ struct PfPlan {
 //       key tiles of all / work-groups at a time * us a tile,
 //       K and V at 4.5 TB/s) + what the join costs.
 // A tile of pf_rows32 (256 rows, 64 keys, one work-group per compute unit) takes
-// 1.95 us, of pf_few (32 rows, two waves with 32 keys each, two work-groups) 1.3, of
-// pf_rows16 (64 rows, 32 keys, two) 2.6; the join a launch (4 us), a round
-// trip per 16 splits and the partial states there and back at 4 TB/s.  us measured, pf_few / pf_rows32 unsplit or split /
-// estimates, Llama heads: 250 rows 10 / 16 / 9 and 8, 1000 rows 31 / 44 (two splits)
-// / 21 and 31 (unsplit), the Qwen heads' 2000 rows 78 / 62 / 69 and 62, 100 rows over
-// 5000 keys 32 (four splits) / 29 (16) / 31 and 27.
+// 1.95 us (1.15 at d 64), of pf_few (32 rows, two waves with 32 keys each, two
+// work-groups) 1.3 (0.9), of pf_rows16 (64 rows, 32 keys, two) 2.6; the join a launch
+// (4 us), a round trip per 16 splits and the partial states there and back at 4 TB/s.
+// us measured, pf_few / pf_rows32 (its splits): 250 rows of 32 heads 10.5 / 16 (1), 500
+// rows of 28 heads 16 / 26 (3), 1000 rows of 32 heads 33 / 44 (2), 2000 of 28 heads
+// 78 / 62 (1), 100 rows over 5000 keys 32 / 29 (16); d 64, 4000 rows of 16 heads 75
+// in one piece, 69 in two.
 PfPlan pf_plan(const PrefillArgs& a) {
   const int64_t packed = (int64_t)a.q_len * a.G, heads = (int64_t)a.batch * a.H;
   PfPlan best = {};
@@ -652,7 +655,7 @@ PfPlan pf_plan(const PrefillArgs& a) {
     const double span = (double)a.window + a.sinks + (double)rows / a.G;
     if (a.window > 0 && span < most) most = span;
     if (mean > most) mean = most;
-    const double state = 2.0 * a.batch * a.HQ * a.q_len * (a.D + 2) * 4 / 4e6;  // us per split
+    const double state = 2.0 * a.batch * a.HQ * a.q_len * (a.D + kStateHead) * 4 / 4e6;  // us per split
     const double all = groups * (mean / keys) / at_a_time * us;
     const double read = heads * most * 2 * a.D * a.esize / 4.5e6;
     const double floor = all > read ? all : read;
@@ -671,10 +674,10 @@ PfPlan pf_plan(const PrefillArgs& a) {
   if (a.esize == 4) {
     consider(kRows16, kPfRows, kPfKeys, 512, 2.6);
   } else {
-    consider(kRows32, kPf32Rows, kPf32Keys, 256, 1.95);
-    consider(kFew, kPfFewRows, 2 * kPfFewKeys, 512, 1.3);
+    consider(kRows32, kPf32Rows, kPf32Keys, 256, a.D == 64 ? 1.15 : 1.95);
+    consider(kFew, kPfFewRows, 2 * kPfFewKeys, 512, a.D == 64 ? 0.9 : 1.3);
   }
-  best.bytes = best.S > 1 ? (size_t)a.batch * a.HQ * a.q_len * best.S * (a.D + 2) * 4 : 0;
+  best.bytes = best.S > 1 ? (size_t)a.batch * a.HQ * a.q_len * best.S * (a.D + kStateHead) * 4 : 0;
   return best;
 }
 
