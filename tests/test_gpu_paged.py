@@ -197,6 +197,57 @@ def test_decode_far_offsets(gpu_lib):
         assert acc[p].equal(small.acc[small.table[0, j].item()])
 
 
+def test_append_and_evict_far_offsets(gpu_lib):
+    """The same rows in the last pages of a pool of 4.4 GB and in a small one."""
+    import torch
+    kv, H, page, d, n_pages = gpu_lib, 2, 1024, 128, 8300
+    small = Cache(kv, [2000], H, 2, d, page, "bf16", seed=41)
+    where = [n_pages - 1, n_pages - 7]
+    big = {}
+    for name, like in (("k", small.k), ("v", small.v), ("acc", small.acc), ("pos", small.pos)):
+        big[name] = torch.empty((n_pages, *like.shape[1:]), dtype=like.dtype, device="cuda")
+        for j, p in enumerate(where):
+            big[name][p] = like[small.table[0, j]].cuda()
+    small.cuda()
+    cfg = kv.PagedConfig(1, H, 2 * H, d, page, n_pages, 2)
+    table, lens = torch.tensor([where], dtype=torch.int32, device="cuda"), small.lens
+    q, k, v = (small.rand(9, h, d).bfloat16().cuda() for h in (2 * H, H, H))
+    fr = torch.rand(d // 2, dtype=torch.float64, device="cuda")
+    at = torch.arange(1500, 1509)
+    pos = at.int().cuda()
+    outs = []
+    for c, tb, t in ((cfg, table, big), (small.cfg, small.table, dict(k=small.k, v=small.v, acc=small.acc, pos=small.pos))):
+        slots = (tb[0].long()[(at // page).cuda()] * page + (at % page).cuda())
+        q_out = torch.empty_like(q)
+        kv.kvec_paged_append(c, q, k, v, pos, slots, q_out, t["k"], t["v"], inv_freq=fr, acc=t["acc"], pos=t["pos"])
+        ws = torch.empty(kv.kvec_paged_evict_workspace_size(c, None, 900), dtype=torch.uint8, device="cuda")
+        kept, out = torch.empty((1, H, 900), dtype=torch.int32, device="cuda"), torch.empty(1, dtype=torch.int32, device="cuda")
+        kv.kvec_paged_evict(c, 900, t["k"], t["v"], tb, lens, lens, t["acc"], t["pos"], out, ws, window=50, n_sinks=4, kept=kept)
+        outs.append((q_out, kept, out, *(t[n][tb[0].long()].nan_to_num(9) for n in ("k", "v", "acc")), t["pos"][tb[0].long()]))
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)
+
+
+def test_two_streams_at_once(gpu_lib):
+    """Calls on two streams, each with a workspace of its own, over one pool."""
+    import torch
+    c = Cache(gpu_lib, [3000, 2500, 100], 4, 4, 128, 64, "bf16", seed=42).cuda()
+    qs = [c.rand(3, 16, 128).bfloat16().cuda() for _ in range(2)]
+    wants = [_decode(c, q, acc=False) for q in qs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    size = gpu_lib.kvec_paged_decode_workspace_size(c.cfg)
+    ws = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    outs = [[torch.empty(3, 16, 128, device="cuda") for _ in range(20)] for _ in range(2)]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for j, s in enumerate(streams):
+            gpu_lib.kvec_paged_decode(c.cfg, qs[j], c.k, c.v, c.table, c.lens, outs[j][i], ws[j], stream=s)
+    torch.cuda.synchronize()
+    for j in range(2):
+        assert all(o.equal(wants[j][0]) for o in outs[j])
+
+
 APPEND = [  # tokens, H, G, d, page, dtype, rot, norm, start
     (1, 8, 4, 128, 64, "bf16", 128, True, 130000),
     (5, 4, 7, 128, 16, "bf16", 64, False, 7),

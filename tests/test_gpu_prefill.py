@@ -157,6 +157,31 @@ def test_prefill_strides_of_outputs_and_shared_keys(gpu_lib):
     assert torch.all(big_lse[:, 0] == 77) and torch.all(big_lse[:, 5] == 77) and torch.all(big_lse[:, :, :3] == 77) and torch.all(big_lse[:, :, 73:] == 77)
 
 
+def test_prefill_far_offsets(gpu_lib):
+    """Sequences 2^31 elements and more apart, and keys that span almost 2 GiB."""
+    import torch
+    kv, gap = gpu_lib, (1 << 31) + 4096
+    q, k, v = _tensors(2, 1, 2, 64, 300, 300, "bf16", seed=12)
+    out, lse = _run(kv, q, k, v)
+    buf = torch.empty(gap + 300 * 64 * 2, dtype=torch.bfloat16, device="cuda")
+    for x in (q, k, v):
+        y = buf.as_strided(x.shape, (gap, x.stride(1), 64, 1))
+        y.copy_(x)
+        o2 = torch.empty_like(out)
+        kv.kvec_prefill_attention(kv.AttentionConfig(2, 1, 2, 64, 300, 300), *(y if x is t else t for t in (q, k, v)), o2)
+        assert o2.equal(out)
+    y = buf.as_strided(out.shape, (gap, out.stride(1), 64, 1))
+    y.fill_(0)
+    kv.kvec_prefill_attention(kv.AttentionConfig(2, 1, 2, 64, 300, 300), q, k, v, y)
+    assert torch.equal(y, out)
+    row = ((1 << 30) - 1) // 300 // 8 * 8  # 300 rows of this stride: just below 2 GiB
+    wide = buf.as_strided((1, 1, 300, 64), (0, 0, row, 1))
+    wide.copy_(k[:1])
+    o2 = torch.empty_like(out[:1])
+    kv.kvec_prefill_attention(kv.AttentionConfig(1, 1, 2, 64, 300, 300), q[:1], wide, v[:1], o2)
+    assert o2.equal(out[:1])
+
+
 def test_prefill_graph_and_stream(gpu_lib):
     """Two captured calls that share a workspace, replayed with eager work between."""
     import torch
