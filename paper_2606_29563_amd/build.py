@@ -1,4 +1,4 @@
-"""Build libkvec.so (HIP, gfx950) in-tree with hipcc."""
+"""Build libkvec.so (HIP, gfx950) in-tree with hipcc, and the binding's marshalling module."""
 from __future__ import annotations
 
 import concurrent.futures as cf
@@ -11,6 +11,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libkvec.so")
+BIND = os.path.join(HERE, "_kvec_bind.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 
 # (source, object name, extra flags): the step kernel is instantiated once per
@@ -43,11 +44,35 @@ def _compile(item) -> str:
     return obj
 
 
+def build_binding() -> str:
+    """The compiled marshalling module of the Python binding (host code, against torch's headers)."""
+    import sysconfig
+
+    import torch
+    base = os.path.dirname(torch.__file__)
+    tmp = BIND + ".tmp"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE,
+           "-isystem", os.path.join(base, "include"),
+           "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
+           "-isystem", os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include"),
+           "-isystem", sysconfig.get_paths()["include"],
+           os.path.join(CSRC, "kvec_bind.cpp"), "-o", tmp,
+           "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{cmd[0]} failed for kvec_bind.cpp:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, BIND)
+    return BIND
+
+
 def build(verbose: bool = True) -> str:
     os.makedirs(BUILD_DIR, exist_ok=True)
     workers = max(1, min(len(SOURCES), int(os.environ.get("MAX_JOBS", os.cpu_count() or 1))))
     with cf.ThreadPoolExecutor(max_workers=workers) as ex:
+        binding = ex.submit(build_binding)
         objs = list(ex.map(_compile, SOURCES))
+        binding.result()
     tmp = LIB + ".tmp"
     r = subprocess.run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", tmp],
                        capture_output=True, text=True)

@@ -12,6 +12,7 @@ from dataclasses import dataclass, fields
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libkvec.so")
+BIND_PATH = os.path.join(HERE, "_kvec_bind.so")
 
 KVEC_OK, KVEC_ERR_INVALID, KVEC_ERR_UNSUPPORTED, KVEC_ERR_WORKSPACE, KVEC_ERR_DEVICE = range(5)
 KVEC_BF16, KVEC_F32 = 0, 1
@@ -153,12 +154,11 @@ def _rebuild(cfg):
 
 
 def _fix(cfg, c, **more) -> None:
-    """Keeps the C view of a frozen configuration, a reference to it, the types (of elements, float32,
-    int32) and the shapes it implies."""
+    """Keeps the C view of a frozen configuration, a reference to it and its address, the types (of
+    elements, float32, int32) and the shapes it implies."""
     import torch
     types = (torch.bfloat16 if cfg.dtype == KVEC_BF16 else torch.float32, torch.float32, torch.int32)
-    more["long_types"] = (torch.float64, torch.int64)
-    for name, value in dict(_c=c, ref=ctypes.byref(c), types=types, **more).items():
+    for name, value in dict(_c=c, ref=ctypes.byref(c), addr=ctypes.addressof(c), types=types, **more).items():
         object.__setattr__(cfg, name, value)
 
 
@@ -460,15 +460,52 @@ def kvec_decode_attention_noalloc(cfg: Config, q, k_cache, v_cache, out, idx=Non
            "kvec_decode_attention_noalloc")
 
 
-# The calls below are made once per layer and token, where the launch is as short as
-# the marshalling: each checks its tensors in one expression, and only a failure goes
-# through them again for the message.
+# The calls below are made once per layer and token, where a launch is shorter than the
+# reading of a dozen tensors' attributes: the compiled module _kvec_bind checks and
+# marshals them, and only where it finds something wrong Python goes through them again,
+# for the message.
 
-_I64x2, _I64x3 = ctypes.c_int64 * 2, ctypes.c_int64 * 3
+_bind = None
 
 
-def _refuse(name: str, *tensors) -> None:
-    """Raises for the first of (what, tensor, shape, dtype, contiguous) that is not what it says."""
+def _bound():
+    """The compiled marshalling module, with the library's entry points."""
+    global _bind
+    if _bind is None:
+        import torch  # noqa: F401  (its libraries, before the module that needs them)
+        lib = load()
+        if not os.path.exists(BIND_PATH):
+            from . import build as _build
+            _build.build_binding()
+        from . import _kvec_bind
+        _kvec_bind.bind(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in (
+            "kvec_prefill_attention", "kvec_paged_append", "kvec_paged_decode", "kvec_paged_evict")))
+        _bind = _kvec_bind
+    return _bind
+
+
+def _serve(name: str, cfg, dev: int, stream, args, tensors) -> None:
+    """_kvec_bind's call `name` with device `dev` current, on its current stream unless one
+    is given.  tensors(): (what, tensor, shape, dtype, contiguous) of the arguments."""
+    import torch
+    status = -1
+    if dev >= 0:
+        fn = getattr(_bind or _bound(), name[5:])
+        # the current stream's handle, without a Stream object around it
+        st = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+        if dev == torch._C._cuda_getDevice():
+            status = fn(cfg.addr, dev, st, *args)
+        else:
+            with torch.cuda.device(dev):
+                status = fn(cfg.addr, dev, st, *args)
+    if status > 0:
+        raise KvecError(status, name)
+    if status < 0:
+        _refuse(name, tensors())
+
+
+def _refuse(name: str, tensors) -> None:
+    """Raises for the first tensor that is not what its entry says."""
     first = tensors[0][1]
     for what, t, shape, dtype, dense in tensors:
         if t is None:
@@ -478,21 +515,7 @@ def _refuse(name: str, *tensors) -> None:
         assert t.is_contiguous() if dense else t.stride(-1) == 1, \
             f"{name}: {what} must be contiguous" + ("" if dense else " in its last dimension")
         assert t.is_cuda and t.device == first.device, f"{name}: {what} must be on the GPU of the other tensors"
-    raise AssertionError(f"{name}: K and V pools must have the same strides, and a workspace be on their GPU")
-
-
-def _launch(fn, dev: int, stream, args, name: str) -> None:
-    """fn(*args, stream handle) with device `dev` current, on its current stream unless one is given."""
-    import torch
-    # the current stream's handle, without a Stream object around it
-    st = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
-    if dev == torch._C._cuda_getDevice():
-        status = fn(*args, st)
-    else:
-        with torch.cuda.device(dev):
-            status = fn(*args, st)
-    if status:
-        _check(status, name)
+    raise AssertionError(f"{name}: K and V pools must have the same strides, and a workspace be contiguous on their GPU")
 
 
 def kvec_prefill_workspace_size(cfg: AttentionConfig) -> int:
@@ -507,31 +530,10 @@ def kvec_prefill_attention(cfg: AttentionConfig, q, k, v, out, ws=None, lse=None
     [b][HQ][q_len], rows contiguous; q_lens, kv_lens int32 [b].  ws may be None when
     kvec_prefill_workspace_size(cfg) is 0."""
     dt, f32, i32 = cfg.types
-    dev, qs, ks, vs, os_ = q.get_device(), q.stride(), k.stride(), v.stride(), out.stride()
-    if not (q.shape == cfg.q_shape and out.shape == cfg.q_shape and k.shape == cfg.k_shape and v.shape == cfg.k_shape
-            and q.dtype is dt and out.dtype is dt and k.dtype is dt and v.dtype is dt
-            and qs[3] == 1 and os_[3] == 1 and ks[3] == 1 and vs[3] == 1
-            and dev >= 0 and k.get_device() == dev and v.get_device() == dev and out.get_device() == dev
-            and (ws is None or ws.get_device() == dev)
-            and (lse is None or lse.shape == cfg.lse_shape and lse.dtype is f32 and lse.stride(2) == 1
-                 and lse.get_device() == dev)
-            and (q_lens is None or q_lens.shape == cfg.len_shape and q_lens.dtype is i32
-                 and q_lens.is_contiguous() and q_lens.get_device() == dev)
-            and (kv_lens is None or kv_lens.shape == cfg.len_shape and kv_lens.dtype is i32
-                 and kv_lens.is_contiguous() and kv_lens.get_device() == dev)):
-        _refuse("kvec_prefill_attention", ("q", q, cfg.q_shape, dt, False), ("out", out, cfg.q_shape, dt, False),
-                ("k", k, cfg.k_shape, dt, False), ("v", v, cfg.k_shape, dt, False),
-                ("lse", lse, cfg.lse_shape, f32, False), ("q_lens", q_lens, cfg.len_shape, i32, True),
-                ("kv_lens", kv_lens, cfg.len_shape, i32, True))
-    ls = None
-    if lse is not None:
-        st = lse.stride()
-        ls = _I64x2(st[0], st[1])
-    _launch((_lib or load()).kvec_prefill_attention, dev, stream, (
-        cfg.ref, q.data_ptr(), _I64x3(qs[0], qs[1], qs[2]), k.data_ptr(), _I64x3(ks[0], ks[1], ks[2]),
-        v.data_ptr(), _I64x3(vs[0], vs[1], vs[2]), _ptr(q_lens), _ptr(kv_lens), out.data_ptr(),
-        _I64x3(os_[0], os_[1], os_[2]), _ptr(lse), ls, _ptr(ws), 0 if ws is None else ws.nbytes),
-        "kvec_prefill_attention")
+    _serve("kvec_prefill_attention", cfg, q.get_device(), stream, (q, k, v, out, ws, lse, q_lens, kv_lens), lambda: (
+        ("q", q, cfg.q_shape, dt, False), ("k", k, cfg.k_shape, dt, False), ("v", v, cfg.k_shape, dt, False),
+        ("out", out, cfg.q_shape, dt, False), ("lse", lse, cfg.lse_shape, f32, False),
+        ("q_lens", q_lens, cfg.len_shape, i32, True), ("kv_lens", kv_lens, cfg.len_shape, i32, True)))
 
 
 def kvec_paged_append(cfg: PagedConfig, q, k, v, positions, slots, q_out, k_pool, v_pool, q_weight=None,
@@ -540,42 +542,19 @@ def kvec_paged_append(cfg: PagedConfig, q, k, v, positions, slots, q_out, k_pool
     [n], slots int64 [n] (page * page_size + row; -1: not stored), pools
     [n_pages][H][page_size][d]; weights [d] (None: no norm); inv_freq float64 [rot_dim / 2]
     (None: no rotation); acc fp32 and pos int32 [n_pages][H][page_size]."""
-    dt, f32, i32 = cfg.types
-    n, d, meta, f64, i64 = q.shape[0], cfg.head_dim, cfg.meta_shape, *cfg.long_types
-    queries, keys = (n, cfg.n_q_heads, d), (n, cfg.n_kv_heads, d)
-    dev, qs, ks, vs, os_, ps = k_pool.get_device(), q.stride(), k.stride(), v.stride(), q_out.stride(), k_pool.stride()
-    half = 0 if inv_freq is None else inv_freq.shape[0]
-    if not (q.shape == queries and q_out.shape == queries and k.shape == keys and v.shape == keys
-            and k_pool.shape == cfg.pool_shape and v_pool.shape == cfg.pool_shape and v_pool.stride() == ps
-            and q.dtype is dt and q_out.dtype is dt and k.dtype is dt and v.dtype is dt and k_pool.dtype is dt
-            and v_pool.dtype is dt and qs[2] == 1 and os_[2] == 1 and ks[2] == 1 and vs[2] == 1 and ps[3] == 1
-            and positions.shape == (n,) and positions.dtype is i32 and positions.is_contiguous()
-            and slots.shape == (n,) and slots.dtype is i64 and slots.is_contiguous()
-            and dev >= 0 and q.get_device() == dev and k.get_device() == dev and v.get_device() == dev
-            and q_out.get_device() == dev and v_pool.get_device() == dev and positions.get_device() == dev
-            and slots.get_device() == dev
-            and (q_weight is None or q_weight.shape == (d,) and q_weight.dtype is dt and q_weight.is_contiguous()
-                 and q_weight.get_device() == dev)
-            and (k_weight is None or k_weight.shape == (d,) and k_weight.dtype is dt and k_weight.is_contiguous()
-                 and k_weight.get_device() == dev)
-            and (inv_freq is None or inv_freq.dtype is f64 and inv_freq.is_contiguous() and inv_freq.dim() == 1
-                 and inv_freq.get_device() == dev)
-            and (acc is None or acc.shape == meta and acc.dtype is f32 and acc.is_contiguous()
-                 and acc.get_device() == dev)
-            and (pos is None or pos.shape == meta and pos.dtype is i32 and pos.is_contiguous()
-                 and pos.get_device() == dev)):
-        _refuse("kvec_paged_append", ("k_pool", k_pool, cfg.pool_shape, dt, False),
-                ("v_pool", v_pool, cfg.pool_shape, dt, False), ("q", q, queries, dt, False),
-                ("q_out", q_out, queries, dt, False), ("k", k, keys, dt, False), ("v", v, keys, dt, False),
-                ("positions", positions, (n,), i32, True), ("slots", slots, (n,), i64, True),
+    def tensors():
+        import torch
+        (dt, f32, i32), n, d = cfg.types, q.shape[0], cfg.head_dim
+        half = 0 if inv_freq is None else inv_freq.shape[0]
+        return (("k_pool", k_pool, cfg.pool_shape, dt, False), ("v_pool", v_pool, cfg.pool_shape, dt, False),
+                ("q", q, (n, cfg.n_q_heads, d), dt, False), ("k", k, (n, cfg.n_kv_heads, d), dt, False),
+                ("v", v, (n, cfg.n_kv_heads, d), dt, False), ("q_out", q_out, (n, cfg.n_q_heads, d), dt, False),
+                ("positions", positions, (n,), i32, True), ("slots", slots, (n,), torch.int64, True),
                 ("q_weight", q_weight, (d,), dt, True), ("k_weight", k_weight, (d,), dt, True),
-                ("inv_freq", inv_freq, (half,), f64, True), ("acc", acc, meta, f32, True),
-                ("pos", pos, meta, i32, True))
-    _launch((_lib or load()).kvec_paged_append, dev, stream, (
-        cfg.ref, n, q.data_ptr(), _I64x2(qs[0], qs[1]), k.data_ptr(), _I64x2(ks[0], ks[1]), v.data_ptr(),
-        _I64x2(vs[0], vs[1]), _ptr(q_weight), _ptr(k_weight), eps, positions.data_ptr(), _ptr(inv_freq), 2 * half,
-        slots.data_ptr(), q_out.data_ptr(), _I64x2(os_[0], os_[1]), k_pool.data_ptr(), v_pool.data_ptr(),
-        _I64x3(ps[0], ps[1], ps[2]), _ptr(acc), _ptr(pos)), "kvec_paged_append")
+                ("inv_freq", inv_freq, (half,), torch.float64, True), ("acc", acc, cfg.meta_shape, f32, True),
+                ("pos", pos, cfg.meta_shape, i32, True))
+    _serve("kvec_paged_append", cfg, k_pool.get_device(), stream, (
+        q, k, v, positions, slots, q_out, k_pool, v_pool, q_weight, k_weight, eps, inv_freq, acc, pos), tensors)
 
 
 def _max_len(cfg: PagedConfig, max_len) -> int:
@@ -596,28 +575,13 @@ def kvec_paged_decode(cfg: PagedConfig, q, k_pool, v_pool, page_table, lens, out
     page_table int32 [b][max_pages]; lens int32 [b]; out fp32 [b][HQ][d]; lse fp32
     [b][HQ]; acc fp32 [n_pages][H][page_size].  max_len None: every slot of the table."""
     dt, f32, i32 = cfg.types
-    dev, qs, ps = q.get_device(), q.stride(), k_pool.stride()
-    if not (q.shape == cfg.q_shape and out.shape == cfg.q_shape and k_pool.shape == cfg.pool_shape
-            and v_pool.shape == cfg.pool_shape and v_pool.stride() == ps and q.dtype is dt and k_pool.dtype is dt
-            and v_pool.dtype is dt and out.dtype is f32 and qs[2] == 1 and ps[3] == 1 and out.is_contiguous()
-            and page_table.shape == cfg.table_shape and page_table.dtype is i32 and page_table.is_contiguous()
-            and lens.shape == cfg.len_shape and lens.dtype is i32 and lens.is_contiguous()
-            and dev >= 0 and k_pool.get_device() == dev and v_pool.get_device() == dev and out.get_device() == dev
-            and page_table.get_device() == dev and lens.get_device() == dev
-            and (ws is None or ws.get_device() == dev)
-            and (lse is None or lse.shape == cfg.lse_shape and lse.dtype is f32 and lse.is_contiguous()
-                 and lse.get_device() == dev)
-            and (acc is None or acc.shape == cfg.meta_shape and acc.dtype is f32 and acc.is_contiguous()
-                 and acc.get_device() == dev)):
-        _refuse("kvec_paged_decode", ("q", q, cfg.q_shape, dt, False), ("k_pool", k_pool, cfg.pool_shape, dt, False),
-                ("v_pool", v_pool, cfg.pool_shape, dt, False), ("page_table", page_table, cfg.table_shape, i32, True),
-                ("lens", lens, cfg.len_shape, i32, True), ("out", out, cfg.q_shape, f32, True),
-                ("lse", lse, cfg.lse_shape, f32, True), ("acc", acc, cfg.meta_shape, f32, True))
-    _launch((_lib or load()).kvec_paged_decode, dev, stream, (
-        cfg.ref, q.data_ptr(), _I64x2(qs[0], qs[1]), k_pool.data_ptr(), v_pool.data_ptr(),
-        _I64x3(ps[0], ps[1], ps[2]), page_table.data_ptr(), lens.data_ptr(), _max_len(cfg, max_len), window,
-        n_sinks, out.data_ptr(), _ptr(lse), _ptr(acc), _ptr(ws), 0 if ws is None else ws.nbytes),
-        "kvec_paged_decode")
+    n = cfg.max_pages * cfg.page_size if max_len is None else max_len
+    _serve("kvec_paged_decode", cfg, q.get_device(), stream, (
+        q, k_pool, v_pool, page_table, lens, out, ws, n, window, n_sinks, lse, acc), lambda: (
+        ("q", q, cfg.q_shape, dt, False), ("k_pool", k_pool, cfg.pool_shape, dt, False),
+        ("v_pool", v_pool, cfg.pool_shape, dt, False), ("page_table", page_table, cfg.table_shape, i32, True),
+        ("lens", lens, cfg.len_shape, i32, True), ("out", out, cfg.q_shape, f32, True),
+        ("lse", lse, cfg.lse_shape, f32, True), ("acc", acc, cfg.meta_shape, f32, True)))
 
 
 def kvec_paged_evict_workspace_size(cfg: PagedConfig, max_len: int | None, budget: int) -> int:
@@ -633,28 +597,11 @@ def kvec_paged_evict(cfg: PagedConfig, budget: int, k_pool, v_pool, page_table, 
     [n_pages][H][page_size]; lens, n_seen, lens_out int32 [b] (lens_out may be lens);
     kept int32 [b][H][budget]."""
     dt, f32, i32 = cfg.types
-    dev, ps, meta, one, kept_shape = k_pool.get_device(), k_pool.stride(), cfg.meta_shape, cfg.len_shape, \
-        (cfg.batch, cfg.n_kv_heads, budget)
-    if not (k_pool.shape == cfg.pool_shape and v_pool.shape == cfg.pool_shape and v_pool.stride() == ps
-            and k_pool.dtype is dt and v_pool.dtype is dt and ps[3] == 1
-            and page_table.shape == cfg.table_shape and page_table.dtype is i32 and page_table.is_contiguous()
-            and lens.shape == one and lens.dtype is i32 and lens.is_contiguous()
-            and n_seen.shape == one and n_seen.dtype is i32 and n_seen.is_contiguous()
-            and lens_out.shape == one and lens_out.dtype is i32 and lens_out.is_contiguous()
-            and acc.shape == meta and acc.dtype is f32 and acc.is_contiguous()
-            and pos.shape == meta and pos.dtype is i32 and pos.is_contiguous()
-            and dev >= 0 and v_pool.get_device() == dev and page_table.get_device() == dev
-            and lens.get_device() == dev and n_seen.get_device() == dev and lens_out.get_device() == dev
-            and acc.get_device() == dev and pos.get_device() == dev and (ws is None or ws.get_device() == dev)
-            and (kept is None or kept.shape == kept_shape and kept.dtype is i32 and kept.is_contiguous()
-                 and kept.get_device() == dev)):
-        _refuse("kvec_paged_evict", ("k_pool", k_pool, cfg.pool_shape, dt, False),
-                ("v_pool", v_pool, cfg.pool_shape, dt, False), ("page_table", page_table, cfg.table_shape, i32, True),
-                ("lens", lens, one, i32, True), ("n_seen", n_seen, one, i32, True),
-                ("lens_out", lens_out, one, i32, True), ("acc", acc, meta, f32, True), ("pos", pos, meta, i32, True),
-                ("kept", kept, kept_shape, i32, True))
-    _launch((_lib or load()).kvec_paged_evict, dev, stream, (
-        cfg.ref, budget, window, n_sinks, k_pool.data_ptr(), v_pool.data_ptr(), _I64x3(ps[0], ps[1], ps[2]),
-        page_table.data_ptr(), lens.data_ptr(), n_seen.data_ptr(), _max_len(cfg, max_len), acc.data_ptr(),
-        pos.data_ptr(), _ptr(kept), lens_out.data_ptr(), _ptr(ws), 0 if ws is None else ws.nbytes),
-        "kvec_paged_evict")
+    n = cfg.max_pages * cfg.page_size if max_len is None else max_len
+    _serve("kvec_paged_evict", cfg, k_pool.get_device(), stream, (
+        budget, k_pool, v_pool, page_table, lens, n_seen, acc, pos, lens_out, ws, window, n_sinks, kept, n), lambda: (
+        ("k_pool", k_pool, cfg.pool_shape, dt, False), ("v_pool", v_pool, cfg.pool_shape, dt, False),
+        ("page_table", page_table, cfg.table_shape, i32, True), ("lens", lens, cfg.len_shape, i32, True),
+        ("n_seen", n_seen, cfg.len_shape, i32, True), ("lens_out", lens_out, cfg.len_shape, i32, True),
+        ("acc", acc, cfg.meta_shape, f32, True), ("pos", pos, cfg.meta_shape, i32, True),
+        ("kept", kept, (cfg.batch, cfg.n_kv_heads, budget), i32, True)))
