@@ -355,9 +355,9 @@ __device__ __forceinline__ void store_column(const PfArgs& a, const Columns32<TT
         col.m == -INFINITY ? -INFINITY : (col.m + log2f(col.l)) * 0.69314718055994531f;
 }
 
-// Many rows: a work-group of eight waves takes 256 packed rows, 32 a wave.  Tiles of
-// 64 keys are copied into one of two LDS buffers while the other is used; one
-// barrier per tile.
+// Many rows: a work-group of eight or four waves (pf_plan chooses) takes 256 or 128
+// packed rows, 32 a wave.  Tiles of 64 keys are copied into one of two LDS buffers
+// while the other is used; one barrier per tile.
 //
 // Bound by the matrix cores and the vector work of the softmax, which mostly add
 // up (the counters see them together in 28% of the matrix cores' busy cycles).
@@ -369,13 +369,14 @@ __device__ __forceinline__ void store_column(const PfArgs& a, const Columns32<TT
 // dropped: three LDS buffers (540 for 535), the next tile's logits computed beside this
 // tile's exponentials (561 for 549), waves 4-7 half a tile behind waves 0-3, in
 // step by barriers (607), raised wave priority around the products (549 for 545).
-constexpr int kPf32Threads = 512, kPf32Rows = 256, kPf32Keys = 64;
+constexpr int kPf32Keys = 64;
 
-template <class TT, int D>
+template <class TT, int D, int WAVES>
 __device__ __forceinline__ void rows32(const PfArgs& a) {
+  constexpr int kPf32Rows = 32 * WAVES;
   constexpr int ES = elem_bytes<TT>();
   constexpr int HALF = kPf32Keys * D * 2;     // bytes of the K (or V) rows of a tile
-  constexpr int PER = HALF / 1024 / 8;        // copies per wave of each
+  constexpr int PER = HALF / 1024 / WAVES;    // copies per wave of each
   constexpr int DT = D / 32;
   __shared__ __align__(1024) char smem[2 * 2 * HALF];
   const PrefillArgs& p = a.p;
@@ -453,8 +454,8 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
   if (live) store_column(a, col, b, j, r, split);
 }
 
-template <class TT, int D>
-__global__ __launch_bounds__(kPf32Threads, 2) void pf_rows32(PfArgs a) { rows32<TT, D>(a); }
+template <class TT, int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void pf_rows32(PfArgs a) { rows32<TT, D, WAVES>(a); }
 
 // Few rows, bf16: a work-group of two waves takes 32 packed rows, both waves the
 // same ones.  The waves go over the 32-key steps of the work-group's split in
@@ -624,7 +625,7 @@ void launch_join(const PfArgs& a, hipStream_t s) {
   else hipLaunchKernelGGL((pf_join<T, D, false, 8>), one, dim3(256), 0, s, a);
 }
 
-enum PfKernel { kRows16, kRows32, kFew };
+enum PfKernel { kRows16, kRows32, kRows32Half, kFew };
 
 struct PfPlan {
   PfKernel kernel;
@@ -633,22 +634,30 @@ struct PfPlan {
 };
 
 // Kernel and splits over the keys: the pair with the least estimated time
-//   max(key tiles of the longest work-group * us a tile,
-//       key tiles of all / work-groups at a time * us a tile,
-//       K and V at 4.5 TB/s) + what the join costs.
-// A tile of pf_rows32 (256 rows, 64 keys, one work-group per compute unit) takes
-// 1.95 us (1.15 at d 64), of pf_few (32 rows, two waves with 32 keys each, two
-// work-groups) 1.3 (0.9), of pf_rows16 (64 rows, 32 keys, two) 2.6; the join a launch
-// (4 us), a round trip per 16 splits and the partial states there and back at 4 TB/s.
-// us measured, pf_few / pf_rows32 (its splits): 250 rows of 32 heads 10.5 / 16 (1), 500
-// rows of 28 heads 16 / 26 (3), 1000 rows of 32 heads 33 / 44 (2), 2000 of 28 heads
-// 78 / 62 (1), 100 rows over 5000 keys 32 / 29 (16); d 64, 4000 rows of 16 heads 75
-// in one piece, 69 in two.
+//   max(the longest work-group, all of them over what runs at a time, K and V at 4.5 TB/s)
+//     + what the join costs,
+// a work-group taking so long per key tile and so long besides (first loads, masked
+// tiles, stores):
+//   pf_rows32, 8 waves  256 rows, 64 keys, 256 at a time: 1.9 us a tile (alone 1.78) + 6
+//   pf_rows32, 4 waves  128 rows, 64 keys, 512 at a time: 2.05 us (alone 1.5) + 5
+//   pf_few              32 rows, 2 x 32 keys, 512 at a time: 1.3 us + 5
+//   pf_rows16           64 rows, 32 keys, 512 at a time: 2.2 us (alone 2.8) + 4
+// (less with d = 64, where four waves are better at every size: 8000 rows of 16 heads
+// 167 us, eight waves 186; 4 x 4000 rows behind a window of 1000 93, 112).  A
+// join is a launch (4 us), a round trip per 16 splits and the partial states there and
+// back at 4 TB/s.
+// Measured us, 8 waves / 4 waves / pf_few, in one piece: 500 rows of 28 heads 23 / 18 /
+// 16, 1000 rows of 32 heads 34 / 29 / 32, 1500 rows 48 / 43 / 60, 1900 rows over 5900
+// keys 173 / 170, 8192 rows 520 / 535; 2048 rows of 28 heads behind a window of 4096
+// 134 / 139, 3000 rows behind one of 500 56 / 45.
 PfPlan pf_plan(const PrefillArgs& a) {
   const int64_t packed = (int64_t)a.q_len * a.G, heads = (int64_t)a.batch * a.H;
   PfPlan best = {};
   double least = 0;
-  auto consider = [&](PfKernel kernel, int rows, int keys, int at_a_time, double us) {
+  struct Cost {
+    double busy, alone, besides;  // us of a tile among others and alone, us besides
+  };
+  auto consider = [&](PfKernel kernel, int rows, int keys, int at_a_time, Cost c) {
     const int64_t tiles = (packed + rows - 1) / rows, groups = tiles * heads;
     // keys that a row tile sees at most, and on average
     double most = a.kv_len, mean = a.kv_len - 0.5 * (a.q_len < a.kv_len ? a.q_len : a.kv_len);
@@ -656,26 +665,32 @@ PfPlan pf_plan(const PrefillArgs& a) {
     if (a.window > 0 && span < most) most = span;
     if (mean > most) mean = most;
     const double state = 2.0 * a.batch * a.HQ * a.q_len * (a.D + kStateHead) * 4 / 4e6;  // us per split
-    const double all = groups * (mean / keys) / at_a_time * us;
     const double read = heads * most * 2 * a.D * a.esize / 4.5e6;
-    const double floor = all > read ? all : read;
     for (int S = 1; S <= 64 && (S == 1 || most / S >= 64); ++S) {
-      const double longest = ((double)(int64_t)((most / keys + S - 0.001) / S) + 1) * us;
-      const double t = (longest > floor ? longest : floor) + (S > 1 ? 4.0 + 0.7 * ((S + 15) / 16) + S * state : 0.0);
+      const double longest = ceil(most / keys / S) * c.alone + c.besides;
+      // behind a window all work-groups are alike and run in whole rounds
+      double rounds = (double)groups * S / at_a_time;
+      if (a.window > 0) rounds = ceil(rounds);
+      const double all = rounds * (mean / keys / S * c.busy + c.besides);
+      double t = longest > all ? longest : all;
+      if (t < read) t = read;
+      if (S > 1) t += 4.0 + 0.7 * ((S + 15) / 16) + S * state;
       if (best.S == 0 || t < least) {
         least = t;
         best.kernel = kernel;
         best.S = S;
         best.tiles = (int)tiles;
       }
-      if (longest <= floor) break;  // more splits only add states
+      if (longest <= all || longest <= read) break;  // more splits only add states
     }
   };
+  const bool d64 = a.D == 64;
   if (a.esize == 4) {
-    consider(kRows16, kPfRows, kPfKeys, 512, 2.6);
+    consider(kRows16, kPfRows, kPfKeys, 512, Cost{2.2, 2.8, 4});
   } else {
-    consider(kRows32, kPf32Rows, kPf32Keys, 256, a.D == 64 ? 1.15 : 1.95);
-    consider(kFew, kPfFewRows, 2 * kPfFewKeys, 512, a.D == 64 ? 0.9 : 1.3);
+    consider(kFew, kPfFewRows, 2 * kPfFewKeys, 512, d64 ? Cost{0.9, 0.9, 4} : Cost{1.3, 1.3, 5});
+    consider(kRows32Half, 128, kPf32Keys, 512, d64 ? Cost{1.15, 0.9, 4} : Cost{2.05, 1.5, 5});
+    if (!d64) consider(kRows32, 256, kPf32Keys, 256, Cost{1.9, 1.78, 6});
   }
   best.bytes = best.S > 1 ? (size_t)a.batch * a.HQ * a.q_len * best.S * (a.D + kStateHead) * 4 : 0;
   return best;
@@ -696,8 +711,10 @@ hipError_t run_prefill(const PrefillArgs& p, char* ws, hipStream_t s) {
   const dim3 grid(pf_grid(a));
   const bool d64 = p.D == 64;
   if (pl.kernel == kRows32) {
-    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64>), grid, dim3(kPf32Threads), 0, s, a);
-    else hipLaunchKernelGGL((pf_rows32<BF16, 128>), grid, dim3(kPf32Threads), 0, s, a);
+    hipLaunchKernelGGL((pf_rows32<BF16, 128, 8>), grid, dim3(512), 0, s, a);
+  } else if (pl.kernel == kRows32Half) {
+    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64, 4>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((pf_rows32<BF16, 128, 4>), grid, dim3(256), 0, s, a);
   } else if (pl.kernel == kFew) {
     if (d64) hipLaunchKernelGGL((pf_few<BF16, 64>), grid, dim3(kPfFewThreads), 0, s, a);
     else hipLaunchKernelGGL((pf_few<BF16, 128>), grid, dim3(kPfFewThreads), 0, s, a);

@@ -114,6 +114,9 @@ LONG = [  # b, H, G, d, q rows, keys, dtype, window, sinks, q_lens, kv_lens
     # ... split over the keys
     (1, 8, 4, 128, 100, 5000, "bf16", 0, 0, None, None),
     (1, 8, 4, 64, 200, 9000, "bf16", 4000, 65, None, None),
+    (1, 2, 4, 128, 600, 3000, "bf16", 0, 0, None, None),
+    (2, 2, 4, 128, 1000, 2100, "bf16", 2000, 3, [1000, 997], [2100, 2040]),
+    (1, 8, 4, 128, 500, 7001, "bf16", 0, 0, None, None),
 ]
 
 
