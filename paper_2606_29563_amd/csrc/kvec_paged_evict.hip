@@ -9,9 +9,10 @@
 //           and NaN at the bottom.  A radix select over 11, 11 and 10 bits
 //           finds the B-th largest key; of the slots that have it, the lowest are
 //           kept.  Kept slots behind B and evicted ones below it go to two lists
-//           in ascending order: a thread counts both over a run of neighbouring
-//           slots, one sum over the threads gives its places in the lists.
-//   move    pairs of the lists: K, V, acc and pos.
+//           in ascending order: a thread finds both in a run of neighbouring slots,
+//           one sum over the threads gives its places in the lists.
+//   move    pairs of the lists: K, V, acc and pos; bound by memory (113 MB to and fro in
+//           25 us).
 #include "kvec_attn_dev.h"
 #include "kvec_serve.h"
 
@@ -45,20 +46,32 @@ __device__ __forceinline__ int ev_page(const EvArgs& a, int b, int slot) {
   return page >= 0 && page < a.c.n_pages ? page : -1;
 }
 
+// Inclusive prefix over a wave, in registers: shifts by 1, 2, 4 and 8 within rows of 16
+// lanes, then lane 15 of a row to the next one, and lane 31 to the upper half.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+  return v;
+}
+
 // Exclusive prefix of v over the work-group and its total.  Barriers: one; tmp may be
 // written again behind the caller's next one.
 __device__ __forceinline__ int scan_before(int v, int* tmp, int& total) {
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int incl = wave_incl_scan(v);
+  const int incl = wave_scan(v);
   if (lane == 63) tmp[w] = incl;
   __syncthreads();
   int before = 0;
   total = 0;
 #pragma unroll
-  for (int i = 0; i < kEvWaves; ++i) {
-    const int x = tmp[i];
-    before += i < w ? x : 0;
-    total += x;
+  for (int i = 0; i < kEvWaves; i += 4) {
+    const int4 x = *reinterpret_cast<const int4*>(tmp + i);
+    before += (i < w ? x.x : 0) + (i + 1 < w ? x.y : 0) + (i + 2 < w ? x.z : 0) + (i + 3 < w ? x.w : 0);
+    total += x.x + x.y + x.z + x.w;
   }
   return before + incl - v;
 }
@@ -67,16 +80,19 @@ __device__ __forceinline__ int scan_before(int v, int* tmp, int& total) {
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
-// The keys of a tile of CAP slots are made in LDS, the loads of EB quads of slots of a
-// thread in flight at once (one round trip for the page entries and one for weights
-// and positions; slot by slot, three of each for 24k slots, the selection of 4 x 24k
-// slots took 26 us instead of 24); sequences of one tile make them once, longer ones in every pass.
+// Bound by latency: page entries, then weights and positions, then three passes with a
+// sum over the threads each (1088 slots: 7 us; 4 x 24571 slots of 8 heads: 18, of which
+// the keys take 5, a pass 2 and the lists 5).  The loads of EB quads of slots of a
+// thread are in flight at once (slot by slot 2 us more for 24k slots; 6 or 8 instead of
+// 3 no different).  Keys lie in LDS, those of sequences of one tile for all passes;
+// longer ones make them again in each.  Keys counted as they are made, LDS read four at
+// a time and once for both lists, and sums by register shifts took it from 23 to 18.
 template <int CAP, int EB>
 __global__ __launch_bounds__(kEvThreads) void ev_select(EvArgs a) {
   static_assert(CAP < 1 << 16, "two counts of a tile share a word");
   __shared__ __align__(16) uint32_t keys[CAP];
   __shared__ uint32_t hist[2][kEvBins];
-  __shared__ int tmp[2][kEvWaves];
+  __shared__ __align__(16) int tmp[2][kEvWaves];
   __shared__ uint32_t found[3][2];
   const int h = blockIdx.x, b = blockIdx.y, H = a.c.H, B = a.B, tid = threadIdx.x;
   const int n = min(max(a.c.lens[b], 0), a.c.max_len);
@@ -91,9 +107,13 @@ __global__ __launch_bounds__(kEvThreads) void ev_select(EvArgs a) {
   }
   const int64_t recent = a.window > 0 ? (int64_t)a.n_seen[b] - a.window : INT64_MAX;
   for (int i = tid; i < 2 * kEvBins; i += kEvThreads) (&hist[0][0])[i] = 0;
+  __syncthreads();
 
-  // four neighbouring slots a load (they share a page)
-  auto make_keys = [&](int t0, int m) {
+  // The keys of a tile's quads of slots to LDS and, as they are made, to f.  Four
+  // neighbouring slots a load (they share a page); the last quad's slots behind the tile
+  // get the lowest key: n > B slots are before them, so they are never kept.
+  uint4* keys4 = reinterpret_cast<uint4*>(keys);
+  auto make_keys = [&](int t0, int m, auto f) {
     const int quads = (m + 3) / 4;
     for (int q0 = 0; q0 < quads; q0 += EB * kEvThreads) {
       int page[EB], row[EB];
@@ -113,31 +133,23 @@ __global__ __launch_bounds__(kEvThreads) void ev_select(EvArgs a) {
       }
 #pragma unroll
       for (int i = 0; i < EB; ++i) {
+        const int q = q0 + i * kEvThreads + tid;
         uint32_t key[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const bool safe = p[i][e] < a.sinks || p[i][e] >= recent;
           // + 0: the two zeros are equal
-          key[e] = page[i] < 0 ? 0u : safe ? 0xffffffffu : x[i][e] != x[i][e] ? 0u : float_key(x[i][e] + 0.f);
+          key[e] = page[i] < 0 || 4 * q + e >= m ? 0u : safe ? 0xffffffffu : x[i][e] != x[i][e] ? 0u : float_key(x[i][e] + 0.f);
         }
-        const int q = q0 + i * kEvThreads + tid;
-        if (q < quads) *reinterpret_cast<uint4*>(keys + 4 * q) = make_uint4(key[0], key[1], key[2], key[3]);
+        if (q < quads) {
+          const uint4 k = make_uint4(key[0], key[1], key[2], key[3]);
+          keys4[q] = k;
+          f(k);
+        }
       }
     }
   };
   const int tiles = (n + CAP - 1) / CAP;
-  // f(tile, first slot, slots of the tile) with the tile's keys in LDS
-  auto each_tile = [&](bool fresh, auto f) {
-    for (int t = 0; t < tiles; ++t) {
-      const int t0 = t * CAP, m = min(CAP, n - t0);
-      if (fresh || tiles > 1) {
-        __syncthreads();
-        make_keys(t0, m);
-        __syncthreads();
-      }
-      f(t0, m);
-    }
-  };
 
   // radix select of the B-th largest key
   uint32_t prefix = 0, mask = 0;
@@ -147,13 +159,17 @@ __global__ __launch_bounds__(kEvThreads) void ev_select(EvArgs a) {
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
     const uint32_t digits = pass == 2 ? 1023u : 2047u;
     uint32_t* hp = hist[pass & 1];
-    each_tile(pass == 0, [&](int, int m) {
-#pragma unroll 4
-      for (int i = tid; i < m; i += kEvThreads) {
-        const uint32_t k = keys[i];
-        if ((k & mask) == prefix) atomicAdd(&hp[(k >> shift) & digits], 1u);
-      }
-    });
+    auto count = [&](uint4 k) {
+      auto one = [&](uint32_t x) {
+        if ((x & mask) == prefix) atomicAdd(&hp[(x >> shift) & digits], 1u);
+      };
+      one(k.x), one(k.y), one(k.z), one(k.w);
+    };
+    // (a thread reads the quads that it wrote itself)
+    if (pass == 0 || tiles > 1)
+      for (int t = 0; t < tiles; ++t) make_keys(t * CAP, min(CAP, n - t * CAP), count);
+    else
+      for (int q = tid; q < (n + 3) / 4; q += kEvThreads) count(keys4[q]);
     __syncthreads();
     // thread t: bins 2047 - 2t and 2046 - 2t, from the largest digit down
     const int top = kEvBins - 1 - 2 * tid;
@@ -173,31 +189,49 @@ __global__ __launch_bounds__(kEvThreads) void ev_select(EvArgs a) {
   }
   const uint32_t cut = prefix;  // the B-th largest key; the `need` lowest slots that have it are kept
 
-  // Thread t goes over the t-th run of a tile's slots; an odd run length, so that the
-  // threads' reads fall in distinct banks.
+  // Thread t goes over the t-th run of a tile's quads; an odd number of them, so that
+  // the threads' reads fall in distinct banks.
+  constexpr int RUN = ((CAP / 4 + kEvThreads - 1) / kEvThreads) | 1;
+  static_assert(4 * RUN <= 64, "a run's slots are bits of a word");
   int32_t* src = a.src + bh * a.cap;
   int32_t* dst = a.dst + bh * a.cap;
   int late0 = 0, hole0 = 0;
-  each_tile(false, [&](int t0, int m) {
-    const int run = ((m + kEvThreads - 1) / kEvThreads) | 1;
-    const int i0 = min(tid * run, m), i1 = min(i0 + run, m);
+  for (int t = 0; t < tiles; ++t) {
+    const int t0 = t * CAP, m = min(CAP, n - t0), quads = (m + 3) / 4;
+    if (tiles > 1) {
+      make_keys(t0, m, [](uint4) {});
+      __syncthreads();
+    }
+    const int run = ((quads + kEvThreads - 1) / kEvThreads) | 1;
+    const int q0 = tid * run, mine = min(max(quads - q0, 0), run);
+    uint4 k[RUN];
     int ties = 0, total;
-#pragma unroll 4
-    for (int i = i0; i < i1; ++i) ties += keys[i] == cut;
-    const int tie0 = need - scan_before(ties, tmp[0], total);  // ties wanted from this run on
+#pragma unroll
+    for (int i = 0; i < RUN; ++i)
+      if (i < mine) {
+        k[i] = keys4[q0 + i];
+        ties += (k[i].x == cut) + (k[i].y == cut) + (k[i].z == cut) + (k[i].w == cut);
+      }
+    int tie = need - scan_before(ties, tmp[0], total);  // ties wanted from this run on
     need -= total;
     // the run as two masks: kept behind B, evicted below it
-    static_assert(((CAP + kEvThreads - 1) / kEvThreads | 1) <= 64, "a run's slots are bits of a word");
+    const int i0 = 4 * q0;
     uint64_t late = 0, holes = 0;
-    int tie = tie0;
-#pragma unroll 4
-    for (int i = i0; i < i1; ++i) {
-      const uint32_t k = keys[i];
-      const bool keep = k > cut || (k == cut && tie > 0), low = t0 + i < B;
-      tie -= k == cut;
-      late |= (uint64_t)(keep && !low) << (i - i0);
-      holes |= (uint64_t)(!keep && low) << (i - i0);
-    }
+#pragma unroll
+    for (int i = 0; i < RUN; ++i)
+      if (i < mine) {
+        uint32_t keep = 0;
+        auto one = [&](uint32_t x, int e) {
+          keep |= (uint32_t)(x > cut || (x == cut && tie > 0)) << e;
+          tie -= x == cut;
+        };
+        one(k[i].x, 0), one(k[i].y, 1), one(k[i].z, 2), one(k[i].w, 3);
+        // of the quad's four slots, those below B
+        const int below = min(max(B - (t0 + i0 + 4 * i), 0), 4);
+        const uint32_t low = (1u << below) - 1;
+        late |= (uint64_t)(keep & ~low) << (4 * i);
+        holes |= (uint64_t)(~keep & low) << (4 * i);
+      }
     const int before = scan_before((int)__popcll(late) | (int)__popcll(holes) << 16, tmp[1], total);
     // (every thread is done with the keys:) the tile's lists, in LDS, then in whole lines
     const int n_late = total & 0xffff, n_holes = (int)((uint32_t)total >> 16);
@@ -209,8 +243,8 @@ __global__ __launch_bounds__(kEvThreads) void ev_select(EvArgs a) {
     for (int i = tid; i < n_holes; i += kEvThreads) dst[hole0 + i] = (int)keys[n_late + i];
     late0 += n_late;
     hole0 += n_holes;
-    __syncthreads();  // tmp, before the next tile
-  });
+    __syncthreads();  // keys and tmp, before the next tile
+  }
   // B slots are kept, so as many are kept behind B as are evicted below it
   if (tid == 0) a.count[bh] = late0;
 }
