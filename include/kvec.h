@@ -373,7 +373,7 @@ kvec_status kvec_decode_attention_noalloc(const kvec_config* cfg,
 /* Shape of one attention over a prompt. */
 typedef struct kvec_attention_config {
   int32_t batch;       /* sequences, 1..65535 */
-  int32_t n_kv_heads;  /* H, 1..1024 */
+  int32_t n_kv_heads;  /* H, 1..1024; batch * H at most 2^22 */
   int32_t n_q_heads;   /* multiple of H; G = n_q_heads / H in 1..16 */
   int32_t head_dim;    /* d in {64, 128} */
   int32_t q_len;       /* query rows per sequence, 1..2^20 */
@@ -412,7 +412,7 @@ kvec_status kvec_prefill_workspace_size(const kvec_attention_config* cfg, size_t
  * rounded to bf16 for the product with V.  The keys below nk have to be finite:
  * a NaN or infinity there can reach rows near it that do not see it.
  * kv_len rows of the k or v stride must span less than 2 GiB, and batch *
- * n_q_heads * q_len must be below 2^31 (else KVEC_ERR_UNSUPPORTED). */
+ * n_q_heads * q_len must be below 2^29 (else KVEC_ERR_UNSUPPORTED). */
 kvec_status kvec_prefill_attention(const kvec_attention_config* cfg,
                                    const void* q, const int64_t q_strides[3],
                                    const void* k, const int64_t k_strides[3],
@@ -442,7 +442,7 @@ kvec_status kvec_prefill_attention(const kvec_attention_config* cfg,
 
 typedef struct kvec_paged_config {
   int32_t batch;       /* sequences, 1..65535 */
-  int32_t n_kv_heads;  /* H, 1..1024 */
+  int32_t n_kv_heads;  /* H, 1..1024; batch * H at most 2^22 */
   int32_t n_q_heads;   /* multiple of H; G = n_q_heads / H in 1..16 */
   int32_t head_dim;    /* d in {64, 128} */
   int32_t page_size;   /* tokens per page, a multiple of 16 */

@@ -27,6 +27,8 @@ kvec_status check_heads(int32_t batch, int32_t H, int32_t HQ, int32_t d, int32_t
   if (batch < 1 || H < 1 || HQ < 1 || HQ % H != 0 || d < 1) return KVEC_ERR_INVALID;
   if (dtype != KVEC_BF16 && dtype != KVEC_F32) return KVEC_ERR_INVALID;
   if (batch > 65535 || H > 1024 || HQ / H > 16 || (d != 64 && d != 128)) return KVEC_ERR_UNSUPPORTED;
+  // with the bound on a prompt's rows: launches stay below 2^32 threads
+  if ((int64_t)batch * H > 1 << 22) return KVEC_ERR_UNSUPPORTED;
   return KVEC_OK;
 }
 
@@ -36,7 +38,7 @@ kvec_status make_prefill(const kvec_attention_config* c, PrefillArgs* a) {
   if (st != KVEC_OK) return st;
   if (c->q_len < 1 || c->kv_len < 1 || c->window < 0 || c->n_sinks < 0) return KVEC_ERR_INVALID;
   if (c->q_len > kMaxLen || c->kv_len > kMaxLen) return KVEC_ERR_UNSUPPORTED;
-  if ((int64_t)c->batch * c->n_q_heads * c->q_len >= (int64_t)1 << 31) return KVEC_ERR_UNSUPPORTED;
+  if ((int64_t)c->batch * c->n_q_heads * c->q_len >= (int64_t)1 << 29) return KVEC_ERR_UNSUPPORTED;
   memset(a, 0, sizeof(*a));
   a->batch = c->batch;
   a->H = c->n_kv_heads;

@@ -25,12 +25,12 @@ def _attn(**kw):
 
 HEADS = [(dict(batch=0), INV), (dict(n_kv_heads=0), INV), (dict(n_q_heads=33), INV), (dict(head_dim=0), INV), (dict(dtype=2), INV),
          (dict(batch=65536), UNS), (dict(n_kv_heads=2, n_q_heads=34), UNS), (dict(n_kv_heads=2048, n_q_heads=2048), UNS),
-         (dict(head_dim=96), UNS)]
+         (dict(head_dim=96), UNS), (dict(batch=4097, n_kv_heads=1024, n_q_heads=1024), UNS)]
 
 
 @pytest.mark.parametrize("over,code", HEADS + [
     (dict(q_len=0), INV), (dict(kv_len=0), INV), (dict(window=-1), INV), (dict(n_sinks=-1), INV),
-    (dict(q_len=(1 << 20) + 1), UNS), (dict(kv_len=(1 << 20) + 1), UNS), (dict(batch=64, n_q_heads=128, q_len=1 << 18), UNS)])
+    (dict(q_len=(1 << 20) + 1), UNS), (dict(kv_len=(1 << 20) + 1), UNS), (dict(batch=64, n_q_heads=128, q_len=1 << 16), UNS)])
 def test_attention_config(over, code):
     with pytest.raises(kvec.KvecError) as e:
         kvec.kvec_prefill_workspace_size(_attn(**over))
