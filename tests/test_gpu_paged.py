@@ -582,3 +582,78 @@ def test_streams_and_graph(gpu_lib):
         for name in ("out", "q_out", "k", "v", "acc", "pos", "lens", "seen"):
             assert torch.equal(eager[name], graphed[name]), name
     assert eager["lens"].tolist() == [60, 60]
+
+
+@pytest.mark.parametrize("dt,G,n", [("bf16", 4, 1500), ("f32", 5, 700)])
+def test_same_bits_twice(gpu_lib, dt, G, n):
+    """A decode step gives the same bits whatever its workspace held."""
+    import torch
+    got = []
+    for fill in (0, 255):
+        c = Cache(gpu_lib, [n, 3, n // 2], 2, G, 64, 32, dt, seed=8).cuda()
+        q = c.rand(3, 2 * G, 64).to(_dt(dt)).cuda()
+        ws = torch.full((gpu_lib.kvec_paged_decode_workspace_size(c.cfg, None, True),), fill, dtype=torch.uint8, device="cuda")
+        out, lse = torch.empty(3, 2 * G, 64, device="cuda"), torch.empty(3, 2 * G, device="cuda")
+        gpu_lib.kvec_paged_decode(c.cfg, q, c.k, c.v, c.table, c.lens, out, ws, lse=lse, acc=c.acc)
+        got.append([x.view(torch.int32) for x in (out, lse, c.acc)])
+    assert all(x.equal(y) for x, y in zip(*got))
+
+
+def test_binding_refuses_on_the_gpu(gpu_lib):
+    """Tensors that do not fit the configuration, and values that the C interface refuses:
+    the error is raised and nothing is written."""
+    import torch
+    kv, b, H, HQ, d, page = gpu_lib, 2, 2, 8, 64, 16
+    cfg = kv.PagedConfig(b, H, HQ, d, page, 6, 3)
+    zeros = lambda *s, t=torch.bfloat16: torch.zeros(s, dtype=t, device="cuda")  # noqa: E731
+    i32 = torch.int32
+    pools = dict(k_pool=zeros(6, H, page, d), v_pool=zeros(6, H, page, d))
+    seq = dict(page_table=torch.arange(6, dtype=i32, device="cuda").view(b, 3), lens=zeros(b, t=i32) + 5)
+    meta = dict(acc=zeros(6, H, page, t=torch.float32), pos=zeros(6, H, page, t=i32))
+    ws = zeros(1 << 20, t=torch.uint8)
+    tok = dict(q=zeros(3, HQ, d) + 1, k=zeros(3, H, d) + 1, v=zeros(3, H, d) + 1, positions=zeros(3, t=i32),
+               slots=torch.arange(3, device="cuda"), q_out=zeros(3, HQ, d))
+    wide, rows = zeros(6, H, page, 2 * d), zeros(6, page, H, d).transpose(1, 2)
+    f32 = torch.float32
+    attn = kv.AttentionConfig(b, H, HQ, d, 7, 40)
+    prompt = dict(q=zeros(b, HQ, 7, d) + 1, k=zeros(b, H, 40, d) + 1, v=zeros(b, H, 40, d) + 1, out=zeros(b, HQ, 7, d), ws=ws)
+    step = dict(q=zeros(b, HQ, d) + 1, out=zeros(b, HQ, d, t=f32), ws=ws)
+    off = lambda t: torch.cat([t.flatten(), t.flatten()])[1:1 + t.numel()].view(t.shape)  # noqa: E731  (2 or 4 bytes off)
+    cases = [
+        (lambda **k: kv.kvec_paged_append(cfg, **k), {**tok, **pools, **meta},
+         [dict(q=tok["q"][:, :7]), dict(k=tok["k"].float()), dict(v=tok["v"][:2]), dict(positions=tok["positions"].long()),
+          dict(slots=tok["slots"].int()), dict(q_out=zeros(3, d, HQ).transpose(1, 2)), dict(k_pool=rows), dict(v_pool=pools["v_pool"].cpu()),
+          dict(v_pool=wide[..., ::2]), dict(q_weight=zeros(d + 8)), dict(k_weight=zeros(d, t=f32)), dict(inv_freq=zeros(d // 2, t=f32)),
+          dict(acc=meta["acc"].half()), dict(pos=meta["pos"][:5])],
+         [dict(q=off(tok["q"])), dict(inv_freq=zeros(d // 2 + 8, t=torch.float64)), dict(inv_freq=zeros(3, t=torch.float64)), dict(eps=-1.0),
+          dict(q_weight=off(zeros(d)))]),
+        (lambda **k: kv.kvec_paged_decode(cfg, **k), {**step, **pools, **seq, "acc": meta["acc"]},
+         [dict(q=step["q"][:1]), dict(out=step["out"].bfloat16()), dict(out=zeros(HQ, b, d, t=f32).transpose(0, 1)), dict(lens=seq["lens"].cpu()),
+          dict(page_table=seq["page_table"][:, :2]), dict(lse=zeros(b, H, t=f32)), dict(acc=zeros(6, page, H, t=f32)), dict(ws=ws[::2]),
+          dict(ws=ws.cpu()), dict(k_pool=wide[..., :d])],
+         [dict(ws=None), dict(ws=ws[:64]), dict(ws=ws[1:]), dict(max_len=0), dict(max_len=49), dict(window=-1), dict(n_sinks=-1), dict(q=off(step["q"]))]),
+        (lambda **k: kv.kvec_paged_evict(cfg, **{**dict(budget=4), **k}), {**pools, **seq, **meta, "n_seen": seq["lens"], "lens_out": zeros(b, t=i32), "ws": ws},
+         [dict(n_seen=zeros(b + 1, t=i32)), dict(lens_out=zeros(b, t=f32)), dict(acc=None), dict(kept=zeros(b, H, 5, t=i32)),
+          dict(kept=zeros(b, 4, H, t=i32).transpose(1, 2)), dict(pos=meta["pos"].cpu())],
+         [dict(budget=0), dict(budget=(1 << 20) + 1), dict(window=4, n_sinks=1), dict(window=-1), dict(ws=None), dict(max_len=49)]),
+        (lambda **k: kv.kvec_prefill_attention(attn, **k), prompt,
+         [dict(q=prompt["q"][:, :, :6]), dict(k=prompt["k"][:, :1]), dict(v=prompt["v"].float()), dict(out=prompt["out"].cpu()),
+          dict(lse=zeros(b, HQ, 7)), dict(lse=zeros(b, 7, HQ, t=f32).transpose(1, 2)), dict(q_lens=zeros(b, t=torch.int64)), dict(kv_lens=zeros(1, t=i32)),
+          dict(k=prompt["k"].transpose(2, 3).contiguous().transpose(2, 3))],
+         [dict(q=off(prompt["q"])), dict(out=zeros(b, HQ, 7, d + 4)[..., :d])]),
+    ]
+    before = [t.clone() for t in (*pools.values(), *meta.values(), tok["q_out"], step["out"], prompt["out"])]
+    for call, good, misfits, invalid in cases:
+        for bad in misfits:
+            with pytest.raises(AssertionError):
+                call(**{**good, **bad})
+        for bad in invalid:
+            with pytest.raises(kv.KvecError):
+                call(**{**good, **bad})
+    torch.cuda.synchronize()
+    for x, t in zip(before, (*pools.values(), *meta.values(), tok["q_out"], step["out"], prompt["out"])):
+        assert x.equal(t)
+    for call, good, _, _ in cases:
+        call(**good)  # and without a fault they run
+    torch.cuda.synchronize()
+    assert pools["k_pool"].any() and step["out"].any() and prompt["out"].any()
