@@ -538,7 +538,8 @@ kvec_status kvec_paged_evict_workspace_size(const kvec_paged_config* cfg, int32_
  *   acc, pos    device in/out.
  *   kept        nullable device out, int32 [batch][H][budget]: the slot that each
  *               slot's content came from; -1 behind n.
- *   lens_out    device out, int32 [batch]: min(n, budget); may be lens.
+ *   lens_out    device out, int32 [batch]: min(n, budget); may be lens (apart from
+ *               lens and n_seen, few rows move in the launch that selects them).
  *   ws          device workspace of kvec_paged_evict_workspace_size() bytes. */
 kvec_status kvec_paged_evict(const kvec_paged_config* cfg, int32_t budget,
                              int32_t window, int32_t n_sinks,

@@ -3,7 +3,8 @@
 // What has to be moved is little: a kept slot behind the budget goes into an
 // evicted slot below it, every other kept slot stays, so at most as many rows
 // move as were evicted, and sources (slots >= B) and targets (slots < B) are
-// disjoint, so all of them can move at once.  Two launches:
+// disjoint, so all of them can move at once.  Two launches (one when there are few and
+// the lengths go to an array of their own):
 //   select  one work-group per (KV head, sequence).  A key orders the slots:
 //           the weight's bits, order preserving, with protected slots on top
 //           and NaN at the bottom.  A radix select over 11, 11 and 10 bits
@@ -76,6 +77,35 @@ __device__ __forceinline__ int scan_before(int v, int* tmp, int& total) {
   return before + incl - v;
 }
 
+// Rows of `count` pairs of slots (pair(i, &from, &to)) by `threads` threads, ROW / 16 of
+// them a row of K and V (ROW: its bytes).
+template <int ROW, class Pair>
+__device__ __forceinline__ void move_rows(const EvArgs& a, int b, int h, int count, int thread, int threads, Pair pair) {
+  constexpr int LPR = ROW / 16;
+  const int H = a.c.H, p = thread % LPR;
+  for (int i = thread / LPR; i < count; i += threads / LPR) {
+    int s, d;
+    pair(i, &s, &d);
+    // the lists of ev_move lie in the caller's workspace: nothing outside the cache is followed
+    if ((uint32_t)s >= (uint32_t)a.c.max_len || (uint32_t)d >= (uint32_t)min(a.B, a.c.max_len)) continue;
+    const int ps = ev_page(a, b, s), pd = ev_page(a, b, d);
+    const int rs = s - ev_page_index(a, s) * a.c.ps, rd = d - ev_page_index(a, d) * a.c.ps;
+    if (p == 0 && a.kept) a.kept[((int64_t)b * H + h) * a.B + d] = s;
+    if (ps < 0 || pd < 0) continue;
+    const int64_t es = a.c.esize;
+    const int64_t from = (ps * a.c.sp + h * a.c.sh + rs * a.c.sr) * es, to = (pd * a.c.sp + h * a.c.sh + rd * a.c.sr) * es;
+    const uint4 kx = reinterpret_cast<const uint4*>(a.c.k + from)[p];
+    const uint4 vx = reinterpret_cast<const uint4*>(a.c.v + from)[p];
+    if (p == 0) {
+      const int64_t f = (ps * (int64_t)H + h) * a.c.ps + rs, t = (pd * (int64_t)H + h) * a.c.ps + rd;
+      a.acc[t] = a.acc[f];
+      a.pos[t] = a.pos[f];
+    }
+    reinterpret_cast<uint4*>(a.c.k + to)[p] = kx;
+    reinterpret_cast<uint4*>(a.c.v + to)[p] = vx;
+  }
+}
+
 // acc and pos are aligned to their elements
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
@@ -87,7 +117,8 @@ typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 // 3 no different).  Keys lie in LDS, those of sequences of one tile for all passes;
 // longer ones make them again in each.  Keys counted as they are made, LDS read four at
 // a time and once for both lists, and sums by register shifts took it from 23 to 18.
-template <int CAP, int EB>
+// MOVE: bytes of a K or V row, moved by this launch (0: by the second).
+template <int CAP, int EB, int MOVE>
 __global__ __launch_bounds__(kEvThreads) void ev_select(EvArgs a) {
   static_assert(CAP < 1 << 16, "two counts of a tile share a word");
   __shared__ __align__(16) uint32_t keys[CAP];
@@ -97,12 +128,12 @@ __global__ __launch_bounds__(kEvThreads) void ev_select(EvArgs a) {
   const int h = blockIdx.x, b = blockIdx.y, H = a.c.H, B = a.B, tid = threadIdx.x;
   const int n = min(max(a.c.lens[b], 0), a.c.max_len);
   const int64_t bh = (int64_t)b * H + h;
-  if (tid == 0 && h == 0) a.new_len[b] = min(n, B);
+  if (tid == 0 && h == 0) (MOVE ? a.lens_out : a.new_len)[b] = min(n, B);
   // what is kept below the budget stays there; the moves fill in the others
   if (a.kept)
     for (int s = tid; s < B; s += kEvThreads) a.kept[bh * B + s] = s < n ? s : -1;
   if (n <= B) {
-    if (tid == 0) a.count[bh] = 0;
+    if (!MOVE && tid == 0) a.count[bh] = 0;
     return;
   }
   const int64_t recent = a.window > 0 ? (int64_t)a.n_seen[b] - a.window : INT64_MAX;
@@ -239,6 +270,13 @@ __global__ __launch_bounds__(kEvThreads) void ev_select(EvArgs a) {
     for (; late; late &= late - 1) keys[at_late++] = t0 + i0 + __builtin_ctzll(late);
     for (; holes; holes &= holes - 1) keys[at_hole++] = t0 + i0 + __builtin_ctzll(holes);
     __syncthreads();
+    if constexpr (MOVE > 0) {  // (one tile: n <= CAP)
+      move_rows<MOVE>(a, b, h, min(n_late, n_holes), tid, kEvThreads, [&](int i, int* from, int* to) {
+        *from = (int)keys[i];
+        *to = (int)keys[n_late + i];
+      });
+      return;
+    }
     for (int i = tid; i < n_late; i += kEvThreads) src[late0 + i] = (int)keys[i];
     for (int i = tid; i < n_holes; i += kEvThreads) dst[hole0 + i] = (int)keys[n_late + i];
     late0 += n_late;
@@ -251,42 +289,26 @@ __global__ __launch_bounds__(kEvThreads) void ev_select(EvArgs a) {
 
 constexpr int kMvThreads = 256;
 
-template <int ROW>  // bytes of a K or V row
+template <int ROW>
 __global__ __launch_bounds__(kMvThreads) void ev_move(EvArgs a) {
-  constexpr int LPR = ROW / 16;
-  const int h = blockIdx.y, b = blockIdx.z, H = a.c.H;
-  const int64_t bh = (int64_t)b * H + h;
+  const int h = blockIdx.y, b = blockIdx.z;
+  const int64_t bh = (int64_t)b * a.c.H + h;
   if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0) a.lens_out[b] = a.new_len[b];
-  const int count = min(a.count[bh], a.cap);
-  const int p = threadIdx.x % LPR;
   const int32_t* src = a.src + bh * a.cap;
   const int32_t* dst = a.dst + bh * a.cap;
-  for (int i = blockIdx.x * (kMvThreads / LPR) + threadIdx.x / LPR; i < count; i += gridDim.x * (kMvThreads / LPR)) {
-    const int s = src[i], d = dst[i];
-    // the lists lie in the caller's workspace: nothing outside the cache is followed
-    if ((uint32_t)s >= (uint32_t)a.c.max_len || (uint32_t)d >= (uint32_t)min(a.B, a.c.max_len)) continue;
-    const int ps = ev_page(a, b, s), pd = ev_page(a, b, d);
-    const int rs = s - ev_page_index(a, s) * a.c.ps, rd = d - ev_page_index(a, d) * a.c.ps;
-    if (p == 0 && a.kept) a.kept[bh * a.B + d] = s;
-    if (ps < 0 || pd < 0) continue;
-    const int64_t es = a.c.esize;
-    const int64_t from = (ps * a.c.sp + h * a.c.sh + rs * a.c.sr) * es, to = (pd * a.c.sp + h * a.c.sh + rd * a.c.sr) * es;
-    const uint4 kx = reinterpret_cast<const uint4*>(a.c.k + from)[p];
-    const uint4 vx = reinterpret_cast<const uint4*>(a.c.v + from)[p];
-    if (p == 0) {
-      const int64_t f = (ps * (int64_t)H + h) * a.c.ps + rs, t = (pd * (int64_t)H + h) * a.c.ps + rd;
-      a.acc[t] = a.acc[f];
-      a.pos[t] = a.pos[f];
-    }
-    reinterpret_cast<uint4*>(a.c.k + to)[p] = kx;
-    reinterpret_cast<uint4*>(a.c.v + to)[p] = vx;
-  }
+  move_rows<ROW>(a, b, h, min(a.count[bh], a.cap), blockIdx.x * kMvThreads + threadIdx.x, gridDim.x * kMvThreads,
+                 [&](int i, int* from, int* to) {
+                   *from = src[i];
+                   *to = dst[i];
+                 });
 }
 
 int move_cap(const PagedView& c, int B) {
   const int over = c.max_len - B;
   return over < 0 ? 0 : over < B ? over : B;
 }
+constexpr int kEvSmall = 4096;           // slots of a sequence selected in one tile
+constexpr int kEvMoveBytes = 64 << 10;   // K (and V) bytes of a head moved by the selecting work-group
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 }  // namespace
@@ -318,11 +340,23 @@ hipError_t run_paged_evict(const PagedView& c, int budget, int window, int sinks
   a.src = reinterpret_cast<int32_t*>(ws);
   a.dst = reinterpret_cast<int32_t*>(ws + up256(bh * a.cap * 4));
   const dim3 grid(c.H, c.batch);
-  if (c.max_len <= 4096) hipLaunchKernelGGL((ev_select<4096, 1>), grid, dim3(kEvThreads), 0, s, a);
-  else hipLaunchKernelGGL((ev_select<32768, 3>), grid, dim3(kEvThreads), 0, s, a);
+  const int row = c.D * c.esize;
+  // One launch where a work-group has few rows to move and no other reads what this one
+  // writes: the lengths, unless they are replaced in place.  us with one launch / two, 8
+  // heads with rows of 256 bytes and 1024 kept: of 1088 slots 9.9 / 12.3, of 1280 11.8 /
+  // 12.3, of 1536 13.7 / 12.5; 32 sequences of 1280 14.1 / 15.8.
+  auto apart = [&](const int32_t* in) { return lens_out + c.batch <= in || in + c.batch <= lens_out; };
+  if (c.max_len <= kEvSmall && (int64_t)a.cap * row <= kEvMoveBytes && apart(c.lens) && apart(n_seen)) {
+    if (row == 128) hipLaunchKernelGGL((ev_select<kEvSmall, 1, 128>), grid, dim3(kEvThreads), 0, s, a);
+    else if (row == 256) hipLaunchKernelGGL((ev_select<kEvSmall, 1, 256>), grid, dim3(kEvThreads), 0, s, a);
+    else hipLaunchKernelGGL((ev_select<kEvSmall, 1, 512>), grid, dim3(kEvThreads), 0, s, a);
+    return hipGetLastError();
+  }
+  if (c.max_len <= kEvSmall) hipLaunchKernelGGL((ev_select<kEvSmall, 1, 0>), grid, dim3(kEvThreads), 0, s, a);
+  else hipLaunchKernelGGL((ev_select<32768, 3, 0>), grid, dim3(kEvThreads), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int row = c.D * c.esize, per = kMvThreads / (row / 16);
+  const int per = kMvThreads / (row / 16);
   int64_t x = (a.cap + per - 1) / per;
   const int64_t most = (2048 + (int64_t)bh - 1) / (int64_t)bh;
   if (x > most) x = most;

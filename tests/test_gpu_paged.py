@@ -428,6 +428,19 @@ def test_evict_few_values_at_the_ends_of_key_tiles(gpu_lib, lens, budget):
     _check_evict(c, before, kept, out, budget, 700, 5, seen)
 
 
+@pytest.mark.parametrize("lens,d,dt,budget", [([300, 257, 256, 5], 64, "bf16", 256), ([290, 500, 0], 128, "bf16", 256), ([200, 129], 128, "f32", 128),
+                                              ([90, 64, 77], 64, "f32", 60), ([40, 60], 128, "bf16", 3)])
+def test_evict_few_rows_with_lengths_apart_and_in_place(gpu_lib, lens, d, dt, budget):
+    """Few rows to move: the same results whether the lengths are replaced in place or not."""
+    import torch
+    seen = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    for in_place in (False, True):
+        c = Cache(gpu_lib, lens, 3, 1, d, 32, dt, seed=budget).cuda()
+        before = [t.clone() for t in (c.k, c.v, c.acc, c.pos)]
+        kept, out = _evict(c, budget, 1, 1, seen, in_place=in_place)
+        _check_evict(c, before, kept, out, budget, 1, 1, seen)
+
+
 def test_evict_in_place_lengths_bad_pages_and_clamped_lengths(gpu_lib):
     """lens_out = lens = n_seen; slots without a page rank last and do not move."""
     import torch
