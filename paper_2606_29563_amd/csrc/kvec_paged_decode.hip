@@ -1,6 +1,6 @@
 // One new token's attention over a paged cache.
 //
-// Bound by reading the visible K and V rows once.  Two launches:
+// Bound by reading the visible K and V rows once.  Two launches, or one:
 //   partial  one work-group of four waves per (split, KV head, sequence).  The
 //            visible slots of a sequence, in groups of 16 (a group lies in one
 //            page), are divided evenly over the splits, from the device's own
@@ -69,9 +69,40 @@ __device__ __forceinline__ bool page_ok(const PdArgs& a, int page) { return page
 // Groups of a split: `per` from x * per on.
 __device__ __forceinline__ int split_groups(const Visible& v, int S) { return (v.groups + S - 1) / S; }
 
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));  // acc is aligned to its elements
+
+// Adds the mean over the query heads of 2^(logit - norm) to four neighbouring slots:
+// y: the first four heads' logits, lg: the first head's in memory; whole: all four slots
+// are visible, and held `old`.
+__device__ __forceinline__ void add_weights(const PdArgs& a, const Visible& vis, int slot, float* acc, bool whole,
+                                            f32x4 old, const f32x4 (&y)[4], const float* lg, const float* norm) {
+  const int G = a.c.G;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int g = 0; g < 4; ++g)
+    if (g < G)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] += __builtin_amdgcn_exp2f(y[g][i] - norm[g]);
+#pragma unroll 4
+  for (int g = 4; g < G; ++g) {
+    const f32x4 z = *reinterpret_cast<const f32x4*>(lg + (int64_t)g * a.pad);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] += __builtin_amdgcn_exp2f(z[i] - norm[g]);
+  }
+  const float mean = 1.f / G;
+  if (whole) {
+    *reinterpret_cast<f32x4_any*>(acc) = old + sum * mean;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (vis.sees(slot + i)) acc[i] += sum[i] * mean;
+  }
+}
+
 constexpr int kPdRing = 2;  // groups of 16 slots in flight per wave
 
-template <class TT, int D>
+// ONE: the sequence is not split, its work-group finishes the results itself.
+template <class TT, int D, bool ONE>
 __device__ __forceinline__ void partial(const PdArgs& a, char* smem) {
   using RG = RowGroup<TT, D>;
   constexpr int ES = RG::ES;
@@ -167,6 +198,7 @@ __device__ __forceinline__ void partial(const PdArgs& a, char* smem) {
   __syncthreads();
 
   // merge the four waves through LDS (the ring is free)
+  __shared__ float norm[16];  // (ONE:) base-2 normaliser of a query head
   float* sm = reinterpret_cast<float*>(smem);  // [waves][16][D + 2]
   col.l = col_sum4(col.l);
 #pragma unroll
@@ -186,26 +218,54 @@ __device__ __forceinline__ void partial(const PdArgs& a, char* smem) {
       const float* p = sm + (ww * 16 + g) * (D + 2);
       state_merge(m, l, o, p[0], p[1], p[2 + e]);
     }
-    float* pp = a.part + (((int64_t)b * a.c.HQ + h * G + g) * a.S + s) * (D + 2);
-    pp[2 + e] = o;
-    if (e == 0) {
-      pp[0] = m;
-      pp[1] = l;
+    const int64_t j = (int64_t)b * a.c.HQ + h * G + g;
+    if constexpr (ONE) {
+      a.out[j * D + e] = m == -INFINITY ? 0.f : o / l;
+      if (e == 0) {
+        const float ln2 = m + log2f(l);
+        norm[g] = ln2;
+        if (a.lse) a.lse[j] = m == -INFINITY ? -INFINITY : ln2 * 0.69314718055994531f;
+      }
+    } else {
+      float* pp = a.part + (j * a.S + s) * (D + 2);
+      pp[2 + e] = o;
+      if (e == 0) {
+        pp[0] = m;
+        pp[1] = l;
+      }
+    }
+  }
+  if constexpr (ONE) {
+    if (!a.acc) return;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 4 * vis.groups; i += kPdThreads) {
+      int row, slot = vis.slot0(i >> 2);
+      const int page = page_of(a, b, slot, &row);
+      if (!page_ok(a, page)) continue;
+      row += 4 * (i & 3);
+      slot += 4 * (i & 3);
+      const float* lg = a.logits + ((int64_t)b * a.c.H + h) * G * a.pad + slot;
+      f32x4 y[4], old = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int g = 0; g < 4; ++g) y[g] = *reinterpret_cast<const f32x4*>(lg + (int64_t)min(g, G - 1) * a.pad);
+      float* acc = a.acc + ((int64_t)page * a.c.H + h) * a.c.ps + row;
+      const bool whole = vis.sees(slot) && vis.sees(slot + 1) && vis.sees(slot + 2) && vis.sees(slot + 3);
+      if (whole) old = *reinterpret_cast<const f32x4_any*>(acc);
+      add_weights(a, vis, slot, acc, whole, old, y, lg, norm);
     }
   }
 }
 
-template <class TT, int D>
+template <class TT, int D, bool ONE>
 __global__ __launch_bounds__(kPdThreads) void pd_partial(PdArgs a) {
   constexpr int RING = kPdWaves * kPdRing * 2 * RowGroup<TT, D>::BYTES, MERGE = kPdWaves * 16 * (D + 2) * 4;
   __shared__ __align__(1024) char smem[RING > MERGE ? RING : MERGE];
-  partial<TT, D>(a, smem);
+  partial<TT, D, ONE>(a, smem);
 }
 
 // Work-group x of a (KV head, sequence): the output of query head x while x < G,
 // and the weights of 1024 slots, four a thread.
 constexpr int kPdAccGroups = kPdThreads / 4;
-typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));  // acc is aligned to its elements
 
 template <int D>
 __global__ __launch_bounds__(kPdThreads) void pd_combine(PdArgs a) {
@@ -287,26 +347,7 @@ __global__ __launch_bounds__(kPdThreads) void pd_combine(PdArgs a) {
   }
   __syncthreads();
   if (!ok) return;
-  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int g = 0; g < 4; ++g)
-    if (g < G)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sum[i] += __builtin_amdgcn_exp2f(y[g][i] - norm[g]);
-#pragma unroll 4
-  for (int g = 4; g < G; ++g) {
-    const f32x4 z = *reinterpret_cast<const f32x4*>(lg + (int64_t)g * a.pad);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sum[i] += __builtin_amdgcn_exp2f(z[i] - norm[g]);
-  }
-  const float mean = 1.f / G;
-  if (whole) {
-    *reinterpret_cast<f32x4_any*>(acc) = old + sum * mean;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (vis.sees(slot + i)) acc[i] += sum[i] * mean;
-  }
+  add_weights(a, vis, slot, acc, whole, old, y, lg, norm);
 }
 
 // Bound of a sequence's visible groups.
@@ -319,7 +360,12 @@ int most_groups(const PagedView& c, int window, int sinks) {
 
 template <class TT, int D>
 hipError_t launch(const PdArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((pd_partial<TT, D>), dim3(a.S, a.c.H, a.c.batch), dim3(kPdThreads), 0, s, a);
+  const dim3 grid(a.S, a.c.H, a.c.batch);
+  if (a.S == 1) {
+    hipLaunchKernelGGL((pd_partial<TT, D, true>), grid, dim3(kPdThreads), 0, s, a);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((pd_partial<TT, D, false>), grid, dim3(kPdThreads), 0, s, a);
   const hipError_t e1 = hipGetLastError();
   if (e1 != hipSuccess) return e1;
   int x = a.c.G;
@@ -338,7 +384,8 @@ hipError_t launch(const PdArgs& a, hipStream_t s) {
 // down to one group a wave.  us of both launches with 512 / 1024 / 4096
 // work-groups, 16 sequences of 8k to 16k slots (8 heads, d 128): 169 / 163 / 170;
 // with 256 / 1024 slots at least, one sequence of 32k: 35.2 / 27.5, 32 of 1k to 2k:
-// 48.6 / 50.3.
+// 48.6 / 50.3.  Up to 256 slots are not split: the one launch (us of it / of two; one
+// sequence of 128 slots 9.0 / 10.6, of 256 10.6 / 11.0, of 384 12.2 / 11.6).
 PagedDecodePlan paged_decode_plan(const PagedView& c, int window, int sinks, bool acc) {
   const int64_t bh = (int64_t)c.batch * c.H;
   const int groups = most_groups(c, window, sinks);
@@ -348,6 +395,7 @@ PagedDecodePlan paged_decode_plan(const PagedView& c, int window, int sinks, boo
   if (S < per_bh(256)) S = per_bh(256);
   const int most_s = (groups + kPdWaves - 1) / kPdWaves;
   if (S > most_s) S = most_s;
+  if (groups <= 16) S = 1;
   PagedDecodePlan p;
   p.S = (int)(S < 1 ? 1 : S);
   p.part = ((size_t)c.batch * c.HQ * p.S * (c.D + 2) * 4 + 255) & ~(size_t)255;

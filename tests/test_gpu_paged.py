@@ -118,6 +118,9 @@ DECODE = [  # lens, H, G, d, page, dtype, window, sinks, rows first
     ([333, 18], 2, 2, 128, 16, "f32", 1, 0, False),
     ([333, 18], 2, 2, 128, 16, "bf16", 17, 300, False),
     ([9000], 1, 2, 64, 256, "bf16", 0, 0, False),
+    # more sequences and heads than it takes work-groups: not split
+    ([1100, 0, 5, 290] + [3] * 124, 8, 2, 64, 64, "bf16", 0, 0, False),
+    ([1300, 17, 450] + [20] * 125, 8, 5, 64, 16, "f32", 400, 5, False),
 ]
 
 
