@@ -309,6 +309,29 @@ struct Columns32 {
   }
   // Element of the head dimension that o[dt][e] holds.
   __device__ __forceinline__ int dim(int dt, int e) const { return 32 * dt + 8 * (e >> 2) + 4 * hh + (e & 3); }
+
+  // The closed state of this wave's columns to LDS (per column D + 2 floats), and the
+  // join with the state of another wave there.
+  __device__ __forceinline__ void give(float* sm) const {
+    float* mine = sm + n * (D + 2);
+    mine[0] = m;
+    mine[1] = l;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mine[2 + dim(dt, e)] = o[dt][e];
+  }
+  __device__ __forceinline__ void take(const float* sm) {
+    const float* other = sm + n * (D + 2);
+    const float m2 = other[0], mm = fmaxf(m, m2), ref = mm == -INFINITY ? 0.f : mm;
+    const float f1 = __builtin_amdgcn_exp2f(m - ref), f2 = __builtin_amdgcn_exp2f(m2 - ref);
+    m = mm;
+    l = l * f1 + other[1] * f2;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[dt][e] = o[dt][e] * f1 + other[2 + dim(dt, e)] * f2;
+  }
 };
 
 // Copies of a block of rows by direct global-to-LDS loads: row and byte (K's and V's
@@ -361,7 +384,9 @@ __device__ __forceinline__ void store_column(const PfArgs& a, const Columns32<TT
 
 // Many rows: a work-group of eight or four waves (pf_plan chooses) takes 256 or 128
 // packed rows, 32 a wave.  Tiles of 64 keys are copied into one of two LDS buffers
-// while the other is used; one barrier per tile.
+// while the other is used; one barrier per tile.  Prompts whose longest work-group
+// would outlast all others give 128 rows to four waves and four more, that go over
+// every other key tile with buffers of their own; the states meet in LDS.
 //
 // Bound by the matrix cores and the vector work of the softmax, which mostly add
 // up (the counters see them together in 28% of the matrix cores' busy cycles).
@@ -375,23 +400,27 @@ __device__ __forceinline__ void store_column(const PfArgs& a, const Columns32<TT
 // step by barriers (607), raised wave priority around the products (549 for 545).
 constexpr int kPf32Keys = 64;
 
-template <class TT, int D, int WAVES>
+// RW waves of rows, KW times (KW = 2: half the waves take every other key tile).
+template <class TT, int D, int RW, int KW>
 __device__ __forceinline__ void rows32(const PfArgs& a) {
-  constexpr int kPf32Rows = 32 * WAVES;
+  constexpr int ROWS = 32 * RW;
   constexpr int ES = elem_bytes<TT>();
   constexpr int HALF = kPf32Keys * D * 2;     // bytes of the K (or V) rows of a tile
-  constexpr int PER = HALF / 1024 / WAVES;    // copies per wave of each
+  constexpr int PER = HALF / 1024 / RW;       // copies per wave of each
   constexpr int DT = D / 32;
-  __shared__ __align__(1024) char smem[2 * 2 * HALF];
+  static_assert(KW == 1 || (KW == 2 && RW * 32 * (D + 2) * 4 <= KW * 4 * HALF), "states of the second half in LDS");
+  __shared__ __align__(1024) char smem_all[KW * 4 * HALF];
   const PrefillArgs& p = a.p;
   const int G = p.G;
   int bh, tile, split;
   if (!pf_item(a, &bh, &tile, &split)) return;
   const int b = bh / p.H, h = bh % p.H;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const Span<kPf32Keys> sp(p, b, tile * kPf32Rows, kPf32Rows);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int w = wave % RW, kw = wave / RW;
+  char* smem = smem_all + kw * 4 * HALF;
+  const Span<kPf32Keys> sp(p, b, tile * ROWS, ROWS);
   if (!sp.any) return;
-  const int i = tile * kPf32Rows + w * 32 + (lane & 31), r = i / G, j = h * G + i % G;
+  const int i = tile * ROWS + w * 32 + (lane & 31), r = i / G, j = h * G + i % G;
   const bool live = r < sp.nq;
   const int pos = live ? sp.shift + r : -1;
   const int per = (sp.n + a.S - 1) / a.S;
@@ -420,12 +449,13 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, dv, 16, in ? key * vstr + rc[q].vb : kOutOfRange, 0, 0, 0);
     }
   };
-  if (t0 < t1) copy(0, t0);
-  for (int t = t0; t < t1; ++t) {
-    const int u = (t - t0) & 1;
+  if (t0 + kw < t1) copy(0, t0 + kw);
+  int u = 0;
+  for (int t = t0 + kw; t - kw < t1; t += KW, u ^= 1) {
     wait_vmem<0>();
     lds_barrier();  // the tile is there, and every wave is done with the other buffer
-    if (t + 1 < t1) copy(u ^ 1, t + 1);
+    if (t + KW < t1) copy(u ^ 1, t + KW);
+    if (KW > 1 && t >= t1) continue;  // the last step's second half (the barriers are behind it)
     const char* kb = smem + u * 2 * HALF;
     const char* vb = kb + HALF;
     f32x16 x[2];
@@ -455,11 +485,19 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
       }
   }
   col.close();
+  if constexpr (KW > 1) {
+    __syncthreads();
+    float* sm = reinterpret_cast<float*>(smem_all) + w * 32 * (D + 2);
+    if (kw == 1) col.give(sm);
+    __syncthreads();
+    if (kw == 1) return;
+    col.take(sm);
+  }
   if (live) store_column(a, col, b, j, r, split);
 }
 
-template <class TT, int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void pf_rows32(PfArgs a) { rows32<TT, D, WAVES>(a); }
+template <class TT, int D, int RW, int KW>
+__global__ __launch_bounds__(64 * RW * KW, 2) void pf_rows32(PfArgs a) { rows32<TT, D, RW, KW>(a); }
 
 // Few rows, bf16: a work-group of two waves takes 32 packed rows, both waves the
 // same ones.  The waves go over the 32-key steps of the work-group's split in
@@ -552,26 +590,11 @@ __device__ __forceinline__ void few(const PfArgs& a) {
   col.close();
   __syncthreads();
   // wave 1 hands its state to wave 0
-  float* sm = reinterpret_cast<float*>(smem);  // [column][D + 2]
-  float* mine = sm + col.n * (D + 2);
-  if (w == 1) {
-    mine[0] = col.m;
-    mine[1] = col.l;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) mine[2 + col.dim(dt, e)] = col.o[dt][e];
-  }
+  float* sm = reinterpret_cast<float*>(smem);
+  if (w == 1) col.give(sm);
   __syncthreads();
   if (w == 1 || !live) return;
-  const float m2 = mine[0], mm = fmaxf(col.m, m2), ref = mm == -INFINITY ? 0.f : mm;
-  const float f1 = __builtin_amdgcn_exp2f(col.m - ref), f2 = __builtin_amdgcn_exp2f(m2 - ref);
-  col.m = mm;
-  col.l = col.l * f1 + mine[1] * f2;
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) col.o[dt][e] = col.o[dt][e] * f1 + mine[2 + col.dim(dt, e)] * f2;
+  col.take(sm);
   store_column(a, col, b, j, r, split);
 }
 
@@ -629,7 +652,7 @@ void launch_join(const PfArgs& a, hipStream_t s) {
   else hipLaunchKernelGGL((pf_join<T, D, false, 8>), one, dim3(256), 0, s, a);
 }
 
-enum PfKernel { kRows16, kRows32, kRows32Half, kFew };
+enum PfKernel { kRows16, kRows32, kRows32Half, kRows32Keys, kFew };
 
 struct PfPlan {
   PfKernel kernel;
@@ -644,16 +667,18 @@ struct PfPlan {
 // tiles, stores):
 //   pf_rows32, 8 waves  256 rows, 64 keys, 256 at a time: 1.9 us a tile (alone 1.78) + 6
 //   pf_rows32, 4 waves  128 rows, 64 keys, 512 at a time: 2.05 us (alone 1.5) + 5
+//   pf_rows32, 4 + 4    128 rows, 2 x 64 keys, 256 at a time: 2.05 us (alone 1.9) + 7
 //   pf_few              32 rows, 2 x 32 keys, 512 at a time: 1.3 us + 5
 //   pf_rows16           64 rows, 32 keys, 512 at a time: 2.2 us (alone 2.8) + 4
 // (less with d = 64, where four waves are better at every size: 8000 rows of 16 heads
 // 167 us, eight waves 186; 4 x 4000 rows behind a window of 1000 93, 112).  A
 // join is a launch (4 us), a round trip per 16 splits and the partial states there and
 // back at 4 TB/s.
-// Measured us, 8 waves / 4 waves / pf_few, in one piece: 500 rows of 28 heads 23 / 18 /
-// 16, 1000 rows of 32 heads 34 / 29 / 32, 1500 rows 48 / 43 / 60, 1900 rows over 5900
-// keys 173 / 170, 8192 rows 520 / 535; 2048 rows of 28 heads behind a window of 4096
-// 134 / 139, 3000 rows behind one of 500 56 / 45.
+// Measured us in one piece, 8 waves / 4 / 4 + 4 / pf_few: 500 rows of 28 heads 23 / 18 /
+// 16 / 16, 1000 rows of 32 heads 34 / 28 / 23 / 32, 1500 rows 48 / 41 / 34 / 60; without
+// pf_few, 3000 rows 95 / 87 / 100, 1900 rows over 5900 keys 173 / 164 / 168, 8192 rows 510
+// / 535 / 555, 2048 rows of 28 heads behind a window of 4096 131 / 139 / 143, 3000 rows
+// behind one of 500 56 / 44 / 53.
 PfPlan pf_plan(const PrefillArgs& a) {
   const int64_t packed = (int64_t)a.q_len * a.G, heads = (int64_t)a.batch * a.H;
   PfPlan best = {};
@@ -694,6 +719,7 @@ PfPlan pf_plan(const PrefillArgs& a) {
   } else {
     consider(kFew, kPfFewRows, 2 * kPfFewKeys, 512, d64 ? Cost{0.9, 0.9, 4} : Cost{1.3, 1.3, 5});
     consider(kRows32Half, 128, kPf32Keys, 512, d64 ? Cost{1.15, 0.9, 4} : Cost{2.05, 1.5, 5});
+    consider(kRows32Keys, 128, 2 * kPf32Keys, 256, d64 ? Cost{1.15, 1.1, 6} : Cost{2.05, 1.9, 7});
     if (!d64) consider(kRows32, 256, kPf32Keys, 256, Cost{1.9, 1.78, 6});
   }
   best.bytes = best.S > 1 ? (size_t)a.batch * a.HQ * a.q_len * best.S * (a.D + kStateHead) * 4 : 0;
@@ -715,10 +741,13 @@ hipError_t run_prefill(const PrefillArgs& p, char* ws, hipStream_t s) {
   const dim3 grid(pf_grid(a));
   const bool d64 = p.D == 64;
   if (pl.kernel == kRows32) {
-    hipLaunchKernelGGL((pf_rows32<BF16, 128, 8>), grid, dim3(512), 0, s, a);
+    hipLaunchKernelGGL((pf_rows32<BF16, 128, 8, 1>), grid, dim3(512), 0, s, a);
   } else if (pl.kernel == kRows32Half) {
-    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64, 4>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((pf_rows32<BF16, 128, 4>), grid, dim3(256), 0, s, a);
+    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64, 4, 1>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((pf_rows32<BF16, 128, 4, 1>), grid, dim3(256), 0, s, a);
+  } else if (pl.kernel == kRows32Keys) {
+    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64, 4, 2>), grid, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((pf_rows32<BF16, 128, 4, 2>), grid, dim3(512), 0, s, a);
   } else if (pl.kernel == kFew) {
     if (d64) hipLaunchKernelGGL((pf_few<BF16, 64>), grid, dim3(kPfFewThreads), 0, s, a);
     else hipLaunchKernelGGL((pf_few<BF16, 128>), grid, dim3(kPfFewThreads), 0, s, a);
