@@ -697,9 +697,10 @@ PfPlan pf_plan(const PrefillArgs& a) {
     const double read = heads * most * 2 * a.D * a.esize / 4.5e6;
     for (int S = 1; S <= 64 && (S == 1 || most / S >= 64); ++S) {
       const double longest = ceil(most / keys / S) * c.alone + c.besides;
-      // behind a window all work-groups are alike and run in whole rounds
+      // behind a window all work-groups are alike and run in whole rounds; so do short
+      // ones, that have not much of a longest (pf_few)
       double rounds = (double)groups * S / at_a_time;
-      if (a.window > 0) rounds = ceil(rounds);
+      if (a.window > 0 || kernel == kFew) rounds = ceil(rounds);
       const double all = rounds * (mean / keys / S * c.busy + c.besides);
       double t = longest > all ? longest : all;
       if (t < read) t = read;
