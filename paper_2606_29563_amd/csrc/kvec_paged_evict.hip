@@ -111,12 +111,14 @@ typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 // Bound by latency: page entries, then weights and positions, then three passes with a
-// sum over the threads each (1088 slots: 7 us; 4 x 24571 slots of 8 heads: 18, of which
-// the keys take 5, a pass 2 and the lists 5).  The loads of EB quads of slots of a
+// sum over the threads each (1088 slots: 7 us with the moves; 4 x 24571 slots of 8 heads:
+// 16.5, of which the keys take 5, a pass 2 and the lists 5).  The loads of EB quads of slots of a
 // thread are in flight at once (slot by slot 2 us more for 24k slots; 6 or 8 instead of
 // 3 no different).  Keys lie in LDS, those of sequences of one tile for all passes;
 // longer ones make them again in each.  Keys counted as they are made, LDS read four at
-// a time and once for both lists, and sums by register shifts took it from 23 to 18.
+// a time and once for both lists, and sums by register shifts took it from 23 to 18;
+// no further pass when every key that shares the digits found is kept (mostly so after
+// the second) to 16.5.
 // MOVE: bytes of a K or V row, moved by this launch (0: by the second).
 template <int CAP, int EB, int MOVE>
 __global__ __launch_bounds__(kEvThreads) void ev_select(EvArgs a) {
@@ -124,7 +126,7 @@ __global__ __launch_bounds__(kEvThreads) void ev_select(EvArgs a) {
   __shared__ __align__(16) uint32_t keys[CAP];
   __shared__ uint32_t hist[2][kEvBins];
   __shared__ __align__(16) int tmp[2][kEvWaves];
-  __shared__ uint32_t found[3][2];
+  __shared__ uint32_t found[3][3];
   const int h = blockIdx.x, b = blockIdx.y, H = a.c.H, B = a.B, tid = threadIdx.x;
   const int n = min(max(a.c.lens[b], 0), a.c.max_len);
   const int64_t bh = (int64_t)b * H + h;
@@ -212,13 +214,18 @@ __global__ __launch_bounds__(kEvThreads) void ev_select(EvArgs a) {
       const bool upper = need <= before + c0;
       found[pass][0] = (uint32_t)(upper ? top : top - 1);
       found[pass][1] = (uint32_t)(need - before - (upper ? 0 : c0));
+      found[pass][2] = (uint32_t)(upper ? c0 : c1);
     }
     __syncthreads();
     prefix |= found[pass][0] << shift;
     mask |= digits << shift;
     need = (int)found[pass][1];
+    if (need == (int)found[pass][2]) {  // all that share the prefix are kept: its lowest key is the cut
+      need = n;
+      break;
+    }
   }
-  const uint32_t cut = prefix;  // the B-th largest key; the `need` lowest slots that have it are kept
+  const uint32_t cut = prefix;  // the B-th largest key or less; the `need` lowest slots that have it are kept
 
   // Thread t goes over the t-th run of a tile's quads; an odd number of them, so that
   // the threads' reads fall in distinct banks.
@@ -342,8 +349,8 @@ hipError_t run_paged_evict(const PagedView& c, int budget, int window, int sinks
   const dim3 grid(c.H, c.batch);
   const int row = c.D * c.esize;
   // One launch where a work-group has few rows to move and no other reads what this one
-  // writes: the lengths, unless they are replaced in place.  us with one launch / two, 8
-  // heads with rows of 256 bytes and 1024 kept: of 1088 slots 9.9 / 12.3, of 1280 11.8 /
+  // writes: the lengths, unless they are replaced in place.  us with one launch / two, a
+  // pass more in each, 8 heads with rows of 256 bytes and 1024 kept: of 1088 slots 9.9 / 12.3, of 1280 11.8 /
   // 12.3, of 1536 13.7 / 12.5; 32 sequences of 1280 14.1 / 15.8.
   auto apart = [&](const int32_t* in) { return lens_out + c.batch <= in || in + c.batch <= lens_out; };
   if (c.max_len <= kEvSmall && (int64_t)a.cap * row <= kEvMoveBytes && apart(c.lens) && apart(n_seen)) {
