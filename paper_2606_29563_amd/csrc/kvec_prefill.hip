@@ -385,8 +385,9 @@ __device__ __forceinline__ void store_column(const PfArgs& a, const Columns32<TT
 // Many rows: a work-group of eight or four waves (pf_plan chooses) takes 256 or 128
 // packed rows, 32 a wave.  Tiles of 64 keys are copied into one of two LDS buffers
 // while the other is used; one barrier per tile.  Prompts whose longest work-group
-// would outlast all others give 128 rows to four waves and four more, that go over
-// every other key tile with buffers of their own; the states meet in LDS.
+// would outlast all others divide its keys over waves too: 128 rows are given to four
+// waves and four more, that go over every other key tile with buffers of their own, or 64
+// rows to four times two waves and every fourth tile of 32 keys; the states meet in LDS.
 //
 // Bound by the matrix cores and the vector work of the softmax, which mostly add
 // up (the counters see them together in 28% of the matrix cores' busy cycles).
@@ -400,15 +401,15 @@ __device__ __forceinline__ void store_column(const PfArgs& a, const Columns32<TT
 // step by barriers (607), raised wave priority around the products (549 for 545).
 constexpr int kPf32Keys = 64;
 
-// RW waves of rows, KW times (KW = 2: half the waves take every other key tile).
-template <class TT, int D, int RW, int KW>
+// RW waves of rows, KW times; the k-th of the KW takes every KW-th tile of KT keys.
+template <class TT, int D, int RW, int KW, int KT>
 __device__ __forceinline__ void rows32(const PfArgs& a) {
   constexpr int ROWS = 32 * RW;
   constexpr int ES = elem_bytes<TT>();
-  constexpr int HALF = kPf32Keys * D * 2;     // bytes of the K (or V) rows of a tile
+  constexpr int HALF = KT * D * 2;            // bytes of the K (or V) rows of a tile
   constexpr int PER = HALF / 1024 / RW;       // copies per wave of each
   constexpr int DT = D / 32;
-  static_assert(KW == 1 || (KW == 2 && RW * 32 * (D + 2) * 4 <= KW * 4 * HALF), "states of the second half in LDS");
+  static_assert((KW - 1) * RW * 32 * (D + 2) * 4 <= KW * 4 * HALF, "states in LDS");
   __shared__ __align__(1024) char smem_all[KW * 4 * HALF];
   const PrefillArgs& p = a.p;
   const int G = p.G;
@@ -418,7 +419,7 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int w = wave % RW, kw = wave / RW;
   char* smem = smem_all + kw * 4 * HALF;
-  const Span<kPf32Keys> sp(p, b, tile * ROWS, ROWS);
+  const Span<KT> sp(p, b, tile * ROWS, ROWS);
   if (!sp.any) return;
   const int i = tile * ROWS + w * 32 + (lane & 31), r = i / G, j = h * G + i % G;
   const bool live = r < sp.nq;
@@ -455,26 +456,26 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
     wait_vmem<0>();
     lds_barrier();  // the tile is there, and every wave is done with the other buffer
     if (t + KW < t1) copy(u ^ 1, t + KW);
-    if (KW > 1 && t >= t1) continue;  // the last step's second half (the barriers are behind it)
+    if (KW > 1 && t >= t1) continue;  // behind the last tile (this step's barrier is passed)
     const char* kb = smem + u * 2 * HALF;
     const char* vb = kb + HALF;
-    f32x16 x[2];
+    f32x16 x[KT / 32];
     col.logits(x, kb);
     const int key0 = sp.key0(t);
     if (!sp.open(key0)) {
 #pragma unroll
-      for (int g = 0; g < 2; ++g)
+      for (int g = 0; g < KT / 32; ++g)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
           if (!sp.sees(key0 + col.key(g, e), pos)) x[g][e] = -INFINITY;
     }
-    bf16x8 pf[4];
-    col.template weigh<2, false>(x, a.sc, pf, pf);
+    bf16x8 pf[KT / 16];
+    col.template weigh<KT / 32, false>(x, a.sc, pf, pf);
     // (the compiler's transposing read waits for the copies in flight, which were
     // issued half a tile before; written out with waits of its own it was slower, 566
     // us for 545, because then the products cannot be scheduled between the reads)
 #pragma unroll
-    for (int ss = 0; ss < 4; ++ss)
+    for (int ss = 0; ss < KT / 16; ++ss)
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -488,18 +489,19 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
   if constexpr (KW > 1) {
     __syncthreads();
     float* sm = reinterpret_cast<float*>(smem_all) + w * 32 * (D + 2);
-    if (kw == 1) col.give(sm);
+    if (kw > 0) col.give(sm + (kw - 1) * RW * 32 * (D + 2));
     __syncthreads();
-    if (kw == 1) return;
-    col.take(sm);
+    if (kw > 0) return;
+#pragma unroll
+    for (int i = 0; i < KW - 1; ++i) col.take(sm + i * RW * 32 * (D + 2));
   }
   if (live) store_column(a, col, b, j, r, split);
 }
 
-template <class TT, int D, int RW, int KW>
-__global__ __launch_bounds__(64 * RW * KW, 2) void pf_rows32(PfArgs a) { rows32<TT, D, RW, KW>(a); }
+template <class TT, int D, int RW, int KW, int KT>
+__global__ __launch_bounds__(64 * RW * KW, 2) void pf_rows32(PfArgs a) { rows32<TT, D, RW, KW, KT>(a); }
 
-// Few rows, bf16: a work-group of two waves takes 32 packed rows, both waves the
+// Few rows, bf16, d = 128: a work-group of two waves takes 32 packed rows, both waves the
 // same ones.  The waves go over the 32-key steps of the work-group's split in
 // turn, each with an LDS ring of two steps of its own and no barrier before the
 // end, where their states are joined.  What bounds it is the latency and the reading
@@ -652,7 +654,7 @@ void launch_join(const PfArgs& a, hipStream_t s) {
   else hipLaunchKernelGGL((pf_join<T, D, false, 8>), one, dim3(256), 0, s, a);
 }
 
-enum PfKernel { kRows16, kRows32, kRows32Half, kRows32Keys, kFew };
+enum PfKernel { kRows16, kRows32, kRows32Half, kRows32Keys, kRows32Keys4, kFew };
 
 struct PfPlan {
   PfKernel kernel;
@@ -665,20 +667,22 @@ struct PfPlan {
 //     + what the join costs,
 // a work-group taking so long per key tile and so long besides (first loads, masked
 // tiles, stores):
-//   pf_rows32, 8 waves  256 rows, 64 keys, 256 at a time: 1.9 us a tile (alone 1.78) + 6
+//   pf_rows32, 8 waves  256 rows, 64 keys, 256 at a time: 1.9 us a tile (alone 1.85) + 6
 //   pf_rows32, 4 waves  128 rows, 64 keys, 512 at a time: 2.05 us (alone 1.5) + 5
 //   pf_rows32, 4 + 4    128 rows, 2 x 64 keys, 256 at a time: 2.05 us (alone 1.9) + 7
+//   pf_rows32, 4 x 2    64 rows, 4 x 32 keys, 256 at a time: 1.8 us (alone 1.45) + 7.5
 //   pf_few              32 rows, 2 x 32 keys, 512 at a time: 1.3 us + 5
 //   pf_rows16           64 rows, 32 keys, 512 at a time: 2.2 us (alone 2.8) + 4
-// (less with d = 64, where four waves are better at every size: 8000 rows of 16 heads
-// 167 us, eight waves 186; 4 x 4000 rows behind a window of 1000 93, 112).  A
-// join is a launch (4 us), a round trip per 16 splits and the partial states there and
-// back at 4 TB/s.
-// Measured us in one piece, 8 waves / 4 / 4 + 4 / pf_few: 500 rows of 28 heads 23 / 18 /
-// 16 / 16, 1000 rows of 32 heads 34 / 28 / 23 / 32, 1500 rows 48 / 41 / 34 / 60; without
-// pf_few, 3000 rows 95 / 87 / 100, 1900 rows over 5900 keys 173 / 164 / 168, 8192 rows 510
-// / 535 / 555, 2048 rows of 28 heads behind a window of 4096 131 / 139 / 143, 3000 rows
-// behind one of 500 56 / 44 / 53.
+// (d = 64: four waves, 4 + 4 and, 512 at a time, 4 x 2, which is as good as pf_few on few
+// rows).  A join is a launch (4 us), a round trip per 16 splits and the partial states
+// there and back at 4 TB/s.
+// Measured us in one piece, 8 waves / 4 / 4 + 4 / 4 x 2 / pf_few: 250 rows of 32 heads - /
+// - / 12 / 11 / 10.5, 500 rows of 28 heads 23 / 18 / 16 / 14 / 16, 1000 rows of 32 34 / 28
+// / 24 / 27 / 32, 1500 rows 48 / 41 / 35 / 48 / 60, 8192 rows 510 / 535 / 555 / 702 / -;
+// 3000 rows 95 / 87 / 100 / 128, 1900 rows over 5900 keys 173 / 164 / 168 / -, 500 over 2000
+// - / - / 34 / 27, 2048 rows of 28 heads behind a window of 4096 131 / 139 / 143 / -, 3000
+// behind one of 500 56 / 44 / 53 / -; d 64, 16 heads, 4 / 4 + 4 / 4 x 2: 1000 rows 19 / 15 / 12,
+// 1500 rows - / 20 / 16, 4000 rows 61 / 52 / 53, 8000 rows 150 / 172 / 176.
 PfPlan pf_plan(const PrefillArgs& a) {
   const int64_t packed = (int64_t)a.q_len * a.G, heads = (int64_t)a.batch * a.H;
   PfPlan best = {};
@@ -696,16 +700,21 @@ PfPlan pf_plan(const PrefillArgs& a) {
     const double state = 2.0 * a.batch * a.HQ * a.q_len * (a.D + kStateHead) * 4 / 4e6;  // us per split
     const double read = heads * most * 2 * a.D * a.esize / 4.5e6;
     for (int S = 1; S <= 64 && (S == 1 || most / S >= 64); ++S) {
-      const double longest = ceil(most / keys / S) * c.alone + c.besides;
+      // more than one a compute unit: the longest shares it with the 257th, as long as
+      // that lasts (lengths fall evenly from the longest to twice the mean less that)
+      const double all_groups = (double)groups * S;
+      const double company = all_groups > 256 ? fmax(1 - 256 / all_groups * 2 * (1 - mean / most), 0) : 0;
+      const double longest = ceil(most / keys / S) * (c.alone + fmax(c.busy - c.alone, 0) * company) + c.besides;
       // behind a window all work-groups are alike and run in whole rounds; so do short
-      // ones, that have not much of a longest (pf_few)
-      double rounds = (double)groups * S / at_a_time;
-      if (a.window > 0 || kernel == kFew) rounds = ceil(rounds);
+      // ones, whose keys are divided over waves
+      double rounds = all_groups / at_a_time;
+      if (rounds > 1 && (a.window > 0 || kernel == kFew || kernel == kRows32Keys || kernel == kRows32Keys4)) rounds = ceil(rounds);
       const double all = rounds * (mean / keys / S * c.busy + c.besides);
       double t = longest > all ? longest : all;
       if (t < read) t = read;
       if (S > 1) t += 4.0 + 0.7 * ((S + 15) / 16) + S * state;
-      if (best.S == 0 || t < least) {
+      // (pf_few's probabilities are more exact: taken unless another is clearly faster)
+      if (best.S == 0 || t < least * (best.kernel == kFew && kernel != kFew ? 0.95 : 1.0)) {
         least = t;
         best.kernel = kernel;
         best.S = S;
@@ -717,11 +726,16 @@ PfPlan pf_plan(const PrefillArgs& a) {
   const bool d64 = a.D == 64;
   if (a.esize == 4) {
     consider(kRows16, kPfRows, kPfKeys, 512, Cost{2.2, 2.8, 4});
+  } else if (d64) {
+    consider(kRows32Half, 128, kPf32Keys, 512, Cost{1.15, 0.9, 4});
+    consider(kRows32Keys, 128, 2 * kPf32Keys, 256, Cost{1.15, 0.85, 5.5});
+    consider(kRows32Keys4, 64, 4 * 32, 512, Cost{1.15, 0.7, 4.3});
   } else {
-    consider(kFew, kPfFewRows, 2 * kPfFewKeys, 512, d64 ? Cost{0.9, 0.9, 4} : Cost{1.3, 1.3, 5});
-    consider(kRows32Half, 128, kPf32Keys, 512, d64 ? Cost{1.15, 0.9, 4} : Cost{2.05, 1.5, 5});
-    consider(kRows32Keys, 128, 2 * kPf32Keys, 256, d64 ? Cost{1.15, 1.1, 6} : Cost{2.05, 1.9, 7});
-    if (!d64) consider(kRows32, 256, kPf32Keys, 256, Cost{1.9, 1.78, 6});
+    consider(kFew, kPfFewRows, 2 * kPfFewKeys, 512, Cost{1.3, 1.3, 5});
+    consider(kRows32Half, 128, kPf32Keys, 512, Cost{2.05, 1.5, 5});
+    consider(kRows32Keys, 128, 2 * kPf32Keys, 256, Cost{2.05, 1.9, 7});
+    consider(kRows32Keys4, 64, 4 * 32, 256, Cost{1.8, 1.45, 7.5});
+    consider(kRows32, 256, kPf32Keys, 256, Cost{1.9, 1.85, 6});
   }
   best.bytes = best.S > 1 ? (size_t)a.batch * a.HQ * a.q_len * best.S * (a.D + kStateHead) * 4 : 0;
   return best;
@@ -742,16 +756,18 @@ hipError_t run_prefill(const PrefillArgs& p, char* ws, hipStream_t s) {
   const dim3 grid(pf_grid(a));
   const bool d64 = p.D == 64;
   if (pl.kernel == kRows32) {
-    hipLaunchKernelGGL((pf_rows32<BF16, 128, 8, 1>), grid, dim3(512), 0, s, a);
+    hipLaunchKernelGGL((pf_rows32<BF16, 128, 8, 1, 64>), grid, dim3(512), 0, s, a);
   } else if (pl.kernel == kRows32Half) {
-    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64, 4, 1>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((pf_rows32<BF16, 128, 4, 1>), grid, dim3(256), 0, s, a);
+    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64, 4, 1, 64>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((pf_rows32<BF16, 128, 4, 1, 64>), grid, dim3(256), 0, s, a);
   } else if (pl.kernel == kRows32Keys) {
-    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64, 4, 2>), grid, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((pf_rows32<BF16, 128, 4, 2>), grid, dim3(512), 0, s, a);
+    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64, 4, 2, 64>), grid, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((pf_rows32<BF16, 128, 4, 2, 64>), grid, dim3(512), 0, s, a);
+  } else if (pl.kernel == kRows32Keys4) {
+    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64, 2, 4, 32>), grid, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((pf_rows32<BF16, 128, 2, 4, 32>), grid, dim3(512), 0, s, a);
   } else if (pl.kernel == kFew) {
-    if (d64) hipLaunchKernelGGL((pf_few<BF16, 64>), grid, dim3(kPfFewThreads), 0, s, a);
-    else hipLaunchKernelGGL((pf_few<BF16, 128>), grid, dim3(kPfFewThreads), 0, s, a);
+    hipLaunchKernelGGL((pf_few<BF16, 128>), grid, dim3(kPfFewThreads), 0, s, a);
   } else {
     if (d64) hipLaunchKernelGGL(pf_rows16<64>, grid, dim3(kPfThreads), 0, s, a);
     else hipLaunchKernelGGL(pf_rows16<128>, grid, dim3(kPfThreads), 0, s, a);

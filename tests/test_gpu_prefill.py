@@ -119,10 +119,13 @@ LONG = [  # b, H, G, d, q rows, keys, dtype, window, sinks, q_lens, kv_lens
     (1, 8, 4, 128, 500, 7001, "bf16", 0, 0, None, None),
     (1, 1, 8, 128, 2000, 30001, "bf16", 0, 0, None, None),
     (1, 4, 7, 128, 500, 8003, "bf16", 0, 0, None, None),
-    # work-groups of four waves, with and without a second half on the other key tiles
+    # work-groups of four waves, alone or with the keys divided over several times as many
     (2, 4, 7, 128, 900, 900, "bf16", 100, 0, None, [900, 450]),
     (1, 8, 4, 128, 900, 2900, "bf16", 700, 10, None, None),
     (4, 8, 2, 64, 300, 1300, "bf16", 0, 0, [300, 1, 0, 299], [1300, 1290, 700, 0]),
+    (2, 1, 8, 128, 300, 1501, "bf16", 0, 0, [300, 171], [1501, 1500]),
+    (1, 3, 8, 64, 900, 900, "bf16", 0, 0, None, None),
+    (1, 8, 4, 64, 200, 300, "bf16", 0, 0, None, None),
 ]
 
 
