@@ -121,6 +121,10 @@ DECODE = [  # lens, H, G, d, page, dtype, window, sinks, rows first
     # more sequences and heads than it takes work-groups: not split
     ([1100, 0, 5, 290] + [3] * 124, 8, 2, 64, 64, "bf16", 0, 0, False),
     ([1300, 17, 450] + [20] * 125, 8, 5, 64, 16, "f32", 400, 5, False),
+    # many sequences, many heads, a page that holds a whole sequence
+    ([i % 40 for i in range(500)], 1, 1, 64, 16, "bf16", 0, 0, False),
+    ([33, 290], 256, 1, 64, 16, "bf16", 0, 0, False),
+    ([1999, 2048], 2, 3, 128, 2048, "bf16", 0, 0, False),
 ]
 
 
@@ -381,6 +385,9 @@ EVICT = [  # lens, H, d, page, dtype, budget, window, sinks, rows first
     ([4096, 4095], 2, 64, 256, "bf16", 1, 0, 1, False),
     ([5000, 3000, 10], 2, 64, 128, "bf16", 2999, 100, 16, False),
     ([33000], 1, 64, 1024, "bf16", 3001, 8, 8, False),
+    ([i % 50 for i in range(400)], 2, 64, 16, "bf16", 20, 5, 3, False),
+    ([60, 41], 200, 64, 16, "f32", 40, 40, 0, True),
+    ([4097, 4096, 4099], 1, 128, 2048, "bf16", 4096, 10, 10, False),
 ]
 
 

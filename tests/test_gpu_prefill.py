@@ -85,6 +85,10 @@ CASES = [  # b, H, G, d, q rows, keys, dtype, window, sinks, q_lens, kv_lens, la
     (1, 1, 2, 128, 5, 1200, "f32", 0, 0, None, None, "bhtd"),
     (1, 1, 2, 64, 4, 4000, "bf16", 1500, 9, None, None, "bhtd"),
     (2, 1, 2, 64, 4, 2000, "bf16", 0, 0, [4, 2], [1, 2000], "bhtd"),
+    # many sequences, many heads
+    (300, 2, 1, 64, 3, 9, "bf16", 0, 0, None, None, "bhtd"),
+    (1, 160, 1, 128, 20, 33, "bf16", 5, 2, None, None, "bthd"),
+    (1, 96, 2, 64, 20, 33, "f32", 0, 0, None, None, "bhtd"),
 ]
 
 
