@@ -262,6 +262,9 @@ APPEND = [  # tokens, H, G, d, page, dtype, rot, norm, start
     (37, 1, 16, 64, 16, "f32", 16, True, 1000000),
     (1030, 2, 1, 128, 256, "f32", 128, False, 5),
     (1031, 1, 3, 64, 16, "bf16", 48, True, 100),
+    # several tokens a work-group, the last one with fewer
+    (1537, 2, 1, 128, 256, "f32", 128, False, 5),
+    (1551, 1, 3, 64, 16, "bf16", 48, True, 100),
     (3, 2, 2, 128, 16, "f32", 112, True, -5),
     (4, 2, 2, 64, 16, "bf16", 0, True, 0),
     (4, 2, 2, 64, 16, "f32", 0, False, 0),
