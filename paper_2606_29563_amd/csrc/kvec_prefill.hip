@@ -89,23 +89,27 @@ constexpr int kPfRows = 64;  // packed rows per work-group, 16 per wave
 constexpr int kPfKeys = 32;
 
 // float32: a work-group of four waves takes 64 packed rows, 16 a wave (Columns16), on
-// the 16x16x4 f32 product; tiles of 32 keys in two LDS buffers.  Bound by that
+// the 16x16x4 f32 product; tiles of 32 keys in two LDS buffers.  With KW = 2 four more
+// waves take every other tile, and the states meet in LDS.  Bound by that
 // product's rate (a sixteenth of the bf16 one's) and the softmax between two products:
 // 4000 rows of 8 query and 4 KV heads, d 64, in 186 us, 88 TFLOP/s of 153.
-template <int D>
-__global__ __launch_bounds__(kPfThreads) void pf_rows16(PfArgs a) {
+template <int D, int KW>
+__global__ __launch_bounds__(kPfThreads * KW) void pf_rows16(PfArgs a) {
   using TT = F32;
   using RG = RowGroup<TT, D>;
   constexpr int ES = RG::ES, GRPS = kPfKeys / 16;
   constexpr int BUF = 2 * GRPS * RG::BYTES;       // K groups, then V groups
   constexpr int PER = 2 * GRPS * RG::NI / 4;      // copies per wave and tile
-  __shared__ __align__(1024) char smem[2 * BUF];
+  static_assert((KW - 1) * kPfRows * (D + 2) * 4 <= KW * 2 * BUF, "states in LDS");
+  __shared__ __align__(1024) char smem_all[KW * 2 * BUF];
   const PrefillArgs& p = a.p;
   const int G = p.G;
   int bh, tile, split;
   if (!pf_item(a, &bh, &tile, &split)) return;
   const int b = bh / p.H, h = bh % p.H;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int w = wave % 4, kw = wave / 4;
+  char* smem = smem_all + kw * 2 * BUF;
   const int n = lane & 15, c = lane >> 4;
   const Span<kPfKeys> sp(p, b, tile * kPfRows, kPfRows);
   if (!sp.any) return;
@@ -140,12 +144,13 @@ __global__ __launch_bounds__(kPfThreads) void pf_rows16(PfArgs a) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(is_v ? vr : kr, dst, 16, off, 0, 0, 0);
     }
   };
-  if (t0 < t1) copy(0, t0);
-  for (int t = t0; t < t1; ++t) {
-    const int u = (t - t0) & 1;
+  if (t0 + kw < t1) copy(0, t0 + kw);
+  int u = 0;
+  for (int t = t0 + kw; t - kw < t1; t += KW, u ^= 1) {
     wait_vmem<0>();
     lds_barrier();  // the tile is there, and every wave is done with the other buffer
-    if (t + 1 < t1) copy(u ^ 1, t + 1);
+    if (t + KW < t1) copy(u ^ 1, t + KW);
+    if (KW > 1 && t >= t1) continue;  // behind the last tile (this step's barrier is passed)
     const char* kb = smem + u * BUF;
     const int key0 = sp.key0(t);
     f32x4 x[GRPS];
@@ -162,6 +167,34 @@ __global__ __launch_bounds__(kPfThreads) void pf_rows16(PfArgs a) {
     col.absorb(x, kb + GRPS * RG::BYTES, lane);
   }
   col.l = col_sum4(col.l);
+  if constexpr (KW > 1) {
+    __syncthreads();
+    float* sm = reinterpret_cast<float*>(smem_all) + (w * 16 + n) * (D + 2);
+    constexpr int NEXT = kPfRows * (D + 2);
+    if (kw > 0) {
+      float* mine = sm + (kw - 1) * NEXT;
+      mine[0] = col.m;
+      mine[1] = col.l;
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mine[2 + 16 * t + 4 * c + e] = col.o[t][e];
+    }
+    __syncthreads();
+    if (kw > 0) return;
+#pragma unroll
+    for (int k = 0; k < KW - 1; ++k) {
+      const float* other = sm + k * NEXT;
+      const float mm = fmaxf(col.m, other[0]), ref = mm == -INFINITY ? 0.f : mm;
+      const float f1 = __builtin_amdgcn_exp2f(col.m - ref), f2 = __builtin_amdgcn_exp2f(other[0] - ref);
+      col.m = mm;
+      col.l = col.l * f1 + other[1] * f2;
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) col.o[t][e] = col.o[t][e] * f1 + other[2 + 16 * t + 4 * c + e] * f2;
+    }
+  }
   if (!live) return;
   const int64_t row = ((int64_t)b * p.HQ + j) * p.q_len + r;
   if (a.S > 1) {
@@ -654,7 +687,7 @@ void launch_join(const PfArgs& a, hipStream_t s) {
   else hipLaunchKernelGGL((pf_join<T, D, false, 8>), one, dim3(256), 0, s, a);
 }
 
-enum PfKernel { kRows16, kRows32, kRows32Half, kRows32Keys, kRows32Keys4, kFew };
+enum PfKernel { kRows16, kRows16Keys, kRows32, kRows32Half, kRows32Keys, kRows32Keys4, kFew };
 
 struct PfPlan {
   PfKernel kernel;
@@ -672,8 +705,9 @@ struct PfPlan {
 //   pf_rows32, 4 + 4    128 rows, 2 x 64 keys, 256 at a time: 2.05 us (alone 1.9) + 7
 //   pf_rows32, 4 x 2    64 rows, 4 x 32 keys, 256 at a time: 1.8 us (alone 1.45) + 7.5
 //   pf_few              32 rows, 2 x 32 keys, 512 at a time: 1.3 us + 5
-//   pf_rows16           64 rows, 32 keys, 512 at a time: 2.2 us (alone 2.8) + 4
-// (d = 64: four waves, 4 + 4 and, 512 at a time, 4 x 2, which is as good as pf_few on few
+//   pf_rows16           64 rows, 32 keys, 512 at a time: 4.8 us (alone 3.2) + 3
+//   pf_rows16, 4 + 4    64 rows, 2 x 32 keys, 256 at a time: 5.2 us + 4
+// (d = 64: half of pf_rows16's; four waves, 4 + 4 and, 512 at a time, 4 x 2, which is as good as pf_few on few
 // rows).  A join is a launch (4 us), a round trip per 16 splits and the partial states
 // there and back at 4 TB/s.
 // Measured us in one piece, 8 waves / 4 / 4 + 4 / 4 x 2 / pf_few: 250 rows of 32 heads - /
@@ -683,6 +717,8 @@ struct PfPlan {
 // - / - / 34 / 27, 2048 rows of 28 heads behind a window of 4096 131 / 139 / 143 / -, 3000
 // behind one of 500 56 / 44 / 53 / -; d 64, 16 heads, 4 / 4 + 4 / 4 x 2: 1000 rows 19 / 15 / 12,
 // 1500 rows - / 20 / 16, 4000 rows 61 / 52 / 53, 8000 rows 150 / 172 / 176.
+// float32, pf_rows16 / 4 + 4: 1000 rows of 32 heads, d 128, 115 / 98, 2000 rows 338 / 336;
+// d 64, 1500 rows of 8 heads behind a window of 200 22 / 16, 1000 rows in splits 26 / 28.
 PfPlan pf_plan(const PrefillArgs& a) {
   const int64_t packed = (int64_t)a.q_len * a.G, heads = (int64_t)a.batch * a.H;
   PfPlan best = {};
@@ -691,6 +727,7 @@ PfPlan pf_plan(const PrefillArgs& a) {
     double busy, alone, besides;  // us of a tile among others and alone, us besides
   };
   auto consider = [&](PfKernel kernel, int rows, int keys, int at_a_time, Cost c) {
+    const bool shared = kernel == kFew || kernel == kRows32Keys || kernel == kRows32Keys4;
     const int64_t tiles = (packed + rows - 1) / rows, groups = tiles * heads;
     // keys that a row tile sees at most, and on average
     double most = a.kv_len, mean = a.kv_len - 0.5 * (a.q_len < a.kv_len ? a.q_len : a.kv_len);
@@ -705,10 +742,10 @@ PfPlan pf_plan(const PrefillArgs& a) {
       const double all_groups = (double)groups * S;
       const double company = all_groups > 256 ? fmax(1 - 256 / all_groups * 2 * (1 - mean / most), 0) : 0;
       const double longest = ceil(most / keys / S) * (c.alone + fmax(c.busy - c.alone, 0) * company) + c.besides;
-      // behind a window all work-groups are alike and run in whole rounds; so do short
-      // ones, whose keys are divided over waves
+      // behind a window, and where the rows are few for their keys, all work-groups are
+      // alike and run in whole rounds; so do short ones, whose keys are divided over waves
       double rounds = all_groups / at_a_time;
-      if (rounds > 1 && (a.window > 0 || kernel == kFew || kernel == kRows32Keys || kernel == kRows32Keys4)) rounds = ceil(rounds);
+      if (rounds > 1 && (a.window > 0 || mean > 0.75 * most || shared)) rounds = ceil(rounds);
       const double all = rounds * (mean / keys / S * c.busy + c.besides);
       double t = longest > all ? longest : all;
       if (t < read) t = read;
@@ -725,7 +762,8 @@ PfPlan pf_plan(const PrefillArgs& a) {
   };
   const bool d64 = a.D == 64;
   if (a.esize == 4) {
-    consider(kRows16, kPfRows, kPfKeys, 512, Cost{2.2, 2.8, 4});
+    consider(kRows16, kPfRows, kPfKeys, 512, d64 ? Cost{2.3, 1.6, 3} : Cost{4.8, 3.2, 3});
+    consider(kRows16Keys, kPfRows, 2 * kPfKeys, d64 ? 512 : 256, d64 ? Cost{4.6, 2.7, 4.5} : Cost{5.2, 5.2, 4});
   } else if (d64) {
     consider(kRows32Half, 128, kPf32Keys, 512, Cost{1.15, 0.9, 4});
     consider(kRows32Keys, 128, 2 * kPf32Keys, 256, Cost{1.15, 0.85, 5.5});
@@ -766,11 +804,14 @@ hipError_t run_prefill(const PrefillArgs& p, char* ws, hipStream_t s) {
   } else if (pl.kernel == kRows32Keys4) {
     if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64, 2, 4, 32>), grid, dim3(512), 0, s, a);
     else hipLaunchKernelGGL((pf_rows32<BF16, 128, 2, 4, 32>), grid, dim3(512), 0, s, a);
+  } else if (pl.kernel == kRows16Keys) {
+    if (d64) hipLaunchKernelGGL((pf_rows16<64, 2>), grid, dim3(2 * kPfThreads), 0, s, a);
+    else hipLaunchKernelGGL((pf_rows16<128, 2>), grid, dim3(2 * kPfThreads), 0, s, a);
   } else if (pl.kernel == kFew) {
     hipLaunchKernelGGL((pf_few<BF16, 128>), grid, dim3(kPfFewThreads), 0, s, a);
   } else {
-    if (d64) hipLaunchKernelGGL(pf_rows16<64>, grid, dim3(kPfThreads), 0, s, a);
-    else hipLaunchKernelGGL(pf_rows16<128>, grid, dim3(kPfThreads), 0, s, a);
+    if (d64) hipLaunchKernelGGL((pf_rows16<64, 1>), grid, dim3(kPfThreads), 0, s, a);
+    else hipLaunchKernelGGL((pf_rows16<128, 1>), grid, dim3(kPfThreads), 0, s, a);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || pl.S == 1) return e;

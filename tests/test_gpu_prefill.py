@@ -130,6 +130,12 @@ LONG = [  # b, H, G, d, q rows, keys, dtype, window, sinks, q_lens, kv_lens
     (2, 1, 8, 128, 300, 1501, "bf16", 0, 0, [300, 171], [1501, 1500]),
     (1, 3, 8, 64, 900, 900, "bf16", 0, 0, None, None),
     (1, 8, 4, 64, 200, 300, "bf16", 0, 0, None, None),
+    (1, 4, 2, 64, 1500, 1500, "f32", 200, 0, None, None),
+    (2, 4, 4, 128, 300, 300, "f32", 0, 0, None, [300, 211]),
+    (2, 8, 4, 128, 260, 400, "f32", 0, 0, [260, 33], [399, 400]),
+    (1, 1, 16, 64, 300, 900, "f32", 0, 0, None, None),
+    (1, 1, 2, 64, 4, 4000, "f32", 0, 0, None, None),
+    (1, 8, 2, 64, 300, 6000, "bf16", 0, 0, None, None),
 ]
 
 
