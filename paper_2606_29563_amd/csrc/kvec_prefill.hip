@@ -92,7 +92,7 @@ constexpr int kPfKeys = 32;
 // the 16x16x4 f32 product; tiles of 32 keys in two LDS buffers.  With KW = 2 four more
 // waves take every other tile, and the states meet in LDS.  Bound by that
 // product's rate (a sixteenth of the bf16 one's) and the softmax between two products:
-// 4000 rows of 8 query and 4 KV heads, d 64, in 186 us, 88 TFLOP/s of 153.
+// 4000 rows of 8 query and 4 KV heads, d 64, in 180 us, 91 TFLOP/s of 153.
 template <int D, int KW>
 __global__ __launch_bounds__(kPfThreads * KW) void pf_rows16(PfArgs a) {
   using TT = F32;
