@@ -392,7 +392,9 @@ kvec_status kvec_prefill_workspace_size(const kvec_attention_config* cfg, size_t
  *   out[b][j][r] = sum_t softmax_t(q_{b,j,r} . k_{b,h,t} / sqrt(d)) v_{b,h,t},
  *   lse[b][j][r] = ln sum_t exp(q_{b,j,r} . k_{b,h,t} / sqrt(d)),  h = j / G,
  * over the keys t <= p with t > p - window (window 0: every t <= p) or
- * t < n_sinks.  A row that sees no key (nq > nk) gets zeros and lse = -inf.
+ * t < n_sinks.  A row that sees no key (nq > nk) gets zeros and lse = -inf, and so
+ * does one whose logits are all -infinity; one with a NaN or +infinity among its
+ * logits (a query that is no number) gets NaN in out and lse.
  *   q        device, cfg->dtype [batch][n_q_heads][q_len][d] (post-RoPE),
  *            strides q_strides = {batch, head, row}.
  *   k, v     device, cfg->dtype [batch][H][kv_len][d], strides {batch, head, t}.
@@ -507,7 +509,10 @@ kvec_status kvec_paged_decode_workspace_size(const kvec_paged_config* cfg, int32
  *   acc         nullable device in/out: acc[s] += mean over the G query heads of
  *               p_{j,s}, every visible slot (always the same bits: no atomics).
  *   ws          device workspace of kvec_paged_decode_workspace_size() bytes.
- * What masked and missing slots hold (NaN too) never matters. */
+ * What masked and missing slots hold (NaN too) never matters.  A head whose visible
+ * logits are all -infinity counts as one with no visible slot (and adds nothing to acc);
+ * a NaN or +infinity among them makes its out, its lse and the acc of the visible
+ * slots of its KV head NaN. */
 kvec_status kvec_paged_decode(const kvec_paged_config* cfg,
                               const void* q, const int64_t q_strides[2],
                               const void* k_pool, const void* v_pool,

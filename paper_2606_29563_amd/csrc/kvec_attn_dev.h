@@ -215,7 +215,17 @@ __device__ __forceinline__ int piece_in_copy(int i, int lane) {
   return (lane % RG::CPR) ^ (row_in_copy<TT, D>(i, lane) & RG::SWZ);
 }
 
-// Merge of (m2, l2, a2) into (m, l, a); m = -inf means an empty state.
+// Results of a closed state.  Only the sum tells an empty state, 0, from one of logits
+// that were NaN: maxima pass over NaN and can be -inf in both, the sum then is NaN, and
+// so become the outputs and the log-sum-exp.  (A state that holds a finite maximum has the
+// exponential of its largest logit, 1, in its sum.)
+__device__ __forceinline__ bool state_empty(float l) { return l == 0.f; }
+__device__ __forceinline__ float state_inverse(float l) { return state_empty(l) ? 0.f : 1.f / l; }
+__device__ __forceinline__ float state_lse(float m, float l) {
+  return state_empty(l) ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+
+// Merge of (m2, l2, a2) into (m, l, a); an empty state is (-inf, 0, 0).
 __device__ __forceinline__ void state_merge(float& m, float& l, float& a, float m2, float l2, float a2) {
   const float mm = fmaxf(m, m2);
   const float ref = mm == -INFINITY ? 0.f : mm;

@@ -70,6 +70,9 @@ __device__ __forceinline__ bool page_ok(const PdArgs& a, int page) { return page
 // Groups of a split: `per` from x * per on.
 __device__ __forceinline__ int split_groups(const Visible& v, int S) { return (v.groups + S - 1) / S; }
 
+// Base-2 normaliser of a head's weights; a head whose logits are all -inf gives none.
+__device__ __forceinline__ float base2_norm(float m, float l) { return state_empty(l) ? 0.f : m + log2f(l); }
+
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));  // acc is aligned to its elements
 
 // Adds the mean over the query heads of 2^(logit - norm) to four neighbouring slots:
@@ -221,11 +224,10 @@ __device__ __forceinline__ void partial(const PdArgs& a, char* smem) {
     }
     const int64_t j = (int64_t)b * a.c.HQ + h * G + g;
     if constexpr (ONE) {
-      a.out[j * D + e] = m == -INFINITY ? 0.f : o / l;
+      a.out[j * D + e] = state_empty(l) ? 0.f : o / l;
       if (e == 0) {
-        const float ln2 = m + log2f(l);
-        norm[g] = ln2;
-        if (a.lse) a.lse[j] = m == -INFINITY ? -INFINITY : ln2 * 0.69314718055994531f;
+        norm[g] = base2_norm(m, l);
+        if (a.lse) a.lse[j] = state_lse(m, l);
       }
     } else {
       a.part[(j * a.S + s) * D + e] = o;
@@ -379,8 +381,8 @@ __global__ __launch_bounds__(kPdThreads) void pd_combine(PdArgs a) {
 #pragma unroll
       for (int i = 1; i < PARTS; ++i) r += st[i][e];
       const int64_t j = j0 + x;
-      a.out[j * D + e] = top == -INFINITY ? 0.f : r / l;
-      if (a.lse && e == 0) a.lse[j] = top == -INFINITY ? -INFINITY : (top + log2f(l)) * 0.69314718055994531f;
+      a.out[j * D + e] = state_empty(l) ? 0.f : r / l;
+      if (a.lse && e == 0) a.lse[j] = state_lse(top, l);
     }
   }
   if constexpr (ACC) {
@@ -393,7 +395,7 @@ __global__ __launch_bounds__(kPdThreads) void pd_combine(PdArgs a) {
       next = split(g + kPdWaves);
       float l;
       const float top = total(g, z, l);
-      if (lane == 0) norm[g] = top + log2f(l);
+      if (lane == 0) norm[g] = base2_norm(top, l);
     }
     __syncthreads();
     if (ok) add_weights(a, vis, slot, acc, whole, old, y, lg, norm);

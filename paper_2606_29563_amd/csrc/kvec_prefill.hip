@@ -208,15 +208,13 @@ __global__ __launch_bounds__(kPfThreads * KW) void pf_rows16(PfArgs a) {
       *reinterpret_cast<f32x4*>(pp + kStateHead + 16 * t + 4 * c) = col.o[t];
     return;
   }
-  const float inv = col.m == -INFINITY ? 0.f : 1.f / col.l;
+  const float inv = state_inverse(col.l);
   char* dst = p.out + ((int64_t)b * p.os[0] + (int64_t)j * p.os[1] + (int64_t)r * p.os[2]) * ES;
 #pragma unroll
   for (int t = 0; t < D / 16; ++t) {
     *reinterpret_cast<f32x4*>(dst + (16 * t + 4 * c) * 4) = col.o[t] * inv;
   }
-  if (p.lse && c == 0)
-    p.lse[(int64_t)b * p.ls[0] + (int64_t)j * p.ls[1] + r] =
-        col.m == -INFINITY ? -INFINITY : (col.m + log2f(col.l)) * 0.69314718055994531f;
+  if (p.lse && c == 0) p.lse[(int64_t)b * p.ls[0] + (int64_t)j * p.ls[1] + r] = state_lse(col.m, col.l);
 }
 
 // bf16: 32 packed rows are the columns of 32x32x16 products (S^T = K Q^T, O^T = V^T
@@ -398,7 +396,7 @@ __device__ __forceinline__ void store_column(const PfArgs& a, const Columns32<TT
             f32x4{col.o[dt][e], col.o[dt][e + 1], col.o[dt][e + 2], col.o[dt][e + 3]};
     return;
   }
-  const float inv = col.m == -INFINITY ? 0.f : 1.f / col.l;
+  const float inv = state_inverse(col.l);
   char* dst = p.out + ((int64_t)b * p.os[0] + (int64_t)j * p.os[1] + (int64_t)r * p.os[2]) * 2;
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
@@ -410,9 +408,7 @@ __device__ __forceinline__ void store_column(const PfArgs& a, const Columns32<TT
       for (int f = 0; f < 4; ++f) v[f] = (__bf16)(col.o[dt][e + f] * inv);
       *reinterpret_cast<bf16x4*>(dst + col.dim(dt, e) * 2) = v;
     }
-  if (p.lse && col.hh == 0)
-    p.lse[(int64_t)b * p.ls[0] + (int64_t)j * p.ls[1] + r] =
-        col.m == -INFINITY ? -INFINITY : (col.m + log2f(col.l)) * 0.69314718055994531f;
+  if (p.lse && col.hh == 0) p.lse[(int64_t)b * p.ls[0] + (int64_t)j * p.ls[1] + r] = state_lse(col.m, col.l);
 }
 
 // Many rows: a work-group of eight or four waves (pf_plan chooses) takes 256 or 128
@@ -672,9 +668,8 @@ __global__ __launch_bounds__(256) void pf_join(PfArgs a) {
     for (int i = 1; i < PARTS; ++i) state_merge(m, l, o, st[i][0][e], st[i][1][e], st[i][2][e]);
   }
   T* dst = reinterpret_cast<T*>(p.out) + (int64_t)b * p.os[0] + (int64_t)j * p.os[1] + (int64_t)r * p.os[2];
-  dst[e] = (T)(m == -INFINITY ? 0.f : o / l);
-  if (p.lse && e == 0)
-    p.lse[(int64_t)b * p.ls[0] + (int64_t)j * p.ls[1] + r] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+  dst[e] = (T)(state_empty(l) ? 0.f : o / l);
+  if (p.lse && e == 0) p.lse[(int64_t)b * p.ls[0] + (int64_t)j * p.ls[1] + r] = state_lse(m, l);
 }
 
 template <class T, int D>
