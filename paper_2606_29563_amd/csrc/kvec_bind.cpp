@@ -133,7 +133,16 @@ PyObject* guarded(F f) {
     return nullptr;
   }
 }
-PyObject* result(const Args& g, kvec_status st) { return g.ok ? PyLong_FromLong(st) : nullptr; }
+// The status of a call of the C interface, made without the interpreter's lock: a launch
+// may wait for room in the device's queue, and other threads run meanwhile (0.03 us a call).
+template <class F>
+PyObject* status_of(F call) {
+  kvec_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = call();
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
 PyObject* unfit() { return PyErr_Occurred() ? nullptr : PyLong_FromLong(-1); }
 
 PyObject* prefill_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -155,7 +164,9 @@ PyObject* prefill_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const int32_t* q_lens = g.dense<int32_t>(at::kInt, {c->batch}, true);
     const int32_t* kv_lens = g.dense<int32_t>(at::kInt, {c->batch}, true);
     if (!g.ok) return unfit();
-    return result(g, g_prefill(c, q, qs, k, ks, v, vs, q_lens, kv_lens, out, os, lse, lse ? ls : nullptr, ws, bytes, stream));
+    return status_of([&] {
+      return g_prefill(c, q, qs, k, ks, v, vs, q_lens, kv_lens, out, os, lse, lse ? ls : nullptr, ws, bytes, stream);
+    });
   });
 }
 
@@ -186,8 +197,10 @@ PyObject* paged_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
     int32_t* pos = g.dense<int32_t>(at::kInt, {c->n_pages, c->n_kv_heads, c->page_size}, true);
     if (!g.ok || ps[0] != ps2[0] || ps[1] != ps2[1] || ps[2] != ps2[2]) return unfit();
     if (tokens > INT32_MAX || half > INT32_MAX / 2) return PyLong_FromLong(KVEC_ERR_UNSUPPORTED);
-    return result(g, g_append(c, (int32_t)tokens, q, qs, k, ks, v, vs, wq, wk, eps, positions, freq, freq ? (int32_t)(2 * half) : 0,
-                              slots, q_out, os, kp, vp, ps, acc, pos, stream));
+    return status_of([&] {
+      return g_append(c, (int32_t)tokens, q, qs, k, ks, v, vs, wq, wk, eps, positions, freq, freq ? (int32_t)(2 * half) : 0,
+                      slots, q_out, os, kp, vp, ps, acc, pos, stream);
+    });
   });
 }
 
@@ -212,7 +225,9 @@ PyObject* paged_decode(PyObject*, PyObject* const* args, Py_ssize_t n) {
     float* lse = g.dense<float>(at::kFloat, {c->batch, c->n_q_heads}, true);
     float* acc = g.dense<float>(at::kFloat, {c->n_pages, c->n_kv_heads, c->page_size}, true);
     if (!g.ok || ps[0] != ps2[0] || ps[1] != ps2[1] || ps[2] != ps2[2]) return unfit();
-    return result(g, g_decode(c, q, qs, kp, vp, ps, table, lens, max_len, window, sinks, out, lse, acc, ws, bytes, stream));
+    return status_of([&] {
+      return g_decode(c, q, qs, kp, vp, ps, table, lens, max_len, window, sinks, out, lse, acc, ws, bytes, stream);
+    });
   });
 }
 
@@ -240,8 +255,9 @@ PyObject* paged_evict(PyObject*, PyObject* const* args, Py_ssize_t n) {
     int32_t* kept = g.dense<int32_t>(at::kInt, {c->batch, c->n_kv_heads, budget}, true);
     const int32_t max_len = g.int32();
     if (!g.ok || ps[0] != ps2[0] || ps[1] != ps2[1] || ps[2] != ps2[2]) return unfit();
-    return result(g, g_evict(c, budget, window, sinks, kp, vp, ps, table, lens, seen, max_len, acc, pos, kept, lens_out, ws, bytes,
-                             stream));
+    return status_of([&] {
+      return g_evict(c, budget, window, sinks, kp, vp, ps, table, lens, seen, max_len, acc, pos, kept, lens_out, ws, bytes, stream);
+    });
   });
 }
 

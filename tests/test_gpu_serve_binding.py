@@ -1,0 +1,49 @@
+"""The serving calls' compiled marshalling module, with tensors on the GPU."""
+import ctypes
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+def _calls(kv):
+    """(name, call, its arguments) of the four serving calls."""
+    import torch
+    b, H, HQ, d, page = 2, 2, 8, 64, 16
+    cfg, attn = kv.PagedConfig(b, H, HQ, d, page, 6, 3), kv.AttentionConfig(b, H, HQ, d, 7, 40)
+    i32, f32 = torch.int32, torch.float32
+    zeros = lambda *s, t=torch.bfloat16: torch.zeros(s, dtype=t, device="cuda")  # noqa: E731
+    pools = dict(k_pool=zeros(6, H, page, d), v_pool=zeros(6, H, page, d))
+    seq = dict(page_table=torch.arange(6, dtype=i32, device="cuda").view(b, 3), lens=zeros(b, t=i32) + 5)
+    meta = dict(acc=zeros(6, H, page, t=f32), pos=zeros(6, H, page, t=i32))
+    ws = zeros(1 << 20, t=torch.uint8)
+    return [
+        ("append", lambda **k: kv.kvec_paged_append(cfg, **k),
+         dict(q=zeros(3, HQ, d), k=zeros(3, H, d), v=zeros(3, H, d), positions=zeros(3, t=i32), slots=torch.arange(3, device="cuda"),
+              q_out=zeros(3, HQ, d), **pools, q_weight=zeros(d), k_weight=zeros(d), inv_freq=zeros(d // 2, t=torch.float64), **meta)),
+        ("decode", lambda **k: kv.kvec_paged_decode(cfg, **k),
+         dict(q=zeros(b, HQ, d), **pools, **seq, out=zeros(b, HQ, d, t=f32), ws=ws, lse=zeros(b, HQ, t=f32), acc=meta["acc"])),
+        ("evict", lambda **k: kv.kvec_paged_evict(cfg, 4, **k),
+         dict(**pools, **seq, n_seen=zeros(b, t=i32), **meta, lens_out=zeros(b, t=i32), ws=ws, kept=zeros(b, H, 4, t=i32))),
+        ("prompt", lambda **k: kv.kvec_prefill_attention(attn, **k),
+         dict(q=zeros(b, HQ, 7, d), k=zeros(b, H, 40, d), v=zeros(b, H, 40, d), out=zeros(b, HQ, 7, d), ws=ws, lse=zeros(b, HQ, 7, t=f32),
+              q_lens=zeros(b, t=i32), kv_lens=zeros(b, t=i32))),
+    ]
+
+
+def test_other_threads_run_during_a_call(gpu_lib):
+    """The interpreter's lock is free while the C interface launches.  Its entry points
+    are replaced by PyGILState_Check, which says whether the calling thread holds the
+    lock: 1 would come back as an error."""
+    kv = gpu_lib
+    bind = kv._bound()
+    held = ctypes.cast(ctypes.pythonapi.PyGILState_Check, ctypes.c_void_p).value
+    entries = [ctypes.cast(getattr(kv.load(), n), ctypes.c_void_p).value
+               for n in ("kvec_prefill_attention", "kvec_paged_append", "kvec_paged_decode", "kvec_paged_evict")]
+    calls = _calls(kv)
+    try:
+        bind.bind(*[held] * 4)
+        for _, call, args in calls:
+            call(**args)
+    finally:
+        bind.bind(*entries)
