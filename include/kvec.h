@@ -373,7 +373,7 @@ kvec_status kvec_decode_attention_noalloc(const kvec_config* cfg,
 /* Shape of one attention over a prompt. */
 typedef struct kvec_attention_config {
   int32_t batch;       /* sequences, 1..65535 */
-  int32_t n_kv_heads;  /* H, 1..1024; batch * H at most 2^22 */
+  int32_t n_kv_heads;  /* H, 1..1024; batch * H below 2^22 */
   int32_t n_q_heads;   /* multiple of H; G = n_q_heads / H in 1..16 */
   int32_t head_dim;    /* d in {64, 128} */
   int32_t q_len;       /* query rows per sequence, 1..2^20 */
@@ -444,7 +444,7 @@ kvec_status kvec_prefill_attention(const kvec_attention_config* cfg,
 
 typedef struct kvec_paged_config {
   int32_t batch;       /* sequences, 1..65535 */
-  int32_t n_kv_heads;  /* H, 1..1024; batch * H at most 2^22 */
+  int32_t n_kv_heads;  /* H, 1..1024; batch * H below 2^22 */
   int32_t n_q_heads;   /* multiple of H; G = n_q_heads / H in 1..16 */
   int32_t head_dim;    /* d in {64, 128} */
   int32_t page_size;   /* tokens per page, a multiple of 16 */

@@ -27,8 +27,9 @@ kvec_status check_heads(int32_t batch, int32_t H, int32_t HQ, int32_t d, int32_t
   if (batch < 1 || H < 1 || HQ < 1 || HQ % H != 0 || d < 1) return KVEC_ERR_INVALID;
   if (dtype != KVEC_BF16 && dtype != KVEC_F32) return KVEC_ERR_INVALID;
   if (batch > 65535 || H > 1024 || HQ / H > 16 || (d != 64 && d != 128)) return KVEC_ERR_UNSUPPORTED;
-  // with the bound on a prompt's rows: launches stay below 2^32 threads
-  if ((int64_t)batch * H > 1 << 22) return KVEC_ERR_UNSUPPORTED;
+  // launches stay below 2^32 threads: the eviction's selection has 1024 for every
+  // (sequence, KV head)
+  if ((int64_t)batch * H >= 1 << 22) return KVEC_ERR_UNSUPPORTED;
   return KVEC_OK;
 }
 
