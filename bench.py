@@ -96,7 +96,7 @@ TRAFFIC_FILE = os.path.join(ROOT, "profiles", "step_kernel_{workload}_traffic.md
 SOURCE_DIRS = (os.path.join(ROOT, "paper_2606_29563_amd", "csrc"), os.path.join(ROOT, "include"))
 # sources outside the step kernel's build (they do not change its counters)
 DIGEST_SKIP = ("kvec_decode.hip", "kvec_serve_api.hip", "kvec_serve.h", "kvec_attn_dev.h", "kvec_prefill.hip",
-               "kvec_append.hip", "kvec_paged_decode.hip", "kvec_paged_evict.hip")
+               "kvec_prefill_plan.h", "kvec_append.hip", "kvec_paged_decode.hip", "kvec_paged_evict.hip")
 
 
 def source_digest() -> str:

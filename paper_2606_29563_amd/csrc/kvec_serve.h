@@ -4,6 +4,7 @@
 #pragma once
 
 #include "kvec_internal.h"
+#include "kvec_prefill_plan.h"
 
 namespace kvec {
 
@@ -59,15 +60,13 @@ hipError_t run_paged_evict(const PagedView& c, int budget, int window, int sinks
                            float* acc, int32_t* pos, int32_t* kept, int32_t* lens_out, char* ws,
                            hipStream_t s);
 
-struct PrefillArgs {
+struct PrefillArgs : PrefillShape {
   const char *q, *k, *v;
   int64_t qs[3], ks[3], vs[3], os[3], ls[2];
   const int32_t *q_lens, *kv_lens;
   char* out;
   float* lse;
-  int batch, H, HQ, G, D, q_len, kv_len, window, sinks, esize;
 };
-size_t prefill_ws(const PrefillArgs& a);
-hipError_t run_prefill(const PrefillArgs& a, char* ws, hipStream_t s);
+hipError_t run_prefill(const PrefillArgs& a, const PfPlan& plan, char* ws, hipStream_t s);
 
 }  // namespace kvec

@@ -112,7 +112,7 @@ kvec_status kvec_prefill_workspace_size(const kvec_attention_config* cfg, size_t
   const kvec_status st = make_prefill(cfg, &a);
   if (st != KVEC_OK) return st;
   if (!bytes) return KVEC_ERR_INVALID;
-  *bytes = prefill_ws(a);
+  *bytes = pf_plan(a).bytes;
   return KVEC_OK;
 }
 
@@ -133,7 +133,8 @@ kvec_status kvec_prefill_attention(const kvec_attention_config* cfg, const void*
   if (lse && !lse_ok(lse, lse_strides, 2)) return KVEC_ERR_INVALID;
   const int64_t span = k_strides[2] > v_strides[2] ? k_strides[2] : v_strides[2];
   if ((int64_t)a.kv_len * (span > a.D ? span : a.D) * a.esize >= (int64_t)1 << 31) return KVEC_ERR_UNSUPPORTED;
-  if ((st = check_size(prefill_ws(a), ws, ws_bytes)) != KVEC_OK) return st;
+  const PfPlan plan = pf_plan(a);
+  if ((st = check_size(plan.bytes, ws, ws_bytes)) != KVEC_OK) return st;
   a.q = static_cast<const char*>(q);
   a.k = static_cast<const char*>(k);
   a.v = static_cast<const char*>(v);
@@ -151,7 +152,7 @@ kvec_status kvec_prefill_attention(const kvec_attention_config* cfg, const void*
     a.ls[0] = lse_strides[0];
     a.ls[1] = lse_strides[1];
   }
-  return dev(run_prefill(a, static_cast<char*>(ws), stream));
+  return dev(run_prefill(a, plan, static_cast<char*>(ws), stream));
 }
 
 kvec_status kvec_paged_append(const kvec_paged_config* cfg, int32_t n_tokens, const void* q,
