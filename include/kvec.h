@@ -414,7 +414,8 @@ kvec_status kvec_prefill_workspace_size(const kvec_attention_config* cfg, size_t
  * rounded to bf16 for the product with V.  The keys below nk have to be finite:
  * a NaN or infinity there can reach rows near it that do not see it.
  * kv_len rows of the k or v stride must span less than 2 GiB, and batch *
- * n_q_heads * q_len must be below 2^29 (else KVEC_ERR_UNSUPPORTED). */
+ * n_q_heads * q_len must be below 2^29 (else KVEC_ERR_UNSUPPORTED; from 2^28 on also
+ * for shapes whose launch would have 2^32 threads). */
 kvec_status kvec_prefill_attention(const kvec_attention_config* cfg,
                                    const void* q, const int64_t q_strides[3],
                                    const void* k, const int64_t k_strides[3],

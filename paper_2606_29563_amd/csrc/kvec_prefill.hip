@@ -77,11 +77,6 @@ __device__ __forceinline__ bool pf_item(const PfArgs& a, int* bh, int* tile, int
   *split = it % a.S;
   return true;
 }
-inline unsigned pf_grid(const PfArgs& a) {
-  const int64_t BH = (int64_t)a.p.batch * a.p.H, items = (int64_t)a.tiles * a.S;
-  return (unsigned)(8 % BH == 0 ? (items + 8 / BH - 1) / (8 / BH) * 8 : items * BH);
-}
-
 // float32: a work-group of four waves takes 64 packed rows, 16 a wave (Columns16), on
 // the 16x16x4 f32 product; tiles of 32 keys in two LDS buffers.  With KW = 2 four more
 // waves take every other tile, and the states meet in LDS.  Bound by that
@@ -681,27 +676,27 @@ hipError_t run_prefill(const PrefillArgs& p, const PfPlan& pl, char* ws, hipStre
   a.tiles = pl.tiles;
   a.part = reinterpret_cast<float*>(ws);
   a.sc = (float)(1.4426950408889634 / sqrt((double)p.D));
-  const dim3 grid(pf_grid(a));
+  const dim3 grid((unsigned)pf_work_groups(p, pl)), group(pf_threads(pl.kernel));
   const bool d64 = p.D == 64;
   if (pl.kernel == kRows32) {
-    hipLaunchKernelGGL((pf_rows32<BF16, 128, 8, 1, 64>), grid, dim3(512), 0, s, a);
+    hipLaunchKernelGGL((pf_rows32<BF16, 128, 8, 1, 64>), grid, group, 0, s, a);
   } else if (pl.kernel == kRows32Half) {
-    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64, 4, 1, 64>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((pf_rows32<BF16, 128, 4, 1, 64>), grid, dim3(256), 0, s, a);
+    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64, 4, 1, 64>), grid, group, 0, s, a);
+    else hipLaunchKernelGGL((pf_rows32<BF16, 128, 4, 1, 64>), grid, group, 0, s, a);
   } else if (pl.kernel == kRows32Keys) {
-    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64, 4, 2, 64>), grid, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((pf_rows32<BF16, 128, 4, 2, 64>), grid, dim3(512), 0, s, a);
+    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64, 4, 2, 64>), grid, group, 0, s, a);
+    else hipLaunchKernelGGL((pf_rows32<BF16, 128, 4, 2, 64>), grid, group, 0, s, a);
   } else if (pl.kernel == kRows32Keys4) {
-    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64, 2, 4, 32>), grid, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((pf_rows32<BF16, 128, 2, 4, 32>), grid, dim3(512), 0, s, a);
+    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64, 2, 4, 32>), grid, group, 0, s, a);
+    else hipLaunchKernelGGL((pf_rows32<BF16, 128, 2, 4, 32>), grid, group, 0, s, a);
   } else if (pl.kernel == kRows16Keys) {
-    if (d64) hipLaunchKernelGGL((pf_rows16<64, 2>), grid, dim3(2 * kPfThreads), 0, s, a);
-    else hipLaunchKernelGGL((pf_rows16<128, 2>), grid, dim3(2 * kPfThreads), 0, s, a);
+    if (d64) hipLaunchKernelGGL((pf_rows16<64, 2>), grid, group, 0, s, a);
+    else hipLaunchKernelGGL((pf_rows16<128, 2>), grid, group, 0, s, a);
   } else if (pl.kernel == kFew) {
-    hipLaunchKernelGGL((pf_few<BF16, 128>), grid, dim3(kPfFewThreads), 0, s, a);
+    hipLaunchKernelGGL((pf_few<BF16, 128>), grid, group, 0, s, a);
   } else {
-    if (d64) hipLaunchKernelGGL((pf_rows16<64, 1>), grid, dim3(kPfThreads), 0, s, a);
-    else hipLaunchKernelGGL((pf_rows16<128, 1>), grid, dim3(kPfThreads), 0, s, a);
+    if (d64) hipLaunchKernelGGL((pf_rows16<64, 1>), grid, group, 0, s, a);
+    else hipLaunchKernelGGL((pf_rows16<128, 1>), grid, group, 0, s, a);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || pl.S == 1) return e;

@@ -26,6 +26,17 @@ struct PfPlan {
   size_t bytes;  // partial states
 };
 
+inline int pf_threads(PfKernel kernel) {
+  return kernel == kFew ? kPfFewThreads : kernel == kRows16 || kernel == kRows32Half ? kPfThreads : 2 * kPfThreads;
+}
+
+// Work-groups of the launch: every (row tile, split) of every (sequence, KV head), or, of
+// fewer than eight of these, as many more as send each one's to XCDs of its own (pf_item).
+inline int64_t pf_work_groups(const PrefillShape& a, const PfPlan& p) {
+  const int64_t BH = (int64_t)a.batch * a.H, items = (int64_t)p.tiles * p.S;
+  return 8 % BH == 0 ? (items + 8 / BH - 1) / (8 / BH) * 8 : items * BH;
+}
+
 inline double pf_ceil(double x) {  // 0 <= x < 2^31
   const int whole = (int)x;
   return whole + (whole < x);

@@ -97,6 +97,12 @@ kvec_status set_lens(PagedView* v, const int32_t* table, const int32_t* lens, in
   return KVEC_OK;
 }
 
+// A prompt's launch stays below 2^32 threads.  Up to eight a row, and 512 for every
+// (sequence, KV head), can pass that from 2^28 rows on.
+kvec_status check_plan(const PrefillShape& a, const PfPlan& p) {
+  return pf_work_groups(a, p) * pf_threads(p.kernel) >= (int64_t)1 << 32 ? KVEC_ERR_UNSUPPORTED : KVEC_OK;
+}
+
 kvec_status check_size(size_t need, const void* ws, size_t ws_bytes) {
   if (ws_bytes < need) return KVEC_ERR_WORKSPACE;
   if (need > 0 && !aligned16(ws)) return KVEC_ERR_INVALID;
@@ -109,10 +115,12 @@ extern "C" {
 
 kvec_status kvec_prefill_workspace_size(const kvec_attention_config* cfg, size_t* bytes) {
   PrefillArgs a;
-  const kvec_status st = make_prefill(cfg, &a);
+  kvec_status st = make_prefill(cfg, &a);
   if (st != KVEC_OK) return st;
   if (!bytes) return KVEC_ERR_INVALID;
-  *bytes = pf_plan(a).bytes;
+  const PfPlan plan = pf_plan(a);
+  if ((st = check_plan(a, plan)) != KVEC_OK) return st;
+  *bytes = plan.bytes;
   return KVEC_OK;
 }
 
@@ -134,6 +142,7 @@ kvec_status kvec_prefill_attention(const kvec_attention_config* cfg, const void*
   const int64_t span = k_strides[2] > v_strides[2] ? k_strides[2] : v_strides[2];
   if ((int64_t)a.kv_len * (span > a.D ? span : a.D) * a.esize >= (int64_t)1 << 31) return KVEC_ERR_UNSUPPORTED;
   const PfPlan plan = pf_plan(a);
+  if ((st = check_plan(a, plan)) != KVEC_OK) return st;
   if ((st = check_size(plan.bytes, ws, ws_bytes)) != KVEC_OK) return st;
   a.q = static_cast<const char*>(q);
   a.k = static_cast<const char*>(k);

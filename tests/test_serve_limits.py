@@ -24,3 +24,13 @@ def test_launches_stay_below_2_32_threads():
         assert e.value.status == UNS
     for call in _heads(4095, 1024):
         call()
+
+
+def test_a_prompts_launch_stays_below_2_32_threads():
+    """4.1 million heads of 129 rows over many keys: three work-groups of 512 threads each."""
+    many = kvec.AttentionConfig(batch=4064, n_kv_heads=1024, n_q_heads=1024, head_dim=64, q_len=129, kv_len=8192)
+    with pytest.raises(kvec.KvecError) as e:
+        kvec.kvec_prefill_workspace_size(many)
+    assert e.value.status == UNS
+    fewer = kvec.AttentionConfig(batch=2032, n_kv_heads=1024, n_q_heads=1024, head_dim=64, q_len=129, kv_len=8192)
+    kvec.kvec_prefill_workspace_size(fewer)
