@@ -368,6 +368,9 @@ kvec_status kvec_decode_attention_noalloc(const kvec_config* cfg,
 
 /* ---------------------------------------------------------------------------
  * The prompt's attention
+ *
+ * Here and below strides are less than 2^40 elements, and no dimension spans 2^60
+ * bytes (KVEC_ERR_INVALID).
  * ------------------------------------------------------------------------- */
 
 /* Shape of one attention over a prompt. */

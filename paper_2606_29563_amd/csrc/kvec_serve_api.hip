@@ -4,6 +4,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <initializer_list>
+
 #include "kvec_serve.h"
 
 using namespace kvec;
@@ -14,12 +16,21 @@ constexpr int32_t kMaxLen = 1 << 20;
 
 bool aligned(const void* p, size_t n) { return p && ((uintptr_t)p & (n - 1)) == 0; }
 bool aligned_or_null(const void* p, size_t n) { return !p || ((uintptr_t)p & (n - 1)) == 0; }
-// Strides of rows read in 16-byte pieces; bounded so that offsets fit 64 bits.
-bool row_strides_ok(const int64_t* s, int n, int esize) {
+// Dimensions of these extents and strides, each of fewer than 2^60 bytes: sums of offsets
+// in three of them fit 64 bits.
+bool spans_ok(const int64_t* s, std::initializer_list<int64_t> extents, int esize) {
+  for (const int64_t n : extents) {
+    if (n > 1 && *s >= ((int64_t)1 << 60) / esize / (n - 1)) return false;
+    ++s;
+  }
+  return true;
+}
+// Strides of rows read in 16-byte pieces.
+bool row_strides_ok(const int64_t* s, std::initializer_list<int64_t> extents, int esize) {
   if (!s) return false;
-  for (int i = 0; i < n; ++i)
-    if (s[i] < 0 || s[i] >= (int64_t)1 << 40) return false;
-  return strides_ok(s, n, esize);
+  for (size_t i = 0; i < extents.size(); ++i)
+    if (s[i] >= (int64_t)1 << 40) return false;
+  return strides_ok(s, (int)extents.size(), esize) && spans_ok(s, extents, esize);
 }
 
 // What both configurations share.
@@ -78,7 +89,7 @@ kvec_status make_paged(const kvec_paged_config* c, PagedView* v) {
 // Pools and their strides; the rows of a group of 16 are addressed with 31-bit
 // offsets.
 kvec_status set_pools(PagedView* v, const void* k_pool, const void* v_pool, const int64_t strides[3]) {
-  if (!aligned16(k_pool) || !aligned16(v_pool) || !row_strides_ok(strides, 3, v->esize)) return KVEC_ERR_INVALID;
+  if (!aligned16(k_pool) || !aligned16(v_pool) || !row_strides_ok(strides, {v->n_pages, v->H, v->ps}, v->esize)) return KVEC_ERR_INVALID;
   if (strides[2] * v->esize >= (int64_t)1 << 26) return KVEC_ERR_UNSUPPORTED;
   v->k = static_cast<char*>(const_cast<void*>(k_pool));
   v->v = static_cast<char*>(const_cast<void*>(v_pool));
@@ -134,11 +145,13 @@ kvec_status kvec_prefill_attention(const kvec_attention_config* cfg, const void*
   kvec_status st = make_prefill(cfg, &a);
   if (st != KVEC_OK) return st;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) ||
-      !row_strides_ok(q_strides, 3, a.esize) || !row_strides_ok(k_strides, 3, a.esize) ||
-      !row_strides_ok(v_strides, 3, a.esize) || !row_strides_ok(out_strides, 3, a.esize) ||
+      !row_strides_ok(q_strides, {a.batch, a.HQ, a.q_len}, a.esize) ||
+      !row_strides_ok(k_strides, {a.batch, a.H, a.kv_len}, a.esize) ||
+      !row_strides_ok(v_strides, {a.batch, a.H, a.kv_len}, a.esize) ||
+      !row_strides_ok(out_strides, {a.batch, a.HQ, a.q_len}, a.esize) ||
       !aligned_or_null(q_lens, 4) || !aligned_or_null(kv_lens, 4))
     return KVEC_ERR_INVALID;
-  if (lse && !lse_ok(lse, lse_strides, 2)) return KVEC_ERR_INVALID;
+  if (lse && !(lse_ok(lse, lse_strides, 2) && spans_ok(lse_strides, {a.batch, a.HQ}, 4))) return KVEC_ERR_INVALID;
   const int64_t span = k_strides[2] > v_strides[2] ? k_strides[2] : v_strides[2];
   if ((int64_t)a.kv_len * (span > a.D ? span : a.D) * a.esize >= (int64_t)1 << 31) return KVEC_ERR_UNSUPPORTED;
   const PfPlan plan = pf_plan(a);
@@ -176,8 +189,8 @@ kvec_status kvec_paged_append(const kvec_paged_config* cfg, int32_t n_tokens, co
   if (st != KVEC_OK) return st;
   if (n_tokens < 0 || !(eps >= 0.f) || !isfinite(eps) || rot_dim < 0 || rot_dim > c.D) return KVEC_ERR_INVALID;
   if (n_tokens > 1 << 24 || rot_dim % 16 != 0) return KVEC_ERR_UNSUPPORTED;
-  if (!row_strides_ok(q_strides, 2, c.esize) || !row_strides_ok(k_strides, 2, c.esize) ||
-      !row_strides_ok(v_strides, 2, c.esize) || !row_strides_ok(q_out_strides, 2, c.esize))
+  if (!row_strides_ok(q_strides, {n_tokens, c.HQ}, c.esize) || !row_strides_ok(k_strides, {n_tokens, c.H}, c.esize) ||
+      !row_strides_ok(v_strides, {n_tokens, c.H}, c.esize) || !row_strides_ok(q_out_strides, {n_tokens, c.HQ}, c.esize))
     return KVEC_ERR_INVALID;
   if ((st = set_pools(&c, k_pool, v_pool, pool_strides)) != KVEC_OK) return st;
   if (n_tokens == 0) return KVEC_OK;  // the token tensors may be empty, without an address
@@ -234,7 +247,7 @@ kvec_status kvec_paged_decode(const kvec_paged_config* cfg, const void* q, const
   if (st != KVEC_OK) return st;
   if ((st = set_pools(&c, k_pool, v_pool, pool_strides)) != KVEC_OK) return st;
   if ((st = set_lens(&c, page_table, lens, max_len)) != KVEC_OK) return st;
-  if (window < 0 || n_sinks < 0 || !aligned16(q) || !row_strides_ok(q_strides, 2, c.esize) || !aligned(out, 4) ||
+  if (window < 0 || n_sinks < 0 || !aligned16(q) || !row_strides_ok(q_strides, {c.batch, c.HQ}, c.esize) || !aligned(out, 4) ||
       !aligned_or_null(lse, 4) || !aligned_or_null(acc, 4))
     return KVEC_ERR_INVALID;
   const int w = window >= max_len ? 0 : window;
