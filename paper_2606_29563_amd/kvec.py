@@ -505,17 +505,22 @@ def _serve(name: str, cfg, dev: int, stream, args, tensors) -> None:
 
 
 def _refuse(name: str, tensors) -> None:
-    """Raises for the first tensor that is not what its entry says."""
-    first = tensors[0][1]
+    """Raises for the first tensor that is not what its entry says; what each is comes before
+    where they are."""
     for what, t, shape, dtype, dense in tensors:
-        if t is None:
-            continue
+        assert t is not None, f"{name}: {what} must be given"
         assert tuple(t.shape) == tuple(shape), f"{name}: {what} must be {tuple(shape)}, not {tuple(t.shape)}"
         assert t.dtype == dtype, f"{name}: {what} must be {dtype}, not {t.dtype}"
         assert t.is_contiguous() if dense else t.stride(-1) == 1, \
             f"{name}: {what} must be contiguous" + ("" if dense else " in its last dimension")
-        assert t.is_cuda and t.device == first.device, f"{name}: {what} must be on the GPU of the other tensors"
+    for what, t, *_ in tensors:
+        assert t.is_cuda and t.device == tensors[0][1].device, f"{name}: {what} must be on the GPU of the other tensors"
     raise AssertionError(f"{name}: K and V pools must have the same strides, and a workspace be contiguous on their GPU")
+
+
+def _given(*entries) -> tuple:
+    """Entries of the optional tensors that are there."""
+    return tuple(e for e in entries if e[1] is not None)
 
 
 def kvec_prefill_workspace_size(cfg: AttentionConfig) -> int:
@@ -532,8 +537,9 @@ def kvec_prefill_attention(cfg: AttentionConfig, q, k, v, out, ws=None, lse=None
     dt, f32, i32 = cfg.types
     _serve("kvec_prefill_attention", cfg, q.get_device(), stream, (q, k, v, out, ws, lse, q_lens, kv_lens), lambda: (
         ("q", q, cfg.q_shape, dt, False), ("k", k, cfg.k_shape, dt, False), ("v", v, cfg.k_shape, dt, False),
-        ("out", out, cfg.q_shape, dt, False), ("lse", lse, cfg.lse_shape, f32, False),
-        ("q_lens", q_lens, cfg.len_shape, i32, True), ("kv_lens", kv_lens, cfg.len_shape, i32, True)))
+        ("out", out, cfg.q_shape, dt, False), *_given(
+            ("lse", lse, cfg.lse_shape, f32, False), ("q_lens", q_lens, cfg.len_shape, i32, True),
+            ("kv_lens", kv_lens, cfg.len_shape, i32, True))))
 
 
 def kvec_paged_append(cfg: PagedConfig, q, k, v, positions, slots, q_out, k_pool, v_pool, q_weight=None,
@@ -544,15 +550,15 @@ def kvec_paged_append(cfg: PagedConfig, q, k, v, positions, slots, q_out, k_pool
     (None: no rotation); acc fp32 and pos int32 [n_pages][H][page_size]."""
     def tensors():
         import torch
-        (dt, f32, i32), n, d = cfg.types, q.shape[0], cfg.head_dim
+        (dt, f32, i32), n, d = cfg.types, 0 if q is None else q.shape[0], cfg.head_dim
         half = 0 if inv_freq is None else inv_freq.shape[0]
         return (("k_pool", k_pool, cfg.pool_shape, dt, False), ("v_pool", v_pool, cfg.pool_shape, dt, False),
                 ("q", q, (n, cfg.n_q_heads, d), dt, False), ("k", k, (n, cfg.n_kv_heads, d), dt, False),
                 ("v", v, (n, cfg.n_kv_heads, d), dt, False), ("q_out", q_out, (n, cfg.n_q_heads, d), dt, False),
-                ("positions", positions, (n,), i32, True), ("slots", slots, (n,), torch.int64, True),
-                ("q_weight", q_weight, (d,), dt, True), ("k_weight", k_weight, (d,), dt, True),
-                ("inv_freq", inv_freq, (half,), torch.float64, True), ("acc", acc, cfg.meta_shape, f32, True),
-                ("pos", pos, cfg.meta_shape, i32, True))
+                ("positions", positions, (n,), i32, True), ("slots", slots, (n,), torch.int64, True), *_given(
+                    ("q_weight", q_weight, (d,), dt, True), ("k_weight", k_weight, (d,), dt, True),
+                    ("inv_freq", inv_freq, (half,), torch.float64, True), ("acc", acc, cfg.meta_shape, f32, True),
+                    ("pos", pos, cfg.meta_shape, i32, True)))
     _serve("kvec_paged_append", cfg, k_pool.get_device(), stream, (
         q, k, v, positions, slots, q_out, k_pool, v_pool, q_weight, k_weight, eps, inv_freq, acc, pos), tensors)
 
@@ -580,8 +586,8 @@ def kvec_paged_decode(cfg: PagedConfig, q, k_pool, v_pool, page_table, lens, out
         q, k_pool, v_pool, page_table, lens, out, ws, n, window, n_sinks, lse, acc), lambda: (
         ("q", q, cfg.q_shape, dt, False), ("k_pool", k_pool, cfg.pool_shape, dt, False),
         ("v_pool", v_pool, cfg.pool_shape, dt, False), ("page_table", page_table, cfg.table_shape, i32, True),
-        ("lens", lens, cfg.len_shape, i32, True), ("out", out, cfg.q_shape, f32, True),
-        ("lse", lse, cfg.lse_shape, f32, True), ("acc", acc, cfg.meta_shape, f32, True)))
+        ("lens", lens, cfg.len_shape, i32, True), ("out", out, cfg.q_shape, f32, True), *_given(
+            ("lse", lse, cfg.lse_shape, f32, True), ("acc", acc, cfg.meta_shape, f32, True))))
 
 
 def kvec_paged_evict_workspace_size(cfg: PagedConfig, max_len: int | None, budget: int) -> int:
@@ -604,4 +610,4 @@ def kvec_paged_evict(cfg: PagedConfig, budget: int, k_pool, v_pool, page_table, 
         ("page_table", page_table, cfg.table_shape, i32, True), ("lens", lens, cfg.len_shape, i32, True),
         ("n_seen", n_seen, cfg.len_shape, i32, True), ("lens_out", lens_out, cfg.len_shape, i32, True),
         ("acc", acc, cfg.meta_shape, f32, True), ("pos", pos, cfg.meta_shape, i32, True),
-        ("kept", kept, (cfg.batch, cfg.n_kv_heads, budget), i32, True)))
+        *_given(("kept", kept, (cfg.batch, cfg.n_kv_heads, budget), i32, True))))

@@ -47,3 +47,30 @@ def test_other_threads_run_during_a_call(gpu_lib):
             call(**args)
     finally:
         bind.bind(*entries)
+
+
+def test_every_misfit_is_named(gpu_lib):
+    """Each tensor argument in turn with a wrong type, a wrong shape or on the CPU: the
+    error is about that argument."""
+    import torch
+    for _, call, args in _calls(gpu_lib):
+        call(**args)
+        for name, t in args.items():
+            if name == "ws":
+                with pytest.raises(AssertionError, match="workspace"):
+                    call(**{**args, name: t.cpu()})
+                continue
+            for bad in (t.to(torch.float16), t[..., :-1].contiguous(), t.cpu()):
+                if name == "inv_freq" and bad.dtype == t.dtype and bad.is_cuda:
+                    continue  # any length is a shape of its own
+                with pytest.raises(AssertionError, match=f": {name} must be"):
+                    call(**{**args, name: bad})
+        for name in ("acc", "pos", "n_seen", "lens", "page_table", "out", "slots"):
+            if name in args and not (name in ("acc", "pos") and "n_seen" not in args):  # (elsewhere acc and pos are optional)
+                with pytest.raises(AssertionError, match=f": {name} must be"):
+                    call(**{**args, name: None})
+        if "v_pool" in args:
+            other = args["v_pool"].transpose(1, 2).contiguous().transpose(1, 2)
+            with pytest.raises(AssertionError, match="same strides"):
+                call(**{**args, "v_pool": other})
+    torch.cuda.synchronize()
