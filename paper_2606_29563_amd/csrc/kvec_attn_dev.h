@@ -78,10 +78,10 @@ __device__ __forceinline__ bf16x8 join8(s16x4 a, s16x4 b) {
   return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// Softmax state and output of 16 query columns, NG groups of 16 keys a step.
-// SPLIT: bf16 probabilities as the sum of two bf16 numbers (2^-17 relative
-// instead of 2^-9), at twice the V products.
-template <class TT, int D, int NG, bool SPLIT>
+// Softmax state and output of 16 query columns, NG groups of 16 keys a step.  bf16
+// probabilities go into the V product as the sum of two bf16 numbers, 2^-16 relative
+// instead of 2^-8, at twice the products.
+template <class TT, int D, int NG>
 struct Columns16 {
   using RG = RowGroup<TT, D>;
   static constexpr int DT = D / 16;
@@ -155,15 +155,13 @@ struct Columns16 {
         for (int i = 0; i < 4; ++i) o[t][i] *= f;
     }
     if constexpr (__is_same(TT, BF16)) {
-      // one product over 32 keys, or over 16
-      static_assert(NG == 1 || NG == 2, "keys of a step");
-      typedef __bf16 bf16xk __attribute__((ext_vector_type(4 * NG)));
-      bf16xk hi, lo;
+      static_assert(NG == 1, "keys of a bf16 step");
+      s16x4 hi, lo;
 #pragma unroll
-      for (int i = 0; i < 4 * NG; ++i) {
-        const float v = p[i >> 2][i & 3];
-        hi[i] = (__bf16)v;
-        if (SPLIT) lo[i] = (__bf16)(v - (float)hi[i]);
+      for (int i = 0; i < 4; ++i) {
+        const __bf16 top = (__bf16)p[0][i];
+        hi[i] = __builtin_bit_cast(short, top);
+        lo[i] = __builtin_bit_cast(short, (__bf16)(p[0][i] - (float)top));
       }
       uint32_t at[DT];
       vt_offsets(lane, at);
@@ -172,21 +170,10 @@ struct Columns16 {
       for (int t = 0; t < DT; ++t) at[t] += base;
       s16x4 a0[DT];
       vt_read<0>(at, a0);
-      if constexpr (NG == 2) {
-        s16x4 a1[DT];
-        vt_read<RG::BYTES>(at, a1);
 #pragma unroll
-        for (int t = 0; t < DT; ++t) {
-          const bf16x8 a = join8(a0[t], a1[t]);
-          o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, hi, o[t], 0, 0, 0);
-          if (SPLIT) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, lo, o[t], 0, 0, 0);
-        }
-      } else {
-#pragma unroll
-        for (int t = 0; t < DT; ++t) {
-          o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a0[t], __builtin_bit_cast(s16x4, hi), o[t], 0, 0, 0);
-          if (SPLIT) o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a0[t], __builtin_bit_cast(s16x4, lo), o[t], 0, 0, 0);
-        }
+      for (int t = 0; t < DT; ++t) {
+        o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a0[t], hi, o[t], 0, 0, 0);
+        o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a0[t], lo, o[t], 0, 0, 0);
       }
     } else {
       const int n = lane & 15, c = lane >> 4;

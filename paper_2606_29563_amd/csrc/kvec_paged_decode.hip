@@ -119,7 +119,7 @@ __device__ __forceinline__ void partial(const PdArgs& a, char* smem) {
   const int per = split_groups(vis, a.S);
   const int st0 = min(s * per, vis.groups), st1 = min(st0 + per, vis.groups);
 
-  Columns16<TT, D, 1, true> col;
+  Columns16<TT, D, 1> col;
   col.clear();
   col.q.zero();
   if (n < G) col.q.load(a.q + ((int64_t)b * a.qs_b + (int64_t)(h * G + n) * a.qs_h) * ES, c);

@@ -108,7 +108,7 @@ __global__ __launch_bounds__(kPfThreads * KW) void pf_rows16(PfArgs a) {
   const int per = (sp.n + a.S - 1) / a.S;
   const int t0 = min(split * per, sp.n), t1 = min(t0 + per, sp.n);
 
-  Columns16<TT, D, GRPS, false> col;
+  Columns16<TT, D, GRPS> col;
   col.clear();
   col.q.zero();
   if (live) col.q.load(p.q + ((int64_t)b * p.qs[0] + (int64_t)j * p.qs[1] + (int64_t)r * p.qs[2]) * ES, c);
@@ -231,7 +231,7 @@ __device__ __forceinline__ int v_swizzle(int r) {
 }
 
 // A wave's 32 columns.
-template <class TT, int D>
+template <int D>
 struct Columns32 {
   static constexpr int KS = D / 16, DT = D / 32;
   bf16x8 q[KS];
@@ -368,8 +368,8 @@ struct RowCopy {
 };
 
 // One column's result, or its partial state.
-template <class TT, int D>
-__device__ __forceinline__ void store_column(const PfArgs& a, const Columns32<TT, D>& col, int b, int j, int r, int split) {
+template <int D>
+__device__ __forceinline__ void store_column(const PfArgs& a, const Columns32<D>& col, int b, int j, int r, int split) {
   const PrefillArgs& p = a.p;
   if (a.S > 1) {
     float* pp = a.part + ((((int64_t)b * p.HQ + j) * p.q_len + r) * a.S + split) * (D + kStateHead);
@@ -407,6 +407,11 @@ __device__ __forceinline__ void store_column(const PfArgs& a, const Columns32<TT
 // waves and four more, that go over every other key tile with buffers of their own, or 64
 // rows to four times two waves and every fourth tile of 32 keys; the states meet in LDS.
 //
+// The probabilities are rounded to bf16 once, 2^-8 relative, for the product with V (their
+// sum takes them unrounded).  A second bf16 term for what that leaves, as pf_few has,
+// makes it 2^-16 and half again as many products: the 8k prompt below 730 us for 539, a
+// 32k prompt's chunk behind a window 188 for 141 (one card, in turn).
+//
 // Bound by the matrix cores and the vector work of the softmax, which mostly add
 // up (the counters see them together in 28% of the matrix cores' busy cycles).
 // A causal 8k prompt (32 query, 8 KV heads, d 128): 1.05 PFLOP/s, where a large
@@ -418,10 +423,10 @@ __device__ __forceinline__ void store_column(const PfArgs& a, const Columns32<TT
 // tile's exponentials (561 for 549), waves 4-7 half a tile behind waves 0-3, in
 // step by barriers (607), raised wave priority around the products (549 for 545).
 // RW waves of rows, KW times; the k-th of the KW takes every KW-th tile of KT keys.
-template <class TT, int D, int RW, int KW, int KT>
+template <int D, int RW, int KW, int KT>
 __device__ __forceinline__ void rows32(const PfArgs& a) {
   constexpr int ROWS = 32 * RW;
-  constexpr int ES = elem_bytes<TT>();
+  constexpr int ES = 2;
   constexpr int HALF = KT * D * 2;            // bytes of the K (or V) rows of a tile
   constexpr int PER = HALF / 1024 / RW;       // copies per wave of each
   constexpr int DT = D / 32;
@@ -443,7 +448,7 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
   const int per = (sp.n + a.S - 1) / a.S;
   const int t0 = min(split * per, sp.n), t1 = min(t0 + per, sp.n);
 
-  Columns32<TT, D> col;
+  Columns32<D> col;
   col.init(lane, p.q + ((int64_t)b * p.qs[0] + (int64_t)j * p.qs[1] + (int64_t)r * p.qs[2]) * ES, live);
   const int kstr = (int)(p.ks[2] * ES), vstr = (int)(p.vs[2] * ES);
   const int last = max(sp.nk - 1, 0);
@@ -514,8 +519,8 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
   if (live) store_column(a, col, b, j, r, split);
 }
 
-template <class TT, int D, int RW, int KW, int KT>
-__global__ __launch_bounds__(64 * RW * KW, 2) void pf_rows32(PfArgs a) { rows32<TT, D, RW, KW, KT>(a); }
+template <int D, int RW, int KW, int KT>
+__global__ __launch_bounds__(64 * RW * KW, 2) void pf_rows32(PfArgs a) { rows32<D, RW, KW, KT>(a); }
 
 // Few rows, bf16, d = 128: a work-group of two waves takes 32 packed rows, both waves the
 // same ones.  The waves go over the 32-key steps of the work-group's split in
@@ -523,9 +528,8 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void pf_rows32(PfArgs a) { rows32<
 // end, where their states are joined.  What bounds it is the latency and the reading
 // of K and V (8 rows of 32 heads over 16k keys: 18 us, 3.7 TB/s), so the probabilities
 // go into the product as two bf16 terms.
-template <class TT, int D>
 __device__ __forceinline__ void few(const PfArgs& a) {
-  constexpr int ES = elem_bytes<TT>(), DT = D / 32, WAVES = kPfFewThreads / 64;
+  constexpr int D = 128, ES = 2, DT = D / 32, WAVES = kPfFewThreads / 64;
   constexpr int HALF = kPfFewKeys * D * 2, STEP = 2 * HALF, PER = HALF / 1024;
   constexpr int MERGE = WAVES * 32 * (D + 2) * 4;
   __shared__ __align__(1024) char smem[WAVES * 2 * STEP > MERGE ? WAVES * 2 * STEP : MERGE];
@@ -543,7 +547,7 @@ __device__ __forceinline__ void few(const PfArgs& a) {
   const int per = (sp.n + a.S - 1) / a.S;
   const int t0 = min(split * per, sp.n), t1 = min(t0 + per, sp.n);
 
-  Columns32<TT, D> col;
+  Columns32<D> col;
   col.init(lane, p.q + ((int64_t)b * p.qs[0] + (int64_t)j * p.qs[1] + (int64_t)r * p.qs[2]) * ES, live);
   const int kstr = (int)(p.ks[2] * ES), vstr = (int)(p.vs[2] * ES);
   const int last = max(sp.nk - 1, 0);
@@ -614,8 +618,7 @@ __device__ __forceinline__ void few(const PfArgs& a) {
   store_column(a, col, b, j, r, split);
 }
 
-template <class TT, int D>
-__global__ __launch_bounds__(kPfFewThreads, 1) void pf_few(PfArgs a) { few<TT, D>(a); }
+__global__ __launch_bounds__(kPfFewThreads, 1) void pf_few(PfArgs a) { few(a); }
 
 // Join the splits of the rows: grid (row groups, HQ, batch).  The 256 / D threads of an
 // element take a row each (ROWS; few splits), or share one row's splits.  A batch of
@@ -679,21 +682,21 @@ hipError_t run_prefill(const PrefillArgs& p, const PfPlan& pl, char* ws, hipStre
   const dim3 grid((unsigned)pf_work_groups(p, pl)), group(pf_threads(pl.kernel));
   const bool d64 = p.D == 64;
   if (pl.kernel == kRows32) {
-    hipLaunchKernelGGL((pf_rows32<BF16, 128, 8, 1, 64>), grid, group, 0, s, a);
+    hipLaunchKernelGGL((pf_rows32<128, 8, 1, 64>), grid, group, 0, s, a);
   } else if (pl.kernel == kRows32Half) {
-    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64, 4, 1, 64>), grid, group, 0, s, a);
-    else hipLaunchKernelGGL((pf_rows32<BF16, 128, 4, 1, 64>), grid, group, 0, s, a);
+    if (d64) hipLaunchKernelGGL((pf_rows32<64, 4, 1, 64>), grid, group, 0, s, a);
+    else hipLaunchKernelGGL((pf_rows32<128, 4, 1, 64>), grid, group, 0, s, a);
   } else if (pl.kernel == kRows32Keys) {
-    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64, 4, 2, 64>), grid, group, 0, s, a);
-    else hipLaunchKernelGGL((pf_rows32<BF16, 128, 4, 2, 64>), grid, group, 0, s, a);
+    if (d64) hipLaunchKernelGGL((pf_rows32<64, 4, 2, 64>), grid, group, 0, s, a);
+    else hipLaunchKernelGGL((pf_rows32<128, 4, 2, 64>), grid, group, 0, s, a);
   } else if (pl.kernel == kRows32Keys4) {
-    if (d64) hipLaunchKernelGGL((pf_rows32<BF16, 64, 2, 4, 32>), grid, group, 0, s, a);
-    else hipLaunchKernelGGL((pf_rows32<BF16, 128, 2, 4, 32>), grid, group, 0, s, a);
+    if (d64) hipLaunchKernelGGL((pf_rows32<64, 2, 4, 32>), grid, group, 0, s, a);
+    else hipLaunchKernelGGL((pf_rows32<128, 2, 4, 32>), grid, group, 0, s, a);
   } else if (pl.kernel == kRows16Keys) {
     if (d64) hipLaunchKernelGGL((pf_rows16<64, 2>), grid, group, 0, s, a);
     else hipLaunchKernelGGL((pf_rows16<128, 2>), grid, group, 0, s, a);
   } else if (pl.kernel == kFew) {
-    hipLaunchKernelGGL((pf_few<BF16, 128>), grid, group, 0, s, a);
+    hipLaunchKernelGGL(pf_few, grid, group, 0, s, a);
   } else {
     if (d64) hipLaunchKernelGGL((pf_rows16<64, 1>), grid, group, 0, s, a);
     else hipLaunchKernelGGL((pf_rows16<128, 1>), grid, group, 0, s, a);
