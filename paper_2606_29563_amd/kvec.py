@@ -518,6 +518,11 @@ def _refuse(name: str, tensors) -> None:
     raise AssertionError(f"{name}: K and V pools must have the same strides, and a workspace be contiguous on their GPU")
 
 
+def _other(name: str, kind):
+    """Raises for a configuration of another kind: the compiled module reads it by address."""
+    raise AssertionError(f"{name}: cfg must be a {kind.__name__}")
+
+
 def _given(*entries) -> tuple:
     """Entries of the optional tensors that are there."""
     return tuple(e for e in entries if e[1] is not None)
@@ -534,6 +539,8 @@ def kvec_prefill_attention(cfg: AttentionConfig, q, k, v, out, ws=None, lse=None
     """q, out [b][HQ][q_len][d]; k, v [b][H][kv_len][d] (any leading strides); lse fp32
     [b][HQ][q_len], rows contiguous; q_lens, kv_lens int32 [b].  ws may be None when
     kvec_prefill_workspace_size(cfg) is 0."""
+    if not isinstance(cfg, AttentionConfig):
+        _other("kvec_prefill_attention", AttentionConfig)
     dt, f32, i32 = cfg.types
     _serve("kvec_prefill_attention", cfg, q.get_device(), stream, (q, k, v, out, ws, lse, q_lens, kv_lens), lambda: (
         ("q", q, cfg.q_shape, dt, False), ("k", k, cfg.k_shape, dt, False), ("v", v, cfg.k_shape, dt, False),
@@ -548,6 +555,8 @@ def kvec_paged_append(cfg: PagedConfig, q, k, v, positions, slots, q_out, k_pool
     [n], slots int64 [n] (page * page_size + row; -1: not stored), pools
     [n_pages][H][page_size][d]; weights [d] (None: no norm); inv_freq float64 [rot_dim / 2]
     (None: no rotation); acc fp32 and pos int32 [n_pages][H][page_size]."""
+    if not isinstance(cfg, PagedConfig):
+        _other("kvec_paged_append", PagedConfig)
     def tensors():
         import torch
         (dt, f32, i32), n, d = cfg.types, 0 if q is None else q.shape[0], cfg.head_dim
@@ -580,6 +589,8 @@ def kvec_paged_decode(cfg: PagedConfig, q, k_pool, v_pool, page_table, lens, out
     """q [b][HQ][d]; pools [n_pages][H][page_size][d] (K and V with the same strides);
     page_table int32 [b][max_pages]; lens int32 [b]; out fp32 [b][HQ][d]; lse fp32
     [b][HQ]; acc fp32 [n_pages][H][page_size].  max_len None: every slot of the table."""
+    if not isinstance(cfg, PagedConfig):
+        _other("kvec_paged_decode", PagedConfig)
     dt, f32, i32 = cfg.types
     n = cfg.max_pages * cfg.page_size if max_len is None else max_len
     _serve("kvec_paged_decode", cfg, q.get_device(), stream, (
@@ -602,6 +613,8 @@ def kvec_paged_evict(cfg: PagedConfig, budget: int, k_pool, v_pool, page_table, 
     """Pools and tables as in kvec_paged_decode; acc fp32 and pos int32
     [n_pages][H][page_size]; lens, n_seen, lens_out int32 [b] (lens_out may be lens);
     kept int32 [b][H][budget]."""
+    if not isinstance(cfg, PagedConfig):
+        _other("kvec_paged_evict", PagedConfig)
     dt, f32, i32 = cfg.types
     n = cfg.max_pages * cfg.page_size if max_len is None else max_len
     _serve("kvec_paged_evict", cfg, k_pool.get_device(), stream, (

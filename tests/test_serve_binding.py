@@ -50,3 +50,15 @@ def test_misfits_are_named(call, arg):
     elif arg != first:
         with pytest.raises(AssertionError, match=f": {arg} must be given"):
             f(**{**args, arg: None})
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_a_configuration_of_another_kind_is_refused(call):
+    """The compiled module reads the configuration by its address: the kind is checked first."""
+    kinds = dict(kvec_paged_append=PAGED, kvec_paged_decode=PAGED, kvec_paged_evict=PAGED, kvec_prefill_attention=ATTN)
+    name = "kvec_prefill_attention" if call == "prompt" else f"kvec_paged_{call}"
+    _, args, _ = CALLS[call]
+    more = {} if call in ("append", "prompt") else dict(ws=None, max_len=40)
+    for other in (ATTN if kinds[name] is PAGED else PAGED, kinds[name].c(), None):
+        with pytest.raises(AssertionError, match=f"^{name}: cfg must be"):
+            getattr(kvec, name)(other, *([4] if call == "evict" else []), **args, **more)
