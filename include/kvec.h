@@ -414,8 +414,9 @@ kvec_status kvec_prefill_workspace_size(const kvec_attention_config* cfg, size_t
  *   ws       device workspace of kvec_prefill_workspace_size() bytes (may be
  *            null when that is 0).
  * Softmax statistics and sums are fp32; with bf16 inputs the probabilities are
- * rounded to bf16 for the product with V.  The keys below nk have to be finite:
- * a NaN or infinity there can reach rows near it that do not see it.
+ * rounded to bf16 for the product with V.  What the keys that a row does not see hold
+ * (NaN too) never matters to it.  (Rows whose out holds a NaN or infinity, and those
+ * near them, are computed twice.)
  * kv_len rows of the k or v stride must span less than 2 GiB, and batch *
  * n_q_heads * q_len must be below 2^29 (else KVEC_ERR_UNSUPPORTED; from 2^28 on also
  * for shapes whose launch would have 2^32 threads). */

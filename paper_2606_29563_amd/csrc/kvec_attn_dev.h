@@ -78,6 +78,27 @@ __device__ __forceinline__ bf16x8 join8(s16x4 a, s16x4 b) {
   return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// Values that are no numbers.  A tile that some of its rows see only in part takes the
+// keys that a row does not see with a probability of 0, and 0 times a NaN or infinity in V
+// would stay in its output.  That shows at the end, where the output is no number, and is
+// so rare that everything is done again then, carefully: such values of these tiles are
+// taken as 0 (tame), and the rows that see their keys add them by themselves (add_wild).
+__device__ __forceinline__ bool wild(float v) { return (__float_as_uint(v) & 0x7fffffffu) >= 0x7f800000u; }
+// The lane's pieces of N copies of V in LDS, 1 KiB apart.
+template <class TT, int N>
+__device__ __forceinline__ void tame(char* lds) {
+#pragma unroll 1
+  for (int i = 0; i < 4 * N; ++i) {
+    uint32_t* x = reinterpret_cast<uint32_t*>(lds + (i >> 2) * 1024) + (i & 3);
+    if constexpr (__is_same(TT, BF16)) {
+      const uint32_t lo = wild(__uint_as_float(*x << 16)) ? 0u : *x & 0xffffu, hi = wild(__uint_as_float(*x)) ? 0u : *x & 0xffff0000u;
+      *x = hi | lo;
+    } else {
+      *x = wild(__uint_as_float(*x)) ? 0u : *x;
+    }
+  }
+}
+
 // Softmax state and output of 16 query columns, NG groups of 16 keys a step.  bf16
 // probabilities go into the V product as the sum of two bf16 numbers, 2^-16 relative
 // instead of 2^-8, at twice the products.
@@ -189,6 +210,28 @@ struct Columns16 {
             o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, p[g][i], o[t], 0, 0, 0);
           }
         }
+    }
+  }
+
+  // Whether an element of the lane's output is no number.
+  __device__ __forceinline__ bool wild_output() const {
+    float z[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z[i] = fmaf(o[t][i], 0.f, z[i]);
+    const float any = (z[0] + z[1]) + (z[2] + z[3]);
+    return any != any;
+  }
+  // Adds to the column's output the values of a float32 row of V in memory that are no
+  // numbers, where it sees the row.
+  __device__ __forceinline__ void add_wild(const char* row, int lane, bool seen) {
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(row + (16 * t + 4 * (lane >> 4)) * 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[t][i] += seen && wild(v[i]) ? v[i] : 0.f;
+      __builtin_amdgcn_sched_barrier(0);  // one read's registers at a time
     }
   }
 };

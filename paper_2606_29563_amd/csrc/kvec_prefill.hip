@@ -55,6 +55,29 @@ struct Span {
   }
 };
 
+// Behind a loop over the key tiles t0, t0 + step, ... below t1: add(key) for every key of
+// the tiles that some row sees only in part.
+template <int KT, class Add>
+__device__ __forceinline__ void each_wild(const Span<KT>& sp, int t0, int t1, int step, Add add) {
+#pragma unroll 1
+  for (int t = t0; t < t1; t += step) {
+    const int key0 = sp.key0(t);
+    if (sp.open(key0)) continue;
+#pragma unroll 1
+    for (int key = key0; key < min(key0 + KT, sp.nk); ++key) add(key);
+  }
+}
+// Whether an output of the work-group is no number (flags: one of each wave).  The look at
+// the outputs and the barrier take 0.2 to 0.3 us a call.  Looking at every tile before
+// its use instead, and one loop for both passes, cost 0.4 to 2 us (1500 rows, d 64, 16.0
+// us: 17.4 and 17.6).
+__device__ __forceinline__ bool any_wild(bool* flags, int waves, bool mine) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  flags[wave] = __any(mine);
+  lds_barrier();
+  return __any(flags[lane % waves]);
+}
+
 // Work-group -> (sequence and KV head, row tile, split), longest tiles first.
 // Work-groups go round the eight XCDs, each with an L2 of its own: all that read
 // the K and V of one head run on the same XCD, or, with fewer than eight heads,
@@ -77,6 +100,7 @@ __device__ __forceinline__ bool pf_item(const PfArgs& a, int* bh, int* tile, int
   *split = it % a.S;
   return true;
 }
+
 // float32: a work-group of four waves takes 64 packed rows, 16 a wave (Columns16), on
 // the 16x16x4 f32 product; tiles of 32 keys in two LDS buffers.  With KW = 2 four more
 // waves take every other tile, and the states meet in LDS.  Bound by that
@@ -89,8 +113,10 @@ __global__ __launch_bounds__(kPfThreads * KW) void pf_rows16(PfArgs a) {
   constexpr int ES = RG::ES, GRPS = kPfKeys / 16;
   constexpr int BUF = 2 * GRPS * RG::BYTES;       // K groups, then V groups
   constexpr int PER = 2 * GRPS * RG::NI / 4;      // copies per wave and tile
+  static_assert(GRPS * RG::NI % PER == 0, "a wave copies of K or of V");
   static_assert((KW - 1) * kPfRows * (D + 2) * 4 <= KW * 2 * BUF, "states in LDS");
   __shared__ __align__(1024) char smem_all[KW * 2 * BUF];
+  __shared__ bool flags[4 * KW];
   const PrefillArgs& p = a.p;
   const int G = p.G;
   int bh, tile, split;
@@ -109,7 +135,6 @@ __global__ __launch_bounds__(kPfThreads * KW) void pf_rows16(PfArgs a) {
   const int t0 = min(split * per, sp.n), t1 = min(t0 + per, sp.n);
 
   Columns16<TT, D, GRPS> col;
-  col.clear();
   col.q.zero();
   if (live) col.q.load(p.q + ((int64_t)b * p.qs[0] + (int64_t)j * p.qs[1] + (int64_t)r * p.qs[2]) * ES, c);
 
@@ -117,8 +142,9 @@ __global__ __launch_bounds__(kPfThreads * KW) void pf_rows16(PfArgs a) {
   const int last = max(sp.nk - 1, 0);
   const auto kr = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<char*>(p.k) + ((int64_t)b * p.ks[0] + (int64_t)h * p.ks[1]) * ES, 0, last * kstr + D * ES, kBufferWord3);
-  const auto vr = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<char*>(p.v) + ((int64_t)b * p.vs[0] + (int64_t)h * p.vs[1]) * ES, 0, last * vstr + D * ES, kBufferWord3);
+  char* const v_rows = const_cast<char*>(p.v) + ((int64_t)b * p.vs[0] + (int64_t)h * p.vs[1]) * ES;
+  const auto vr = __builtin_amdgcn_make_buffer_rsrc(v_rows, 0, last * vstr + D * ES, kBufferWord3);
+  auto v_of = [&](int key) { return v_rows + (int64_t)key * vstr; };
   auto copy = [&](int u, int t) {
     const int key0 = sp.key0(t);
 #pragma unroll
@@ -133,28 +159,38 @@ __global__ __launch_bounds__(kPfThreads * KW) void pf_rows16(PfArgs a) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(is_v ? vr : kr, dst, 16, off, 0, 0, 0);
     }
   };
-  if (t0 + kw < t1) copy(0, t0 + kw);
-  int u = 0;
-  for (int t = t0 + kw; t - kw < t1; t += KW, u ^= 1) {
-    wait_vmem<0>();
-    lds_barrier();  // the tile is there, and every wave is done with the other buffer
-    if (t + KW < t1) copy(u ^ 1, t + KW);
-    if (KW > 1 && t >= t1) continue;  // behind the last tile (this step's barrier is passed)
-    const char* kb = smem + u * BUF;
-    const int key0 = sp.key0(t);
-    f32x4 x[GRPS];
-    col.logits(x, kb, lane);
+  auto pass = [&](auto careful) {  // over the key tiles of this split
+    col.clear();
+    if (t0 + kw < t1) copy(0, t0 + kw);
+    int u = 0;
+    for (int t = t0 + kw; t - kw < t1; t += KW, u ^= 1) {
+      wait_vmem<0>();
+      // (the upper half of the waves copies V)
+      if (careful.value && t < t1 && w * PER >= GRPS * RG::NI && !sp.open(sp.key0(t)))
+        tame<TT, PER>(smem + u * BUF + w * PER * 1024 + lane * 16);
+      lds_barrier();  // the tile is there, and every wave is done with the other buffer
+      if (t + KW < t1) copy(u ^ 1, t + KW);
+      if (KW > 1 && t >= t1) continue;  // behind the last tile (this step's barrier is passed)
+      const char* kb = smem + u * BUF;
+      const int key0 = sp.key0(t);
+      f32x4 x[GRPS];
+      col.logits(x, kb, lane);
 #pragma unroll
-    for (int g = 0; g < GRPS; ++g) x[g] *= a.sc;
-    if (!sp.open(key0)) {
+      for (int g = 0; g < GRPS; ++g) x[g] *= a.sc;
+      if (!sp.open(key0)) {
 #pragma unroll
-      for (int g = 0; g < GRPS; ++g)
+        for (int g = 0; g < GRPS; ++g)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (!sp.sees(key0 + 16 * g + 4 * c + e, pos)) x[g][e] = -INFINITY;
+          for (int e = 0; e < 4; ++e)
+            if (!sp.sees(key0 + 16 * g + 4 * c + e, pos)) x[g][e] = -INFINITY;
+      }
+      col.absorb(x, kb + GRPS * RG::BYTES, lane);
     }
-    col.absorb(x, kb + GRPS * RG::BYTES, lane);
-  }
+    if (careful.value)
+      each_wild<kPfKeys>(sp, t0 + kw, t1, KW, [&](int key) { col.add_wild(v_of(key), lane, sp.sees(key, pos)); });
+  };
+  pass(std::false_type{});
+  if (__builtin_expect(any_wild(flags, 4 * KW, col.wild_output()), false)) pass(std::true_type{});
   col.l = col_sum4(col.l);
   if constexpr (KW > 1) {
     __syncthreads();
@@ -244,8 +280,6 @@ struct Columns32 {
   __device__ __forceinline__ void init(int lane, const char* row, bool live) {
     n = lane & 31;
     hh = lane >> 5;
-    m = -INFINITY;
-    l = 0.f;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       q[ks] = __builtin_bit_cast(bf16x8, live ? reinterpret_cast<const uint4*>(row)[2 * ks + hh] : make_uint4(0, 0, 0, 0));
@@ -254,13 +288,20 @@ struct Columns32 {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
-#pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int r = 8 * e + 4 * hh + ((lane & 15) >> 2), piece = 4 * dt + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
         voff[2 * dt + e] = r * D * 2 + (piece ^ v_swizzle<D>(r)) * 16 + (lane & 1) * 8;
       }
     }
+  }
+
+  __device__ __forceinline__ void clear() {
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
   }
 
   // Logits of NB blocks of 32 keys at `kb`.
@@ -319,6 +360,30 @@ struct Columns32 {
       against(ref);
     }
     l += sum;
+  }
+
+  // Whether an element of the lane's output is no number.
+  __device__ __forceinline__ bool wild_output() const {
+    float z[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) z[e & 3] = fmaf(o[dt][e], 0.f, z[e & 3]);
+    const float any = (z[0] + z[1]) + (z[2] + z[3]);
+    return any != any;
+  }
+  // Adds to the column's output the values of a row of V in memory that are no numbers,
+  // where it sees the row.
+  __device__ __forceinline__ void add_wild(const char* row, bool seen) {
+#pragma unroll
+    for (int p = 0; p < 4 * DT; ++p) {  // elements 4 (p % 4) .. + 3 of o[p / 4]
+      const uint2 v = *reinterpret_cast<const uint2*>(row + 16 * p + 8 * hh);
+      const uint32_t f[4] = {v.x << 16, v.x & 0xffff0000u, v.y << 16, v.y & 0xffff0000u};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        o[p >> 2][4 * (p & 3) + e] += seen && wild(__uint_as_float(f[e])) ? __uint_as_float(f[e]) : 0.f;
+      __builtin_amdgcn_sched_barrier(0);  // one read's registers at a time
+    }
   }
 
   // The sum over the column, in both of its lanes.
@@ -422,6 +487,7 @@ __device__ __forceinline__ void store_column(const PfArgs& a, const Columns32<D>
 // dropped: three LDS buffers (540 for 535), the next tile's logits computed beside this
 // tile's exponentials (561 for 549), waves 4-7 half a tile behind waves 0-3, in
 // step by barriers (607), raised wave priority around the products (549 for 545).
+
 // RW waves of rows, KW times; the k-th of the KW takes every KW-th tile of KT keys.
 template <int D, int RW, int KW, int KT>
 __device__ __forceinline__ void rows32(const PfArgs& a) {
@@ -432,6 +498,7 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
   constexpr int DT = D / 32;
   static_assert((KW - 1) * RW * 32 * (D + 2) * 4 <= KW * 4 * HALF, "states in LDS");
   __shared__ __align__(1024) char smem_all[KW * 4 * HALF];
+  __shared__ bool flags[RW * KW];
   const PrefillArgs& p = a.p;
   const int G = p.G;
   int bh, tile, split;
@@ -454,8 +521,9 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
   const int last = max(sp.nk - 1, 0);
   const auto kr = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<char*>(p.k) + ((int64_t)b * p.ks[0] + (int64_t)h * p.ks[1]) * ES, 0, last * kstr + D * ES, kBufferWord3);
-  const auto vr = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<char*>(p.v) + ((int64_t)b * p.vs[0] + (int64_t)h * p.vs[1]) * ES, 0, last * vstr + D * ES, kBufferWord3);
+  char* const v_rows = const_cast<char*>(p.v) + ((int64_t)b * p.vs[0] + (int64_t)h * p.vs[1]) * ES;
+  const auto vr = __builtin_amdgcn_make_buffer_rsrc(v_rows, 0, last * vstr + D * ES, kBufferWord3);
+  auto v_of = [&](int key) { return v_rows + (int64_t)key * vstr; };
   RowCopy<D> rc[PER];
 #pragma unroll
   for (int q = 0; q < PER; ++q) rc[q].init(w * PER + q, lane);
@@ -471,41 +539,49 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, dv, 16, in ? key * vstr + rc[q].vb : kOutOfRange, 0, 0, 0);
     }
   };
-  if (t0 + kw < t1) copy(0, t0 + kw);
-  int u = 0;
-  for (int t = t0 + kw; t - kw < t1; t += KW, u ^= 1) {
-    wait_vmem<0>();
-    lds_barrier();  // the tile is there, and every wave is done with the other buffer
-    if (t + KW < t1) copy(u ^ 1, t + KW);
-    if (KW > 1 && t >= t1) continue;  // behind the last tile (this step's barrier is passed)
-    const char* kb = smem + u * 2 * HALF;
-    const char* vb = kb + HALF;
-    f32x16 x[KT / 32];
-    col.logits(x, kb);
-    const int key0 = sp.key0(t);
-    if (!sp.open(key0)) {
+  auto pass = [&](auto careful) {  // over the key tiles of this split
+    col.clear();
+    if (t0 + kw < t1) copy(0, t0 + kw);
+    int u = 0;
+    for (int t = t0 + kw; t - kw < t1; t += KW, u ^= 1) {
+      wait_vmem<0>();
+      if (careful.value && t < t1 && !sp.open(sp.key0(t)))
+        tame<BF16, PER>(smem + u * 2 * HALF + HALF + w * PER * 1024 + lane * 16);
+      lds_barrier();  // the tile is there, and every wave is done with the other buffer
+      if (t + KW < t1) copy(u ^ 1, t + KW);
+      if (KW > 1 && t >= t1) continue;  // behind the last tile (this step's barrier is passed)
+      const char* kb = smem + u * 2 * HALF;
+      const char* vb = kb + HALF;
+      f32x16 x[KT / 32];
+      col.logits(x, kb);
+      const int key0 = sp.key0(t);
+      if (!sp.open(key0)) {
 #pragma unroll
-      for (int g = 0; g < KT / 32; ++g)
+        for (int g = 0; g < KT / 32; ++g)
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (!sp.sees(key0 + col.key(g, e), pos)) x[g][e] = -INFINITY;
-    }
-    bf16x8 pf[KT / 16];
-    col.template weigh<KT / 32, false>(x, a.sc, pf, pf);
-    // (the compiler's transposing read waits for the copies in flight, which were
-    // issued half a tile before; written out with waits of its own it was slower, 566
-    // us for 545, because then the products cannot be scheduled between the reads)
-#pragma unroll
-    for (int ss = 0; ss < KT / 16; ++ss)
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-        const char* vs = vb + ss * 16 * D * 2;
-        const s16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + col.voff[2 * dt]));
-        const s16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + col.voff[2 * dt + 1]));
-        col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(join8(a0, a1), pf[ss], col.o[dt], 0, 0, 0);
+          for (int e = 0; e < 16; ++e)
+            if (!sp.sees(key0 + col.key(g, e), pos)) x[g][e] = -INFINITY;
       }
-  }
+      bf16x8 pf[KT / 16];
+      col.template weigh<KT / 32, false>(x, a.sc, pf, pf);
+      // (the compiler's transposing read waits for the copies in flight, which were
+      // issued half a tile before; written out with waits of its own it was slower, 566
+      // us for 545, because then the products cannot be scheduled between the reads)
+#pragma unroll
+      for (int ss = 0; ss < KT / 16; ++ss)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+          const char* vs = vb + ss * 16 * D * 2;
+          const s16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + col.voff[2 * dt]));
+          const s16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + col.voff[2 * dt + 1]));
+          col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(join8(a0, a1), pf[ss], col.o[dt], 0, 0, 0);
+        }
+    }
+    if (careful.value) each_wild<KT>(sp, t0 + kw, t1, KW, [&](int key) { col.add_wild(v_of(key), sp.sees(key, pos)); });
+  };
+  pass(std::false_type{});
+  if (__builtin_expect(any_wild(flags, RW * KW, col.wild_output()), false)) pass(std::true_type{});
   col.close();
   if constexpr (KW > 1) {
     __syncthreads();
@@ -553,8 +629,9 @@ __device__ __forceinline__ void few(const PfArgs& a) {
   const int last = max(sp.nk - 1, 0);
   const auto kr = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<char*>(p.k) + ((int64_t)b * p.ks[0] + (int64_t)h * p.ks[1]) * ES, 0, last * kstr + D * ES, kBufferWord3);
-  const auto vr = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<char*>(p.v) + ((int64_t)b * p.vs[0] + (int64_t)h * p.vs[1]) * ES, 0, last * vstr + D * ES, kBufferWord3);
+  char* const v_rows = const_cast<char*>(p.v) + ((int64_t)b * p.vs[0] + (int64_t)h * p.vs[1]) * ES;
+  const auto vr = __builtin_amdgcn_make_buffer_rsrc(v_rows, 0, last * vstr + D * ES, kBufferWord3);
+  auto v_of = [&](int key) { return v_rows + (int64_t)key * vstr; };
   char* ring = smem + w * 2 * STEP;
   RowCopy<D> rc[PER];
 #pragma unroll
@@ -572,41 +649,49 @@ __device__ __forceinline__ void few(const PfArgs& a) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, dv, 16, in ? key * vstr + rc[q].vb : kOutOfRange, 0, 0, 0);
     }
   };
-  copy(0, t0 + w);
-  copy(1, t0 + w + WAVES);
-  int u = 0;
-  for (int t = t0 + w; t < t1; t += WAVES) {
-    wait_vmem<2 * PER>();
-    const char* kb = ring + u * STEP;
-    f32x16 x[1];
-    col.logits(x, kb);
-    const int key0 = sp.key0(t);
-    if (!sp.open(key0)) {
+  auto pass = [&](auto careful) {  // over the key tiles of this split
+    col.clear();
+    copy(0, t0 + w);
+    copy(1, t0 + w + WAVES);
+    int u = 0;
+    for (int t = t0 + w; t < t1; t += WAVES) {
+      wait_vmem<2 * PER>();
+      const char* kb = ring + u * STEP;
+      f32x16 x[1];
+      col.logits(x, kb);
+      const int key0 = sp.key0(t);
+      if (!sp.open(key0)) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (!sp.sees(key0 + col.key(0, e), pos)) x[0][e] = -INFINITY;
+        for (int e = 0; e < 16; ++e)
+          if (!sp.sees(key0 + col.key(0, e), pos)) x[0][e] = -INFINITY;
+        if (careful.value) tame<BF16, PER>(ring + u * STEP + HALF + lane * 16);
+      }
+      bf16x8 pf[2], lo[2];
+      col.template weigh<1, true>(x, a.sc, pf, lo);
+      uint32_t at[2 * DT];
+#pragma unroll
+      for (int e = 0; e < 2 * DT; ++e) at[e] = lds_addr(kb) + HALF + col.voff[e];
+      s16x4 v0[2 * DT], v1[2 * DT];
+      vt_read<0>(at, v0);
+      vt_read<16 * D * 2>(at, v1);
+      // the ring slot is read out (the last statement waited): the next copy may start
+      copy(u, t + 2 * WAVES);
+      u ^= 1;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const bf16x8 a0 = join8(v0[2 * dt], v0[2 * dt + 1]), a1 = join8(v1[2 * dt], v1[2 * dt + 1]);
+        col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a0, pf[0], col.o[dt], 0, 0, 0);
+        col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1, pf[1], col.o[dt], 0, 0, 0);
+        col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a0, lo[0], col.o[dt], 0, 0, 0);
+        col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1, lo[1], col.o[dt], 0, 0, 0);
+      }
     }
-    bf16x8 pf[2], lo[2];
-    col.template weigh<1, true>(x, a.sc, pf, lo);
-    uint32_t at[2 * DT];
-#pragma unroll
-    for (int e = 0; e < 2 * DT; ++e) at[e] = lds_addr(kb) + HALF + col.voff[e];
-    s16x4 v0[2 * DT], v1[2 * DT];
-    vt_read<0>(at, v0);
-    vt_read<16 * D * 2>(at, v1);
-    // the ring slot is read out (the last statement waited): the next copy may start
-    copy(u, t + 2 * WAVES);
-    u ^= 1;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      const bf16x8 a0 = join8(v0[2 * dt], v0[2 * dt + 1]), a1 = join8(v1[2 * dt], v1[2 * dt + 1]);
-      col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a0, pf[0], col.o[dt], 0, 0, 0);
-      col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1, pf[1], col.o[dt], 0, 0, 0);
-      col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a0, lo[0], col.o[dt], 0, 0, 0);
-      col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1, lo[1], col.o[dt], 0, 0, 0);
-    }
-  }
-  wait_vmem<0>();
+    wait_vmem<0>();
+    if (careful.value)
+      each_wild<kPfFewKeys>(sp, t0 + w, t1, WAVES, [&](int key) { col.add_wild(v_of(key), sp.sees(key, pos)); });
+  };
+  pass(std::false_type{});
+  if (__builtin_expect(__any(col.wild_output()), false)) pass(std::true_type{});
   col.close();
   __syncthreads();
   // wave 1 hands its state to wave 0
