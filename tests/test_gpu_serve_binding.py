@@ -74,3 +74,44 @@ def test_every_misfit_is_named(gpu_lib):
             with pytest.raises(AssertionError, match="same strides"):
                 call(**{**args, "v_pool": other})
     torch.cuda.synchronize()
+
+
+def test_two_threads_at_once(gpu_lib):
+    """Calls of two threads, each with a stream and a workspace of its own: the same bits as
+    one after the other."""
+    import threading
+
+    import torch
+    kv = gpu_lib
+    g = torch.Generator(device="cuda").manual_seed(3)
+    cfg = kv.PagedConfig(2, 2, 8, 64, 16, 300, 140)
+    pools = [torch.randn((300, 2, 16, 64), generator=g, device="cuda").bfloat16() for _ in range(2)]
+    table = torch.randperm(300, generator=g, device="cuda")[:280].int().view(2, 140).contiguous()
+    lens = torch.tensor([2200, 900], dtype=torch.int32, device="cuda")
+    qs = [torch.randn((2, 8, 64), generator=g, device="cuda").bfloat16() for _ in range(2)]
+    size = kv.kvec_paged_decode_workspace_size(cfg)
+    ws = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    wants = []
+    for q, w in zip(qs, ws):
+        wants.append(torch.empty((2, 8, 64), device="cuda"))
+        kv.kvec_paged_decode(cfg, q, *pools, table, lens, wants[-1], w)
+    torch.cuda.synchronize()
+    outs = [[torch.empty((2, 8, 64), device="cuda") for _ in range(200)] for _ in range(2)]
+    torch.cuda.synchronize()
+    errors = []
+
+    def work(i):
+        try:
+            stream = torch.cuda.Stream()
+            for o in outs[i]:
+                kv.kvec_paged_decode(cfg, qs[i], *pools, table, lens, o, ws[i], stream=stream)
+            stream.synchronize()
+        except Exception as e:  # noqa: BLE001
+            errors.append(e)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
+    assert all(o.equal(w) for i, w in enumerate(wants) for o in outs[i])
