@@ -105,7 +105,8 @@ __device__ __forceinline__ bool pf_item(const PfArgs& a, int* bh, int* tile, int
 // the 16x16x4 f32 product; tiles of 32 keys in two LDS buffers.  With KW = 2 four more
 // waves take every other tile, and the states meet in LDS.  Bound by that
 // product's rate (a sixteenth of the bf16 one's) and the softmax between two products:
-// 4000 rows of 8 query and 4 KV heads, d 64, in 180 us, 91 TFLOP/s of 153.
+// 4000 rows of 8 query and 4 KV heads, d 64, in 183 us, 90 TFLOP/s of 153; which of LDS
+// reads, product chains or occupancy keeps the two from overlapping more is not known.
 template <int D, int KW>
 __global__ __launch_bounds__(kPfThreads * KW) void pf_rows16(PfArgs a) {
   using TT = F32;
@@ -602,8 +603,9 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void pf_rows32(PfArgs a) { rows32<
 // same ones.  The waves go over the 32-key steps of the work-group's split in
 // turn, each with an LDS ring of two steps of its own and no barrier before the
 // end, where their states are joined.  What bounds it is the latency and the reading
-// of K and V (8 rows of 32 heads over 16k keys: 18 us, 3.7 TB/s), so the probabilities
-// go into the product as two bf16 terms.
+// of K and V (8 rows of 32 heads over 16k keys: 18 us, 3.7 TB/s, where one token's
+// attention over a paged cache reads as many bytes in 14 to 15), so the probabilities go
+// into the product as two bf16 terms.
 __device__ __forceinline__ void few(const PfArgs& a) {
   constexpr int D = 128, ES = 2, DT = D / 32, WAVES = kPfFewThreads / 64;
   constexpr int HALF = kPfFewKeys * D * 2, STEP = 2 * HALF, PER = HALF / 1024;
