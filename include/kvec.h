@@ -538,7 +538,8 @@ kvec_status kvec_paged_evict_workspace_size(const kvec_paged_config* cfg, int32_
  * slots below the budget stay where they are; the i-th kept slot behind it, in
  * ascending order, moves (K, V, acc, pos) to the i-th evicted slot below it.  So
  * no more rows move than were evicted.  Other sequences keep everything.  Slots
- * behind the budget are left as they are, their pages are free.
+ * behind the budget are left as they are, their pages are free.  A slot below the
+ * budget that has no page ranks last and takes nothing: what would move there is lost.
  *   budget      slots kept per head, 1..2^20.
  *   window, n_sinks   >= 0, window + n_sinks <= budget.
  *   lens        device int32 [batch] (taken into 0..max_len).
