@@ -37,6 +37,11 @@
  *                     rotated and written into it; one token's attention over
  *                     it, which also accumulates the weight every slot
  *                     receives; its eviction by that accumulated weight.
+ *   kvec_paged_decode_shared
+ *                     the same attention for a batch behind one common prefix.
+ *   kvec_paged_append_q8, kvec_paged_read_q8, kvec_paged_decode_q8,
+ *   kvec_paged_evict_q8
+ *                     the same cache in eight bits, and its rows read back.
  *   kvec_score_lse, kvec_evict_model_lse
  *                     the same scores and step when the caller already holds
  *                     the softmax normaliser of every window row: K-VEC runs
@@ -559,6 +564,132 @@ kvec_status kvec_paged_evict(const kvec_paged_config* cfg, int32_t budget,
                              const int32_t* n_seen, int32_t max_len,
                              float* acc, int32_t* pos, int32_t* kept, int32_t* lens_out,
                              void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Workspace bytes of kvec_paged_decode_shared (host-only). */
+kvec_status kvec_paged_decode_shared_workspace_size(const kvec_paged_config* cfg, int32_t max_prefix,
+                                                    int32_t max_len, int32_t with_acc, size_t* bytes);
+
+/* kvec_paged_decode for a batch whose sequences begin with the same slots: sequence b is
+ * the P = prefix_len[0] slots of the prefix and, behind them, the n = lens[b] slots of its
+ * row of page_table.  The prefix's K and V are read once for all sequences.  Window and
+ * sinks count from the prefix's first slot: of the P + n slots those >= P + n - window
+ * (window 0: all) or < n_sinks are visible.
+ *   prefix_pages  device int32 [n_prefix_pages], the prefix's pages in order (slot s: row
+ *               s % page_size of page s / page_size); n_prefix_pages * page_size <= 2^20.
+ *   prefix_len  device int32 [1] (taken into 0..max_prefix).
+ *   max_prefix  host bound of it, 1..n_prefix_pages * page_size; sizes the work.
+ *   page_table, lens, max_len  as for kvec_paged_decode, of the slots behind the prefix.
+ *               A sequence of length 0 sees the prefix alone; a row with a negative
+ *               length is none (the padding of a batch): it sees nothing, whatever its
+ *               query holds.
+ *   acc         nullable device in/out: a slot behind the prefix as in kvec_paged_decode;
+ *               a slot of the prefix takes the sum over the sequences (always the same
+ *               bits).  The prefix is cut by its weights with kvec_paged_evict, as one
+ *               sequence.
+ *   ws          device workspace of kvec_paged_decode_shared_workspace_size() bytes.
+ * The others as for kvec_paged_decode, also for what masked slots hold and for logits
+ * that are no numbers (a NaN or +infinity among a row's logits makes the weights that it
+ * adds NaN).  With acc a page must have one place, in the prefix or in one row of the
+ * table.  batch * n_q_heads must be below 2^20 (KVEC_ERR_UNSUPPORTED). */
+kvec_status kvec_paged_decode_shared(const kvec_paged_config* cfg,
+                                     const void* q, const int64_t q_strides[2],
+                                     const void* k_pool, const void* v_pool,
+                                     const int64_t pool_strides[3],
+                                     const int32_t* prefix_pages, int32_t n_prefix_pages,
+                                     const int32_t* prefix_len, int32_t max_prefix,
+                                     const int32_t* page_table, const int32_t* lens, int32_t max_len,
+                                     int32_t window, int32_t n_sinks,
+                                     float* out, float* lse, float* acc,
+                                     void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * A paged cache in eight bits
+ *
+ * As the paged cache above, but the pools hold one byte an element and every row (a
+ * token's key or value of one head) has a scale:
+ *   k_scale, v_scale  fp32 [n_pages][H][page_size], contiguous.
+ * The row y of d elements is held as codes c_i and a scale z >= 2^-126, and stands for
+ * c_i * z:
+ *   z = max(fl(max_i |y_i| / M), 2^-126),   c_i = round(fl(y_i / z)),
+ * fl a rounding to float32, round to the nearest code, ties to the even one, with
+ *   KVEC_Q8_INT8  codes int8, M = 127: off by at most 1 / 254 of the row's largest value;
+ *   KVEC_Q8_E4M3  codes in 8 bits of floating point (1 sign, 4 exponent, 3 mantissa bits, no
+ *                 infinity), M = 448: off by at most 2^-4 relative, or 2^-10 z.
+ * A row with a NaN or an infinity is held as codes 0 and a NaN scale: all of it reads as
+ * NaN.  Pool strides are in elements (bytes), multiples of 16.
+ * ------------------------------------------------------------------------- */
+
+typedef enum kvec_q8_format {
+  KVEC_Q8_INT8 = 0,
+  KVEC_Q8_E4M3 = 1
+} kvec_q8_format;
+
+typedef struct kvec_paged_q8_config {
+  kvec_paged_config paged; /* dtype: of q, of new keys and values, and of rows read back */
+  int32_t format;          /* kvec_q8_format of the pools */
+} kvec_paged_q8_config;
+
+/* kvec_paged_append into a cache in eight bits: keys (normed and rotated in float32, not
+ * rounded before) and values are quantised as they are written, with their scales.  Everything
+ * else, q_out too, as there. */
+kvec_status kvec_paged_append_q8(const kvec_paged_q8_config* cfg, int32_t n_tokens,
+                                 const void* q, const int64_t q_strides[2],
+                                 const void* k, const int64_t k_strides[2],
+                                 const void* v, const int64_t v_strides[2],
+                                 const void* q_weight, const void* k_weight, float eps,
+                                 const int32_t* positions, const double* inv_freq, int32_t rot_dim,
+                                 const int64_t* slots,
+                                 void* q_out, const int64_t q_out_strides[2],
+                                 void* k_pool, void* v_pool, const int64_t pool_strides[3],
+                                 float* k_scale, float* v_scale,
+                                 float* acc, int32_t* pos, hipStream_t stream);
+
+/* The rows that a cache in eight bits stands for, sequence by sequence, as the prompt
+ * attention of a further chunk takes them.
+ *   page_table, lens  as for kvec_paged_decode.
+ *   max_len     rows per sequence of k_out and v_out, 1..max_pages * page_size.
+ *   k_out, v_out  device out, paged.dtype [batch][H][max_len][d], strides {batch, head, row}:
+ *               slot s < lens[b] in row s, c_i * z rounded once; zeros for a slot that has no
+ *               page.  Rows s >= lens[b] are left as they are.  Neither may overlap the
+ *               other or the cache.
+ * No workspace. */
+kvec_status kvec_paged_read_q8(const kvec_paged_q8_config* cfg,
+                               const void* k_pool, const void* v_pool,
+                               const int64_t pool_strides[3],
+                               const float* k_scale, const float* v_scale,
+                               const int32_t* page_table, const int32_t* lens, int32_t max_len,
+                               void* k_out, const int64_t k_out_strides[3],
+                               void* v_out, const int64_t v_out_strides[3], hipStream_t stream);
+
+/* Workspace bytes of kvec_paged_decode_q8 (host-only). */
+kvec_status kvec_paged_decode_q8_workspace_size(const kvec_paged_q8_config* cfg, int32_t max_len,
+                                                int32_t with_acc, size_t* bytes);
+
+/* kvec_paged_decode over a cache in eight bits: of the rows that it stands for, unrounded. */
+kvec_status kvec_paged_decode_q8(const kvec_paged_q8_config* cfg,
+                                 const void* q, const int64_t q_strides[2],
+                                 const void* k_pool, const void* v_pool,
+                                 const int64_t pool_strides[3],
+                                 const float* k_scale, const float* v_scale,
+                                 const int32_t* page_table, const int32_t* lens, int32_t max_len,
+                                 int32_t window, int32_t n_sinks,
+                                 float* out, float* lse, float* acc,
+                                 void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Workspace bytes of kvec_paged_evict_q8 (host-only). */
+kvec_status kvec_paged_evict_q8_workspace_size(const kvec_paged_q8_config* cfg, int32_t max_len,
+                                               int32_t budget, size_t* bytes);
+
+/* kvec_paged_evict of a cache in eight bits: a slot's scales move with its codes, which stay
+ * as they are. */
+kvec_status kvec_paged_evict_q8(const kvec_paged_q8_config* cfg, int32_t budget,
+                                int32_t window, int32_t n_sinks,
+                                void* k_pool, void* v_pool, const int64_t pool_strides[3],
+                                float* k_scale, float* v_scale,
+                                const int32_t* page_table, const int32_t* lens,
+                                const int32_t* n_seen, int32_t max_len,
+                                float* acc, int32_t* pos, int32_t* kept, int32_t* lens_out,
+                                void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* Static description of a status code. */
 const char* kvec_status_string(kvec_status status);

@@ -20,6 +20,8 @@ SOURCES = [("kvec_api.hip", "kvec_api", []), ("kvec_pipeline.hip", "kvec_pipelin
            ("kvec_decode.hip", "kvec_decode", []), ("kvec_serve_api.hip", "kvec_serve_api", []),
            ("kvec_prefill.hip", "kvec_prefill", []), ("kvec_append.hip", "kvec_append", []),
            ("kvec_paged_decode.hip", "kvec_paged_decode", []),
+           ("kvec_paged_decode_q8.hip", "kvec_paged_decode_q8", []),
+           ("kvec_paged_shared.hip", "kvec_paged_shared", []), ("kvec_paged_read.hip", "kvec_paged_read", []),
            ("kvec_paged_evict.hip", "kvec_paged_evict", [])] + [
     ("kvec_step_inst.hip", f"kvec_step_{tt.lower()}_d{d}{'_long' if long == 'true' else ''}",
      [f"-DKVEC_INST_TT={tt}", f"-DKVEC_INST_D={d}", f"-DKVEC_INST_LONG={long}"])

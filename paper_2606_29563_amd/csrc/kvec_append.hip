@@ -1,5 +1,6 @@
 // New tokens into the paged cache: per-head RMS norm of queries and keys, the
-// rotation by position, and the write of K and V rows, in one pass.
+// rotation by position, and the write of K and V rows, in one pass, into pools of their
+// type or, quantised, into a cache in eight bits.
 //
 // Bound by memory: every row is read and written once (2 * (HQ + 2H) * d
 // elements a token).  A row is D/16 lanes of a wave; a lane holds the two
@@ -10,7 +11,7 @@
 // token and frequency, kept in LDS for all the token's heads.
 #include <math.h>
 
-#include "kvec_score_dev.h"
+#include "kvec_q8_dev.h"
 #include "kvec_serve.h"
 
 namespace kvec {
@@ -62,7 +63,8 @@ struct Piece<float> {
   }
 };
 
-template <class T, int D>
+// FORMAT: kvec_q8_format of the pools, or kPlain.
+template <class T, int D, int FORMAT>
 __global__ __launch_bounds__(kAppThreads) void append_kernel(PagedView c, AppendArgs a, int tok) {
   constexpr int LPR = D / 16;            // lanes per row
   constexpr int RPR = kAppThreads / LPR;  // rows per round of the work-group
@@ -102,10 +104,12 @@ __global__ __launch_bounds__(kAppThreads) void append_kernel(PagedView c, Append
     x0.load(src, p0);
     x1.load(src, p1);
     const char* w = is_q ? a.wq : a.wk;
-    if (!is_v && (w || rot)) {
-      float f0[8], f1[8];
+    float f0[8], f1[8];
+    if (FORMAT != kPlain || (!is_v && (w || rot))) {
       x0.get(f0);
       x1.get(f1);
+    }
+    if (!is_v && (w || rot)) {
       if (w) {
         float ss = 0.f;
 #pragma unroll
@@ -136,8 +140,15 @@ __global__ __launch_bounds__(kAppThreads) void append_kernel(PagedView c, Append
           f1[e] = hi * z.x + lo * z.y;
         }
       }
-      x0.set(f0);
-      x1.set(f1);
+      if (FORMAT == kPlain || is_q) {
+        x0.set(f0);
+        x1.set(f1);
+      }
+    }
+    uint2 c0, c1;
+    float scale;
+    if constexpr (FORMAT != kPlain) {
+      if (!is_q) scale = quantise<FORMAT, LPR>(f0, f1, c0, c1);  // (as the norm: by all lanes of the row)
     }
     if (!live) continue;
     if (is_q) {
@@ -149,11 +160,17 @@ __global__ __launch_bounds__(kAppThreads) void append_kernel(PagedView c, Append
       if (slot < 0 || slot >= n_slots) continue;
       const int64_t page = slot / c.ps;
       const int row = (int)(slot - page * c.ps);
-      char* dst = (is_v ? c.v : c.k) + (page * c.sp + h * c.sh + row * c.sr) * sizeof(T);
-      x0.store(dst, p0);
-      x1.store(dst, p1);
+      char* dst = (is_v ? c.v : c.k) + (page * c.sp + h * c.sh + row * c.sr) * (FORMAT == kPlain ? sizeof(T) : 1);
+      const int64_t at = (page * c.H + h) * c.ps + row;
+      if constexpr (FORMAT == kPlain) {
+        x0.store(dst, p0);
+        x1.store(dst, p1);
+      } else {
+        reinterpret_cast<uint2*>(dst)[p0] = c0;
+        reinterpret_cast<uint2*>(dst)[p1] = c1;
+        if (l == 0) (is_v ? c.vs : c.ks)[at] = scale;
+      }
       if (!is_v && l == 0) {
-        const int64_t at = (page * c.H + h) * c.ps + row;
         if (a.acc) a.acc[at] = 0.f;
         if (a.pos) a.pos[at] = a.positions[n];
       }
@@ -171,13 +188,19 @@ hipError_t run_append(const PagedView& c, const AppendArgs& a, hipStream_t s) {
   if (a.n == 0) return hipSuccess;
   const int tok = a.n < 1536 ? 1 : kAppMaxTok;
   const dim3 grid((unsigned)((a.n + tok - 1) / tok));
-  if (c.esize == 2) {
-    if (c.D == 64) hipLaunchKernelGGL((append_kernel<__bf16, 64>), grid, dim3(kAppThreads), 0, s, c, a, tok);
-    else hipLaunchKernelGGL((append_kernel<__bf16, 128>), grid, dim3(kAppThreads), 0, s, c, a, tok);
-  } else {
-    if (c.D == 64) hipLaunchKernelGGL((append_kernel<float, 64>), grid, dim3(kAppThreads), 0, s, c, a, tok);
-    else hipLaunchKernelGGL((append_kernel<float, 128>), grid, dim3(kAppThreads), 0, s, c, a, tok);
-  }
+  auto launch = [&](auto format) {
+    constexpr int F = decltype(format)::value;
+    if (c.esize == 2) {
+      if (c.D == 64) hipLaunchKernelGGL((append_kernel<__bf16, 64, F>), grid, dim3(kAppThreads), 0, s, c, a, tok);
+      else hipLaunchKernelGGL((append_kernel<__bf16, 128, F>), grid, dim3(kAppThreads), 0, s, c, a, tok);
+    } else {
+      if (c.D == 64) hipLaunchKernelGGL((append_kernel<float, 64, F>), grid, dim3(kAppThreads), 0, s, c, a, tok);
+      else hipLaunchKernelGGL((append_kernel<float, 128, F>), grid, dim3(kAppThreads), 0, s, c, a, tok);
+    }
+  };
+  if (!c.ks) launch(std::integral_constant<int, kPlain>{});
+  else if (c.format == KVEC_Q8_INT8) launch(std::integral_constant<int, KVEC_Q8_INT8>{});
+  else launch(std::integral_constant<int, KVEC_Q8_E4M3>{});
   return hipGetLastError();
 }
 

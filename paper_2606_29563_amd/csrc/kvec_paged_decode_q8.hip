@@ -1,0 +1,367 @@
+// One new token's attention over a paged cache in eight bits.
+//
+// A key stands for z k with whole or eight-bit floating codes k, so its logit is z times
+// the product of the query with the codes, and a value's scale goes into its probability:
+//   x_s = zk_s (q . k_s) / sqrt(d),   out = sum_s (p_s zv_s) v_s.
+// Codes are exact in bf16, so the products are those of kvec_paged_decode.hip's bf16 path;
+// float32 queries enter as three bf16 terms, 24 bits.  Probabilities enter the V product as
+// two bf16 terms (three with float32 queries).
+//
+// Bound by reading the visible rows once, half the bytes of bf16 ones.  The launches
+// are those of kvec_paged_decode.hip, the second the same one; here a step of a wave is 32
+// slots, two groups of 16: as many bytes as there, and the reduction of a 16x16x32
+// product.  A K fragment is a 16-byte piece, 16 codes, of a row: two steps of the
+// reduction over d, whose order the query follows.  V comes through the transposing LDS
+// read for bytes: in a group of 16 lanes, lane i gives the address of elements 8 (i % 2) ..
+// + 7 of row i / 2 and receives element i of the eight rows.  The eight rows of lane group
+// c are those whose logits it holds, 4c .. 4c + 3 of both groups.
+#include "kvec_paged_dev.h"
+#include "kvec_q8_dev.h"
+
+namespace kvec {
+namespace {
+
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// 16 rows of D codes in LDS: piece p of row r at position p ^ swizzle(r), so that the
+// fragments' reads fall in distinct banks.
+template <int D>
+struct CodeGroup {
+  static constexpr int CPR = D / 16, BYTES = 16 * D, NI = BYTES / 1024, RPI = 64 / CPR;
+  static __device__ __forceinline__ int swizzle(int r) { return D == 128 ? r >> 1 & 7 : (r ^ r >> 2) & 3; }
+};
+
+// Reads of K and the transposing ones of V, written out with the wait in the same
+// statement: for those that the compiler issues it waits for every copy in flight first (it
+// cannot tell the addresses apart), which would stop the copies of the next step.
+// Two pieces (four) of the two groups, OFF bytes apart.
+template <int OFF>
+__device__ __forceinline__ void k_read(const uint32_t (&at)[1], u32x4 (&u)[2][1]) {
+  asm volatile(
+      "ds_read_b128 %0, %2\n\t"
+      "ds_read_b128 %1, %2 offset:%3\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(u[0][0]), "=&v"(u[1][0])
+      : "v"(at[0]), "n"(OFF)
+      : "memory");
+}
+template <int OFF>
+__device__ __forceinline__ void k_read(const uint32_t (&at)[2], u32x4 (&u)[2][2]) {
+  asm volatile(
+      "ds_read_b128 %0, %4\n\t"
+      "ds_read_b128 %1, %5\n\t"
+      "ds_read_b128 %2, %4 offset:%6\n\t"
+      "ds_read_b128 %3, %5 offset:%6\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(u[0][0]), "=&v"(u[0][1]), "=&v"(u[1][0]), "=&v"(u[1][1])
+      : "v"(at[0]), "v"(at[1]), "n"(OFF)
+      : "memory");
+}
+__device__ __forceinline__ void vt_read8(const uint32_t (&at)[4], i32x2 (&v)[4]) {
+  asm volatile(
+      "ds_read_b64_tr_b8 %0, %4\n\t"
+      "ds_read_b64_tr_b8 %1, %5\n\t"
+      "ds_read_b64_tr_b8 %2, %6\n\t"
+      "ds_read_b64_tr_b8 %3, %7\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+      : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3])
+      : "memory");
+}
+__device__ __forceinline__ void vt_read8(const uint32_t (&at)[8], i32x2 (&v)[8]) {
+  asm volatile(
+      "ds_read_b64_tr_b8 %0, %8\n\t"
+      "ds_read_b64_tr_b8 %1, %9\n\t"
+      "ds_read_b64_tr_b8 %2, %10\n\t"
+      "ds_read_b64_tr_b8 %3, %11\n\t"
+      "ds_read_b64_tr_b8 %4, %12\n\t"
+      "ds_read_b64_tr_b8 %5, %13\n\t"
+      "ds_read_b64_tr_b8 %6, %14\n\t"
+      "ds_read_b64_tr_b8 %7, %15\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7])
+      : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]), "v"(at[7])
+      : "memory");
+}
+
+// A float as the sum of N bf16 terms.
+template <int N>
+__device__ __forceinline__ void terms(float x, __bf16 (&t)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    t[i] = (__bf16)x;
+    x -= (float)t[i];
+  }
+}
+
+// Softmax state and output of 16 query columns over 32 codes' rows a step.  NQ, NP: bf16
+// terms of a query's element and of a probability.
+template <int D, int FORMAT, int NQ>
+struct Columns16Q8 {
+  using CG = CodeGroup<D>;
+  static constexpr int DT = D / 16, KP = D / 64, NP = NQ == 1 ? 2 : 3;
+  bf16x8 q[NQ][2 * KP];
+  float m, l;
+  f32x4 o[DT];
+
+  __device__ __forceinline__ void clear() {
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int t = 0; t < DT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NQ; ++i)
+#pragma unroll
+      for (int j = 0; j < 2 * KP; ++j) q[i][j] = __builtin_bit_cast(bf16x8, make_uint4(0, 0, 0, 0));
+  }
+  // Step 2 m + s of the reduction: elements 8 s .. + 7 of the 16-element piece c + 4 m.
+  __device__ __forceinline__ void load(const char* row, int c) {
+#pragma unroll
+    for (int j = 0; j < 2 * KP; ++j) {
+      const int at = 2 * (c + 4 * (j >> 1)) + (j & 1);
+      if constexpr (NQ == 1) {
+        q[0][j] = __builtin_bit_cast(bf16x8, reinterpret_cast<const uint4*>(row)[at]);
+      } else {
+        const float4 a = reinterpret_cast<const float4*>(row)[2 * at], b = reinterpret_cast<const float4*>(row)[2 * at + 1];
+        const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          __bf16 t[NQ];
+          terms(f[e], t);
+#pragma unroll
+          for (int i = 0; i < NQ; ++i) q[i][j][e] = t[i];
+        }
+      }
+    }
+  }
+
+  // Products with the codes of the two groups at `grp`; lane: keys 4c + i of each.
+  __device__ __forceinline__ void logits(f32x4 (&x)[2], const char* grp, int lane) const {
+    const int n = lane & 15, c = lane >> 4;
+    uint32_t at[KP];
+    u32x4 u[2][KP];
+#pragma unroll
+    for (int p = 0; p < KP; ++p) at[p] = lds_addr(grp) + n * D + (((c + 4 * p) ^ CG::swizzle(n)) << 4);
+    k_read<CG::BYTES>(at, u);
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      x[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int p = 0; p < KP; ++p) {
+        const bf16x8 k0 = Codes<FORMAT>::bf16(u[g][p][0], u[g][p][1]), k1 = Codes<FORMAT>::bf16(u[g][p][2], u[g][p][3]);
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+          x[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[i][2 * p], x[g], 0, 0, 0);
+          x[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[i][2 * p + 1], x[g], 0, 0, 0);
+        }
+      }
+    }
+  }
+
+  // One step of the online softmax (see Columns16): x base-2 logits, -inf where masked;
+  // z the values' scales, 0 where masked.
+  __device__ __forceinline__ void absorb(const f32x4 (&x)[2], const f32x4 (&z)[2], const char* vgrp, int lane) {
+    float mx = m;
+#pragma unroll
+    for (int g = 0; g < 2; ++g) mx = fmaxf(mx, fmaxf(fmaxf(x[g][0], x[g][1]), fmaxf(x[g][2], x[g][3])));
+    mx = col_max4(mx);
+    const float ref = mx == -INFINITY ? 0.f : mx;
+    const float f = __builtin_amdgcn_exp2f(m - ref);
+    m = mx;
+    l *= f;
+    bf16x8 p[NP];
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float e = __builtin_amdgcn_exp2f(x[g][i] - ref);
+        l += e;
+        __bf16 t[NP];
+        terms(e * z[g][i], t);
+#pragma unroll
+        for (int j = 0; j < NP; ++j) p[j][4 * g + i] = t[j];
+      }
+    if (__any(f != 1.f)) {
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[t][i] *= f;
+    }
+    const int n = lane & 15, c = lane >> 4, r = 4 * c + (n >> 1 & 3);
+    uint32_t at[DT];
+    const uint32_t base = lds_addr(vgrp) + (n >> 3) * CG::BYTES + r * D + (n & 1) * 8;
+#pragma unroll
+    for (int t = 0; t < DT; ++t) at[t] = base + ((t ^ CG::swizzle(r)) << 4);
+    i32x2 v[DT];
+    vt_read8(at, v);
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      const bf16x8 a = Codes<FORMAT>::bf16((uint32_t)v[t][0], (uint32_t)v[t][1]);
+#pragma unroll
+      for (int j = 0; j < NP; ++j) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[j], o[t], 0, 0, 0);
+    }
+  }
+};
+
+constexpr int kQ8Ring = 2;  // steps in flight per wave
+
+template <int D>
+constexpr int kQ8Step = 4 * CodeGroup<D>::BYTES;  // K rows, then V rows of two groups
+
+// ONE: the sequence is not split, its work-group finishes the results itself.
+template <int D, int FORMAT, int NQ, bool ONE>
+__device__ __forceinline__ void partial_q8(const PdArgs& a, char* smem, int s, int h, int b) {
+  using CG = CodeGroup<D>;
+  constexpr int QS = NQ == 1 ? 2 : 4;
+  constexpr int STEP = kQ8Step<D>, LOADS = 4 * CG::NI + 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int n = lane & 15, c = lane >> 4, G = a.c.G;
+  const Visible vis(a, b);
+  const int pairs = (vis.groups + 1) / 2, per = (pairs + a.So - 1) / a.So;
+  const int st0 = min(s * per, pairs), st1 = min(st0 + per, pairs);
+
+  Columns16Q8<D, FORMAT, NQ> col;
+  col.clear();
+  if (n < G) col.load(a.q + ((int64_t)b * a.qs_b + (int64_t)(h * G + n) * a.qs_h) * QS, c);
+
+  int voff[CG::NI], rowi[CG::NI];
+#pragma unroll
+  for (int i = 0; i < CG::NI; ++i) {
+    rowi[i] = i * CG::RPI + lane / CG::CPR;
+    voff[i] = rowi[i] * (int)a.c.sr + ((lane % CG::CPR) ^ CG::swizzle(rowi[i])) * 16;
+  }
+  const int extent = 15 * (int)a.c.sr + D;
+  char* ring = smem + w * kQ8Ring * STEP;
+
+  // The wave's steps are st0 + w, st0 + w + 4, ...: number k of them, groups 2 i and 2 i + 1
+  // of step i.  Lane l holds the page entry of group l % 2 of number 32 * (k / 32) + l / 2.
+  const int first = st0 + w, count = (st1 - first + kPdWaves - 1) / kPdWaves;
+  int entry = 0, entry_row = 0;
+  auto group_of = [&](int k, int g) { return 2 * (first + k * kPdWaves) + g; };
+  auto lookup = [&](int k) {
+    const int vg = min(group_of(k + (lane >> 1), lane & 1), vis.groups - 1);
+    entry = page_of(a, b, vis.slot0(vg), &entry_row);
+    asm volatile("" : "+v"(entry));  // waited for here, not at every use in the loop
+  };
+  bool whole[kQ8Ring][2];  // every slot of the group in the ring slot is visible
+  bool ok[kQ8Ring][2];     // ... is one, and lies in a page
+  f32x4 zk[kQ8Ring][2], zv[kQ8Ring][2];  // scales of the lane's keys and of their values
+  auto copy = [&](auto U, int k) {
+    constexpr int u = decltype(U)::value;
+    if ((k & 31) == 0) lookup(k);
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int from = 2 * (k & 31) + g;
+      const int page = __builtin_amdgcn_readlane(entry, from), row0 = __builtin_amdgcn_readlane(entry_row, from);
+      const int vg = group_of(k, g), slot0 = vis.slot0(vg);
+      ok[u][g] = k < count && vg < vis.groups && page_ok(a, page);
+      whole[u][g] = ok[u][g] && slot0 + 16 <= vis.n && (slot0 >= vis.lo || slot0 + 16 <= vis.sinks);
+      const int64_t base = ok[u][g] ? (int64_t)page * a.c.sp + (int64_t)h * a.c.sh + (int64_t)row0 * a.c.sr : 0;
+      // (of a group that is not there the scales of some slots of the pool)
+      const int64_t meta = (ok[u][g] ? ((int64_t)page * a.c.H + h) * a.c.ps + row0 : 0) + 4 * c;
+      zk[u][g] = *reinterpret_cast<const f32x4_any*>(a.c.ks + meta);
+      zv[u][g] = *reinterpret_cast<const f32x4_any*>(a.c.vs + meta);
+      const auto kr = __builtin_amdgcn_make_buffer_rsrc(a.c.k + base, 0, ok[u][g] ? extent : 0, kBufferWord3);
+      const auto vr = __builtin_amdgcn_make_buffer_rsrc(a.c.v + base, 0, ok[u][g] ? extent : 0, kBufferWord3);
+      auto* dk = (__attribute__((address_space(3))) char*)(ring + u * STEP + g * CG::BYTES);
+      auto* dv = (__attribute__((address_space(3))) char*)(ring + u * STEP + (2 + g) * CG::BYTES);
+#pragma unroll
+      for (int i = 0; i < CG::NI; ++i) {
+        const int off = whole[u][g] || vis.sees(slot0 + rowi[i]) ? voff[i] : kOutOfRange;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, dk + i * 1024, 16, off, 0, 0, 2);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, dv + i * 1024, 16, off, 0, 0, 2);
+      }
+    }
+  };
+  float* lg = a.logits && n < G ? a.logits + (((int64_t)b * a.c.H + h) * G + n) * a.pad + 4 * c : nullptr;
+  auto step = [&](auto U, int k) {
+    constexpr int u = decltype(U)::value;
+    wait_vmem<(kQ8Ring - 1) * LOADS>();
+    const char* slot = ring + u * STEP;
+    f32x4 x[2];
+    col.logits(x, slot, lane);
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int s0 = vis.slot0(group_of(k, g));
+      x[g] *= zk[u][g] * a.sc;
+      if (!whole[u][g]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!(ok[u][g] && vis.sees(s0 + 4 * c + i))) {
+            x[g][i] = -INFINITY;
+            zv[u][g][i] = 0.f;
+          }
+      }
+      if (lg && group_of(k, g) < vis.groups) *reinterpret_cast<f32x4*>(lg + s0) = x[g];
+    }
+    col.absorb(x, zv[u], slot + 2 * CG::BYTES, lane);
+    // the ring slot is read out before the next copy into it starts
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    copy(U, k + kQ8Ring);
+  };
+  if (count > 0) {
+    copy(std::integral_constant<int, 0>{}, 0);
+    copy(std::integral_constant<int, 1>{}, 1);
+    // always both: on a way round the loop with one copy less the compiler would wait for
+    // the scales as if there were none behind them
+    int k = 0;
+    for (; k + 1 < count; k += kQ8Ring) {
+      step(std::integral_constant<int, 0>{}, k);
+      step(std::integral_constant<int, 1>{}, k + 1);
+    }
+    if (k < count) step(std::integral_constant<int, 0>{}, k);
+  }
+  wait_vmem<0>();
+  finish<D, ONE>(a, vis, col, smem, s, h, b);
+}
+
+template <int D, int FORMAT, int NQ, bool ONE>
+__global__ __launch_bounds__(kPdThreads) void pd_partial_q8(PdArgs a) {
+  constexpr int RING = kPdWaves * kQ8Ring * kQ8Step<D>;
+  __shared__ __align__(1024) char smem[RING > kPdMerge<D> ? RING : kPdMerge<D>];
+  partial_q8<D, FORMAT, NQ, ONE>(a, smem, blockIdx.x, blockIdx.y, blockIdx.z);
+}
+
+template <int D, int FORMAT, int NQ>
+hipError_t launch(const PdArgs& a, hipStream_t s) {
+  const dim3 grid(a.S, a.c.H, a.c.batch);
+  if (a.S == 1) {
+    hipLaunchKernelGGL((pd_partial_q8<D, FORMAT, NQ, true>), grid, dim3(kPdThreads), 0, s, a);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((pd_partial_q8<D, FORMAT, NQ, false>), grid, dim3(kPdThreads), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : pd_join<D>(a, s);
+}
+
+}  // namespace
+
+// Splits: as many work-groups as for rows of more bytes (paged_decode_plan); a wave's step
+// is twice as many slots.
+PagedDecodePlan paged_decode_q8_plan(const PagedView& c, int window, int sinks, bool acc) {
+  const int64_t bh = (int64_t)c.batch * c.H;
+  const int groups = most_groups(c, window, sinks);
+  auto per_bh = [&](int64_t work_groups) { return (work_groups + bh - 1) / bh; };
+  int64_t S = per_bh(1024);
+  if (S > groups / 64) S = groups / 64;
+  if (S < per_bh(256)) S = per_bh(256);
+  const int most_s = (groups + 2 * kPdWaves - 1) / (2 * kPdWaves);
+  if (S > most_s) S = most_s;
+  if (groups <= 16) S = 1;
+  return pd_plan(c, S < 1 ? 1 : S, acc);
+}
+
+hipError_t run_paged_decode_q8(const PagedView& c, const void* q, const int64_t qs[2], int window, int sinks,
+                               float* out, float* lse, float* acc, char* ws, hipStream_t s) {
+  const PagedDecodePlan p = paged_decode_q8_plan(c, window, sinks, acc != nullptr);
+  const PdArgs a = pd_args(c, p, q, qs, window, sinks, out, lse, acc, ws);
+  auto of = [&](auto format) {
+    constexpr int F = decltype(format)::value;
+    if (c.esize == 2) return c.D == 64 ? launch<64, F, 1>(a, s) : launch<128, F, 1>(a, s);
+    return c.D == 64 ? launch<64, F, 3>(a, s) : launch<128, F, 3>(a, s);
+  };
+  return c.format == KVEC_Q8_INT8 ? of(std::integral_constant<int, KVEC_Q8_INT8>{}) : of(std::integral_constant<int, KVEC_Q8_E4M3>{});
+}
+
+}  // namespace kvec

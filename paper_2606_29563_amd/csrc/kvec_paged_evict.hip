@@ -12,7 +12,7 @@
 //           kept.  Kept slots behind B and evicted ones below it go to two lists
 //           in ascending order: a thread finds both in a run of neighbouring slots,
 //           one sum over the threads gives its places in the lists.
-//   move    pairs of the lists: K, V, acc and pos; bound by memory (113 MB to and fro in
+//   move    pairs of the lists: K, V, acc and pos, and the scales of a cache in eight bits; bound by memory (113 MB to and fro in
 //           25 to 27 us; 20 when the same rows move again, from the memory-side cache).
 #include "kvec_attn_dev.h"
 #include "kvec_serve.h"
@@ -92,7 +92,7 @@ __device__ __forceinline__ void move_rows(const EvArgs& a, int b, int h, int cou
     const int rs = s - ev_page_index(a, s) * a.c.ps, rd = d - ev_page_index(a, d) * a.c.ps;
     if (p == 0 && a.kept) a.kept[((int64_t)b * H + h) * a.B + d] = s;
     if (ps < 0 || pd < 0) continue;
-    const int64_t es = a.c.esize;
+    const int64_t es = a.c.psize;
     const int64_t from = (ps * a.c.sp + h * a.c.sh + rs * a.c.sr) * es, to = (pd * a.c.sp + h * a.c.sh + rd * a.c.sr) * es;
     const uint4 kx = reinterpret_cast<const uint4*>(a.c.k + from)[p];
     const uint4 vx = reinterpret_cast<const uint4*>(a.c.v + from)[p];
@@ -100,6 +100,10 @@ __device__ __forceinline__ void move_rows(const EvArgs& a, int b, int h, int cou
       const int64_t f = (ps * (int64_t)H + h) * a.c.ps + rs, t = (pd * (int64_t)H + h) * a.c.ps + rd;
       a.acc[t] = a.acc[f];
       a.pos[t] = a.pos[f];
+      if (a.c.ks) {
+        a.c.ks[t] = a.c.ks[f];
+        a.c.vs[t] = a.c.vs[f];
+      }
     }
     reinterpret_cast<uint4*>(a.c.k + to)[p] = kx;
     reinterpret_cast<uint4*>(a.c.v + to)[p] = vx;
@@ -347,14 +351,15 @@ hipError_t run_paged_evict(const PagedView& c, int budget, int window, int sinks
   a.src = reinterpret_cast<int32_t*>(ws);
   a.dst = reinterpret_cast<int32_t*>(ws + up256(bh * a.cap * 4));
   const dim3 grid(c.H, c.batch);
-  const int row = c.D * c.esize;
+  const int row = c.D * c.psize;
   // One launch where a work-group has few rows to move and no other reads what this one
   // writes: the lengths, unless they are replaced in place.  us with one launch / two, a
   // pass more in each, 8 heads with rows of 256 bytes and 1024 kept: of 1088 slots 9.9 / 12.3, of 1280 11.8 /
   // 12.3, of 1536 13.7 / 12.5; 32 sequences of 1280 14.1 / 15.8.
   auto apart = [&](const int32_t* in) { return lens_out + c.batch <= in || in + c.batch <= lens_out; };
   if (c.max_len <= kEvSmall && (int64_t)a.cap * row <= kEvMoveBytes && apart(c.lens) && apart(n_seen)) {
-    if (row == 128) hipLaunchKernelGGL((ev_select<kEvSmall, 1, 128>), grid, dim3(kEvThreads), 0, s, a);
+    if (row == 64) hipLaunchKernelGGL((ev_select<kEvSmall, 1, 64>), grid, dim3(kEvThreads), 0, s, a);
+    else if (row == 128) hipLaunchKernelGGL((ev_select<kEvSmall, 1, 128>), grid, dim3(kEvThreads), 0, s, a);
     else if (row == 256) hipLaunchKernelGGL((ev_select<kEvSmall, 1, 256>), grid, dim3(kEvThreads), 0, s, a);
     else hipLaunchKernelGGL((ev_select<kEvSmall, 1, 512>), grid, dim3(kEvThreads), 0, s, a);
     return hipGetLastError();
@@ -369,7 +374,8 @@ hipError_t run_paged_evict(const PagedView& c, int budget, int window, int sinks
   if (x > most) x = most;
   if (x < 1) x = 1;
   const dim3 mgrid((unsigned)x, c.H, c.batch);
-  if (row == 128) hipLaunchKernelGGL(ev_move<128>, mgrid, dim3(kMvThreads), 0, s, a);
+  if (row == 64) hipLaunchKernelGGL(ev_move<64>, mgrid, dim3(kMvThreads), 0, s, a);
+  else if (row == 128) hipLaunchKernelGGL(ev_move<128>, mgrid, dim3(kMvThreads), 0, s, a);
   else if (row == 256) hipLaunchKernelGGL(ev_move<256>, mgrid, dim3(kMvThreads), 0, s, a);
   else hipLaunchKernelGGL(ev_move<512>, mgrid, dim3(kMvThreads), 0, s, a);
   return hipGetLastError();

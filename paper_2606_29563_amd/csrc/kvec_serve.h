@@ -1,6 +1,7 @@
 // Host launchers of the prompt's attention and of the paged cache
-// (kvec_prefill.hip, kvec_append.hip, kvec_paged_decode.hip,
-// kvec_paged_evict.hip), called by the C ABI in kvec_serve_api.hip.
+// (kvec_prefill.hip, kvec_append.hip, kvec_paged_decode.hip, kvec_paged_decode_q8.hip,
+// kvec_paged_shared.hip, kvec_paged_read.hip, kvec_paged_evict.hip), called by the C ABI in
+// kvec_serve_api.hip.
 #pragma once
 
 #include "kvec_internal.h"
@@ -24,9 +25,11 @@ struct PagedView {
   int64_t sp, sh, sr;
   const int32_t* table;  // [batch][max_pages]
   const int32_t* lens;   // [batch]
-  int batch, H, HQ, G, D, esize;
+  int batch, H, HQ, G, D, esize, psize;  // bytes of an element of q, and of the pools
   int ps, n_pages, max_pages, max_len;
   GroupDiv gdiv;         // groups of 16 slots per page
+  float *ks, *vs;        // a cache in eight bits: its scales [page][H][row]
+  int format;            // ... and kvec_q8_format
 };
 
 struct AppendArgs {
@@ -54,6 +57,33 @@ struct PagedDecodePlan {
 PagedDecodePlan paged_decode_plan(const PagedView& c, int window, int sinks, bool acc);
 hipError_t run_paged_decode(const PagedView& c, const void* q, const int64_t qs[2], int window, int sinks,
                             float* out, float* lse, float* acc, char* ws, hipStream_t s);
+
+PagedDecodePlan paged_decode_q8_plan(const PagedView& c, int window, int sinks, bool acc);
+hipError_t run_paged_decode_q8(const PagedView& c, const void* q, const int64_t qs[2], int window, int sinks,
+                               float* out, float* lse, float* acc, char* ws, hipStream_t s);
+
+// What a batch's sequences begin with.
+struct SharedPrefix {
+  const int32_t* pages;
+  const int32_t* len;  // [1]
+  int n_pages, max_len;
+};
+struct SharedPlan {
+  int kernel;            // which prefix kernel
+  int tiles, Sp;         // its column tiles, and splits of the prefix
+  PagedDecodePlan own;   // of the sequences' own slots
+  size_t part, logits, norm;
+  size_t total() const { return part + logits + norm; }
+};
+SharedPlan shared_plan(const PagedView& c, int max_prefix, bool acc);
+hipError_t run_paged_shared(const PagedView& c, const SharedPrefix& p, const void* q, const int64_t qs[2], int window,
+                            int sinks, float* out, float* lse, float* acc, char* ws, hipStream_t s);
+
+struct ReadArgs {
+  char *k, *v;
+  int64_t ks[3], vs[3];  // element strides {batch, head, row}
+};
+hipError_t run_paged_read(const PagedView& c, const ReadArgs& a, hipStream_t s);
 
 size_t paged_evict_ws(const PagedView& c, int budget);
 hipError_t run_paged_evict(const PagedView& c, int budget, int window, int sinks, const int32_t* n_seen,

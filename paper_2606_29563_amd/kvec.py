@@ -17,6 +17,7 @@ BIND_PATH = os.path.join(HERE, "_kvec_bind.so")
 KVEC_OK, KVEC_ERR_INVALID, KVEC_ERR_UNSUPPORTED, KVEC_ERR_WORKSPACE, KVEC_ERR_DEVICE = range(5)
 KVEC_BF16, KVEC_F32 = 0, 1
 KVEC_HEADS_STD, KVEC_HEADS_ENTROPY = 0, 1
+KVEC_Q8_INT8, KVEC_Q8_E4M3 = 0, 1
 
 
 class KvecError(RuntimeError):
@@ -94,6 +95,10 @@ class kvec_paged_config(ctypes.Structure):
                                               "page_size", "n_pages", "max_pages", "dtype")]
 
 
+class kvec_paged_q8_config(ctypes.Structure):
+    _fields_ = [("paged", kvec_paged_config), ("format", ctypes.c_int32)]
+
+
 @dataclass(frozen=True)
 class AttentionConfig:
     """Python view of kvec_attention_config."""
@@ -148,6 +153,34 @@ class PagedConfig:
         return _rebuild(self)
 
 
+@dataclass(frozen=True)
+class PagedQ8Config:
+    """Python view of kvec_paged_q8_config: the fields of a PagedConfig, and the format."""
+    batch: int
+    n_kv_heads: int
+    n_q_heads: int
+    head_dim: int
+    page_size: int
+    n_pages: int
+    max_pages: int
+    dtype: int = KVEC_BF16
+    format: int = KVEC_Q8_INT8
+
+    def __post_init__(self):
+        import torch
+        p = PagedConfig(self.batch, self.n_kv_heads, self.n_q_heads, self.head_dim, self.page_size, self.n_pages,
+                        self.max_pages, self.dtype)
+        _fix(self, kvec_paged_q8_config(p.c(), self.format), **{n: getattr(p, n) for n in (
+            "meta_shape", "pool_shape", "table_shape", "len_shape", "lse_shape", "q_shape")},
+             code=torch.int8 if self.format == KVEC_Q8_INT8 else torch.float8_e4m3fn)
+
+    def c(self) -> kvec_paged_q8_config:
+        return self._c
+
+    def __reduce__(self):
+        return _rebuild(self)
+
+
 def _rebuild(cfg):
     """Copies and pickles of a frozen configuration are made from its fields."""
     return type(cfg), tuple(getattr(cfg, f.name) for f in fields(cfg))
@@ -173,6 +206,9 @@ EXPORTS = ["kvec_workspace_size", "kvec_score", "kvec_score_lse", "kvec_select_c
            "kvec_prefill_workspace_size", "kvec_prefill_attention", "kvec_paged_append",
            "kvec_paged_decode_workspace_size", "kvec_paged_decode",
            "kvec_paged_evict_workspace_size", "kvec_paged_evict",
+           "kvec_paged_decode_shared_workspace_size", "kvec_paged_decode_shared", "kvec_paged_append_q8",
+           "kvec_paged_read_q8", "kvec_paged_decode_q8_workspace_size", "kvec_paged_decode_q8",
+           "kvec_paged_evict_q8_workspace_size", "kvec_paged_evict_q8",
            "kvec_status_string"]
 
 
@@ -225,6 +261,19 @@ def load() -> ctypes.CDLL:
     lib.kvec_paged_evict_workspace_size.argtypes = [C, i32, i32, ctypes.POINTER(sz)]
     lib.kvec_paged_evict.argtypes = [C, i32, i32, i32, vp, vp, I64x, vp, vp, vp, i32, vp, vp, vp, vp, vp,
                                      sz, vp]
+    E = ctypes.POINTER(kvec_paged_q8_config)
+    lib.kvec_paged_decode_shared_workspace_size.argtypes = [C, i32, i32, i32, ctypes.POINTER(sz)]
+    lib.kvec_paged_decode_shared.argtypes = [C, vp, I64x, vp, vp, I64x, vp, i32, vp, i32, vp, vp, i32, i32, i32,
+                                             vp, vp, vp, vp, sz, vp]
+    lib.kvec_paged_append_q8.argtypes = [E, i32, vp, I64x, vp, I64x, vp, I64x, vp, vp, f32, vp, vp, i32, vp,
+                                         vp, I64x, vp, vp, I64x, vp, vp, vp, vp, vp]
+    lib.kvec_paged_read_q8.argtypes = [E, vp, vp, I64x, vp, vp, vp, vp, i32, vp, I64x, vp, I64x, vp]
+    lib.kvec_paged_decode_q8_workspace_size.argtypes = [E, i32, i32, ctypes.POINTER(sz)]
+    lib.kvec_paged_decode_q8.argtypes = [E, vp, I64x, vp, vp, I64x, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp,
+                                         vp, sz, vp]
+    lib.kvec_paged_evict_q8_workspace_size.argtypes = [E, i32, i32, ctypes.POINTER(sz)]
+    lib.kvec_paged_evict_q8.argtypes = [E, i32, i32, i32, vp, vp, I64x, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp,
+                                        vp, sz, vp]
     lib.kvec_status_string.argtypes = [ctypes.c_int]
     lib.kvec_status_string.restype = ctypes.c_char_p
     for name in EXPORTS:
@@ -478,8 +527,10 @@ def _bound():
             from . import build as _build
             _build.build_binding()
         from . import _kvec_bind
-        _kvec_bind.bind(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in (
-            "kvec_prefill_attention", "kvec_paged_append", "kvec_paged_decode", "kvec_paged_evict")))
+        at = lambda *names: (ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names)  # noqa: E731
+        _kvec_bind.bind(*at("kvec_prefill_attention", "kvec_paged_append", "kvec_paged_decode", "kvec_paged_evict"))
+        _kvec_bind.bind_forms(*at("kvec_paged_decode_shared", "kvec_paged_append_q8", "kvec_paged_read_q8",
+                                  "kvec_paged_decode_q8", "kvec_paged_evict_q8"))
         _bind = _kvec_bind
     return _bind
 
@@ -620,6 +671,128 @@ def kvec_paged_evict(cfg: PagedConfig, budget: int, k_pool, v_pool, page_table, 
     _serve("kvec_paged_evict", cfg, k_pool.get_device(), stream, (
         budget, k_pool, v_pool, page_table, lens, n_seen, acc, pos, lens_out, ws, window, n_sinks, kept, n), lambda: (
         ("k_pool", k_pool, cfg.pool_shape, dt, False), ("v_pool", v_pool, cfg.pool_shape, dt, False),
+        ("page_table", page_table, cfg.table_shape, i32, True), ("lens", lens, cfg.len_shape, i32, True),
+        ("n_seen", n_seen, cfg.len_shape, i32, True), ("lens_out", lens_out, cfg.len_shape, i32, True),
+        ("acc", acc, cfg.meta_shape, f32, True), ("pos", pos, cfg.meta_shape, i32, True),
+        *_given(("kept", kept, (cfg.batch, cfg.n_kv_heads, budget), i32, True))))
+
+
+def kvec_paged_decode_shared_workspace_size(cfg: PagedConfig, max_prefix: int, max_len: int | None = None,
+                                            with_acc: bool = False) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().kvec_paged_decode_shared_workspace_size(cfg.ref, max_prefix, _max_len(cfg, max_len), int(with_acc),
+                                                          ctypes.byref(out)),
+           "kvec_paged_decode_shared_workspace_size")
+    return out.value
+
+
+def kvec_paged_decode_shared(cfg: PagedConfig, q, k_pool, v_pool, prefix_pages, prefix_len, page_table, lens, out,
+                             ws, max_prefix=None, max_len=None, window=0, n_sinks=0, lse=None, acc=None,
+                             stream=None) -> None:
+    """As kvec_paged_decode, every sequence behind the prefix_len (int32 [1]) slots of the
+    pages prefix_pages (int32 [n]); lens and max_len count the slots behind it (a negative
+    length: no sequence).  max_prefix None: every slot of the prefix's pages."""
+    if not isinstance(cfg, PagedConfig):
+        _other("kvec_paged_decode_shared", PagedConfig)
+    dt, f32, i32 = cfg.types
+    n = cfg.max_pages * cfg.page_size if max_len is None else max_len
+    pages = prefix_pages.shape[0] if prefix_pages is not None and prefix_pages.dim() else 0
+    p = pages * cfg.page_size if max_prefix is None else max_prefix
+    _serve("kvec_paged_decode_shared", cfg, q.get_device(), stream, (
+        q, k_pool, v_pool, prefix_pages, prefix_len, page_table, lens, out, ws, p, n, window, n_sinks, lse, acc), lambda: (
+        ("q", q, cfg.q_shape, dt, False), ("k_pool", k_pool, cfg.pool_shape, dt, False),
+        ("v_pool", v_pool, cfg.pool_shape, dt, False), ("prefix_pages", prefix_pages, (pages,), i32, True),
+        ("prefix_len", prefix_len, (1,), i32, True), ("page_table", page_table, cfg.table_shape, i32, True),
+        ("lens", lens, cfg.len_shape, i32, True), ("out", out, cfg.q_shape, f32, True), *_given(
+            ("lse", lse, cfg.lse_shape, f32, True), ("acc", acc, cfg.meta_shape, f32, True))))
+
+
+def _q8_pools(cfg: PagedQ8Config, k_pool, v_pool, k_scale, v_scale) -> tuple:
+    """Entries of an 8-bit cache's tensors."""
+    return (("k_pool", k_pool, cfg.pool_shape, cfg.code, False), ("v_pool", v_pool, cfg.pool_shape, cfg.code, False),
+            ("k_scale", k_scale, cfg.meta_shape, cfg.types[1], True), ("v_scale", v_scale, cfg.meta_shape, cfg.types[1], True))
+
+
+def kvec_paged_append_q8(cfg: PagedQ8Config, q, k, v, positions, slots, q_out, k_pool, v_pool, k_scale, v_scale,
+                         q_weight=None, k_weight=None, eps=1e-6, inv_freq=None, acc=None, pos=None,
+                         stream=None) -> None:
+    """As kvec_paged_append, into pools int8 or float8_e4m3fn (cfg.format)
+    [n_pages][H][page_size][d] with scales fp32 [n_pages][H][page_size]."""
+    if not isinstance(cfg, PagedQ8Config):
+        _other("kvec_paged_append_q8", PagedQ8Config)
+    def tensors():
+        import torch
+        (dt, f32, i32), n, d = cfg.types, 0 if q is None else q.shape[0], cfg.head_dim
+        half = 0 if inv_freq is None else inv_freq.shape[0]
+        return (*_q8_pools(cfg, k_pool, v_pool, k_scale, v_scale),
+                ("q", q, (n, cfg.n_q_heads, d), dt, False), ("k", k, (n, cfg.n_kv_heads, d), dt, False),
+                ("v", v, (n, cfg.n_kv_heads, d), dt, False), ("q_out", q_out, (n, cfg.n_q_heads, d), dt, False),
+                ("positions", positions, (n,), i32, True), ("slots", slots, (n,), torch.int64, True), *_given(
+                    ("q_weight", q_weight, (d,), dt, True), ("k_weight", k_weight, (d,), dt, True),
+                    ("inv_freq", inv_freq, (half,), torch.float64, True), ("acc", acc, cfg.meta_shape, f32, True),
+                    ("pos", pos, cfg.meta_shape, i32, True)))
+    _serve("kvec_paged_append_q8", cfg, k_pool.get_device(), stream, (
+        q, k, v, positions, slots, q_out, k_pool, v_pool, k_scale, v_scale, q_weight, k_weight, eps, inv_freq, acc,
+        pos), tensors)
+
+
+def kvec_paged_read_q8(cfg: PagedQ8Config, k_pool, v_pool, k_scale, v_scale, page_table, lens, k_out, v_out,
+                       stream=None) -> None:
+    """The rows of slots 0..lens[b] of every sequence: k_out, v_out [b][H][max_len][d] of
+    cfg.dtype (any leading strides), max_len their own."""
+    if not isinstance(cfg, PagedQ8Config):
+        _other("kvec_paged_read_q8", PagedQ8Config)
+    def tensors():
+        dt, _, i32 = cfg.types
+        n = k_out.shape[2] if k_out is not None and k_out.dim() > 2 else 0
+        shape = (cfg.batch, cfg.n_kv_heads, n, cfg.head_dim)
+        return (*_q8_pools(cfg, k_pool, v_pool, k_scale, v_scale), ("page_table", page_table, cfg.table_shape, i32, True),
+                ("lens", lens, cfg.len_shape, i32, True), ("k_out", k_out, shape, dt, False), ("v_out", v_out, shape, dt, False))
+    _serve("kvec_paged_read_q8", cfg, k_pool.get_device(), stream, (
+        k_pool, v_pool, k_scale, v_scale, page_table, lens, k_out, v_out), tensors)
+
+
+def kvec_paged_decode_q8_workspace_size(cfg: PagedQ8Config, max_len: int | None = None,
+                                        with_acc: bool = False) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().kvec_paged_decode_q8_workspace_size(cfg.ref, _max_len(cfg, max_len), int(with_acc),
+                                                      ctypes.byref(out)), "kvec_paged_decode_q8_workspace_size")
+    return out.value
+
+
+def kvec_paged_decode_q8(cfg: PagedQ8Config, q, k_pool, v_pool, k_scale, v_scale, page_table, lens, out, ws,
+                         max_len=None, window=0, n_sinks=0, lse=None, acc=None, stream=None) -> None:
+    """As kvec_paged_decode, over pools and scales as in kvec_paged_append_q8."""
+    if not isinstance(cfg, PagedQ8Config):
+        _other("kvec_paged_decode_q8", PagedQ8Config)
+    dt, f32, i32 = cfg.types
+    n = cfg.max_pages * cfg.page_size if max_len is None else max_len
+    _serve("kvec_paged_decode_q8", cfg, q.get_device(), stream, (
+        q, k_pool, v_pool, k_scale, v_scale, page_table, lens, out, ws, n, window, n_sinks, lse, acc), lambda: (
+        ("q", q, cfg.q_shape, dt, False), *_q8_pools(cfg, k_pool, v_pool, k_scale, v_scale),
+        ("page_table", page_table, cfg.table_shape, i32, True), ("lens", lens, cfg.len_shape, i32, True),
+        ("out", out, cfg.q_shape, f32, True), *_given(
+            ("lse", lse, cfg.lse_shape, f32, True), ("acc", acc, cfg.meta_shape, f32, True))))
+
+
+def kvec_paged_evict_q8_workspace_size(cfg: PagedQ8Config, max_len: int | None, budget: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().kvec_paged_evict_q8_workspace_size(cfg.ref, _max_len(cfg, max_len), budget, ctypes.byref(out)),
+           "kvec_paged_evict_q8_workspace_size")
+    return out.value
+
+
+def kvec_paged_evict_q8(cfg: PagedQ8Config, budget: int, k_pool, v_pool, k_scale, v_scale, page_table, lens, n_seen,
+                        acc, pos, lens_out, ws, window=0, n_sinks=0, kept=None, max_len=None, stream=None) -> None:
+    """As kvec_paged_evict, over pools and scales as in kvec_paged_append_q8."""
+    if not isinstance(cfg, PagedQ8Config):
+        _other("kvec_paged_evict_q8", PagedQ8Config)
+    _, f32, i32 = cfg.types
+    n = cfg.max_pages * cfg.page_size if max_len is None else max_len
+    _serve("kvec_paged_evict_q8", cfg, k_pool.get_device(), stream, (
+        budget, k_pool, v_pool, k_scale, v_scale, page_table, lens, n_seen, acc, pos, lens_out, ws, window, n_sinks, kept, n),
+        lambda: (
+        *_q8_pools(cfg, k_pool, v_pool, k_scale, v_scale),
         ("page_table", page_table, cfg.table_shape, i32, True), ("lens", lens, cfg.len_shape, i32, True),
         ("n_seen", n_seen, cfg.len_shape, i32, True), ("lens_out", lens_out, cfg.len_shape, i32, True),
         ("acc", acc, cfg.meta_shape, f32, True), ("pos", pos, cfg.meta_shape, i32, True),
