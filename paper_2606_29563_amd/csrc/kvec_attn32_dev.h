@@ -86,22 +86,30 @@ struct Columns32 {
   // Key of element e of block g, from the tile's first.
   __device__ __forceinline__ int key(int g, int e) const { return 32 * g + 8 * (e >> 2) + 4 * hh + (e & 3); }
 
-  // Probabilities of a tile's logits, -inf where masked, as 16-key steps of the V product;
-  // lo: what their rounding to bf16 leaves, rounded again (SPLIT).
-  template <int NB, bool SPLIT>
-  __device__ __forceinline__ void weigh(const f32x16 (&x)[NB], float sc, bf16x8 (&pf)[2 * NB], bf16x8 (&lo)[2 * NB]) {
+  // Probabilities of a tile's logits, -inf where masked, as 16-key steps of the V product:
+  // the sum of TERMS bf16 numbers, each the rounding of what those before it leave.
+  template <int NB, int TERMS>
+  __device__ __forceinline__ void weigh(const f32x16 (&x)[NB], float sc, bf16x8 (&p)[TERMS][2 * NB]) {
     float sum;
     auto against = [&](float ref) {
       sum = 0.f;
 #pragma unroll
       for (int g = 0; g < NB; ++g)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float v = __builtin_amdgcn_exp2f(fmaf(x[g][e], sc, -ref));
-          sum += v;
-          const __bf16 top = (__bf16)v;
-          pf[2 * g + (e >> 3)][e & 7] = top;
-          if constexpr (SPLIT) lo[2 * g + (e >> 3)][e & 7] = (__bf16)(v - (float)top);
+        for (int e = 0; e < 16; e += 2) {
+          float v0 = __builtin_amdgcn_exp2f(fmaf(x[g][e], sc, -ref)), v1 = __builtin_amdgcn_exp2f(fmaf(x[g][e + 1], sc, -ref));
+          sum += v0;
+          sum += v1;
+#pragma unroll
+          for (int i = 0; i < TERMS; ++i) {
+            const bf16x2 top = bf16_pair(v0, v1);
+            p[i][2 * g + (e >> 3)][e & 7] = top[0];
+            p[i][2 * g + (e >> 3)][(e & 7) + 1] = top[1];
+            if (i + 1 < TERMS) {
+              v0 -= first_of(top);
+              v1 -= second_of(top);
+            }
+          }
         }
     };
     against(m);

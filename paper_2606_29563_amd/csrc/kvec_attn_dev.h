@@ -78,6 +78,51 @@ __device__ __forceinline__ bf16x8 join8(s16x4 a, s16x4 b) {
   return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// 16 bytes a lane of `rows` (the words of a buffer) at byte `off` to LDS, lane after lane from
+// `to` on.  Written out: after the compiler's builtin, reads of LDS may wait for every copy in
+// flight (it cannot tell the addresses apart).  Waited for with wait_vmem.
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ i32x4 rows_at(const char* p, int extent) {
+  const uint64_t at = (uint64_t)(uintptr_t)p;
+  return i32x4{(int)__builtin_amdgcn_readfirstlane((int)at), (int)__builtin_amdgcn_readfirstlane((int)(at >> 32) & 0xffff),
+               __builtin_amdgcn_readfirstlane(extent), kBufferWord3};
+}
+template <bool ONCE>  // the rows are not read again
+__device__ __forceinline__ void lds_copy16(i32x4 rows, int off, const char* to) {
+  int kept;  // m0, which the compiler takes as its own
+  const int at = __builtin_amdgcn_readfirstlane((int)lds_addr(to));
+  if constexpr (ONCE) {
+    asm volatile(
+        "s_mov_b32 %0, m0\n\t"
+        "s_mov_b32 m0, %1\n\t"
+        "s_nop 0\n\t"
+        "buffer_load_dwordx4 %2, %3, 0 offen nt lds\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(kept)
+        : "s"(at), "v"(off), "s"(rows)
+        : "memory");
+  } else {
+    asm volatile(
+        "s_mov_b32 %0, m0\n\t"
+        "s_mov_b32 m0, %1\n\t"
+        "s_nop 0\n\t"
+        "buffer_load_dwordx4 %2, %3, 0 offen lds\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(kept)
+        : "s"(at), "v"(off), "s"(rows)
+        : "memory");
+  }
+}
+
+// Two floats rounded to bf16, and what these are.
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ bf16x2 bf16_pair(float a, float b) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  return __builtin_convertvector((f32x2{a, b}), bf16x2);
+}
+__device__ __forceinline__ float first_of(bf16x2 p) { return __uint_as_float(__builtin_bit_cast(uint32_t, p) << 16); }
+__device__ __forceinline__ float second_of(bf16x2 p) { return __uint_as_float(__builtin_bit_cast(uint32_t, p) & 0xffff0000u); }
+
 // Values that are no numbers.  A tile that some of its rows see only in part takes the
 // keys that a row does not see with a probability of 0, and 0 times a NaN or infinity in V
 // would stay in its output.  That shows at the end, where the output is no number, and is

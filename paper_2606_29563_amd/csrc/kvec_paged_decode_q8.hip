@@ -4,8 +4,8 @@
 // the product of the query with the codes, and a value's scale goes into its probability:
 //   x_s = zk_s (q . k_s) / sqrt(d),   out = sum_s (p_s zv_s) v_s.
 // Codes are exact in bf16, so the products are those of kvec_paged_decode.hip's bf16 path;
-// float32 queries enter as three bf16 terms, 24 bits.  Probabilities enter the V product as
-// two bf16 terms (three with float32 queries).
+// float32 queries enter as three bf16 terms, 24 bits, and so do the probabilities enter the V
+// product.
 //
 // Bound by reading the visible rows once, half the bytes of bf16 ones.  The launches
 // are those of kvec_paged_decode.hip, the second the same one; here a step of a wave is 32
@@ -85,14 +85,21 @@ __device__ __forceinline__ void vt_read8(const uint32_t (&at)[8], i32x2 (&v)[8])
       : "memory");
 }
 
-// A float as the sum of N bf16 terms.
+// Eight floats as the sums of N bf16 terms.
 template <int N>
-__device__ __forceinline__ void terms(float x, __bf16 (&t)[N]) {
+__device__ __forceinline__ void terms(float (&f)[8], bf16x8 (&t)[N]) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    t[i] = (__bf16)x;
-    x -= (float)t[i];
-  }
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const bf16x2 top = bf16_pair(f[e], f[e + 1]);
+      t[i][e] = top[0];
+      t[i][e + 1] = top[1];
+      if (i + 1 < N) {
+        f[e] -= first_of(top);
+        f[e + 1] -= second_of(top);
+      }
+    }
 }
 
 // Softmax state and output of 16 query columns over 32 codes' rows a step.  NQ, NP: bf16
@@ -100,7 +107,7 @@ __device__ __forceinline__ void terms(float x, __bf16 (&t)[N]) {
 template <int D, int FORMAT, int NQ>
 struct Columns16Q8 {
   using CG = CodeGroup<D>;
-  static constexpr int DT = D / 16, KP = D / 64, NP = NQ == 1 ? 2 : 3;
+  static constexpr int DT = D / 16, KP = D / 64, NP = 3;
   bf16x8 q[NQ][2 * KP];
   float m, l;
   f32x4 o[DT];
@@ -124,14 +131,11 @@ struct Columns16Q8 {
         q[0][j] = __builtin_bit_cast(bf16x8, reinterpret_cast<const uint4*>(row)[at]);
       } else {
         const float4 a = reinterpret_cast<const float4*>(row)[2 * at], b = reinterpret_cast<const float4*>(row)[2 * at + 1];
-        const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        bf16x8 t[NQ];
+        terms(f, t);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          __bf16 t[NQ];
-          terms(f[e], t);
-#pragma unroll
-          for (int i = 0; i < NQ; ++i) q[i][j][e] = t[i];
-        }
+        for (int i = 0; i < NQ; ++i) q[i][j] = t[i];
       }
     }
   }
@@ -171,17 +175,16 @@ struct Columns16Q8 {
     m = mx;
     l *= f;
     bf16x8 p[NP];
+    float w[8];
 #pragma unroll
     for (int g = 0; g < 2; ++g)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float e = __builtin_amdgcn_exp2f(x[g][i] - ref);
         l += e;
-        __bf16 t[NP];
-        terms(e * z[g][i], t);
-#pragma unroll
-        for (int j = 0; j < NP; ++j) p[j][4 * g + i] = t[j];
+        w[4 * g + i] = e * z[g][i];
       }
+    terms(w, p);
     if (__any(f != 1.f)) {
 #pragma unroll
       for (int t = 0; t < DT; ++t)

@@ -159,8 +159,10 @@ __device__ __forceinline__ void finish(const PdArgs& a, const Visible& vis, Colu
 
 constexpr int kPdRing = 2;  // groups of 16 slots in flight per wave
 
-// ONE: the sequence is not split, its work-group finishes the results itself.
-template <class TT, int D, bool ONE>
+// ONE: the sequence is not split, its work-group finishes the results itself.  CALLER: 0, or
+// of another kernel, where the compiler would wait for the copies in flight at every read of
+// LDS.  (An instance for each: the host's compilation refuses a second use of one.)
+template <class TT, int D, bool ONE, int CALLER = 0>
 __device__ __forceinline__ void partial(const PdArgs& a, char* smem, int s, int h, int b) {
   using RG = RowGroup<TT, D>;
   constexpr int ES = RG::ES;
@@ -206,6 +208,17 @@ __device__ __forceinline__ void partial(const PdArgs& a, char* smem, int s, int 
     ok[u] = k < count && page_ok(a, page);
     whole[u] = ok[u] && slot0 + 16 <= vis.n && (slot0 >= vis.lo || slot0 + 16 <= vis.sinks);
     const int64_t base = ok[u] ? ((int64_t)page * a.c.sp + (int64_t)h * a.c.sh + (int64_t)row0 * a.c.sr) * ES : 0;
+    if constexpr (CALLER != 0) {
+      const i32x4 kr = rows_at(a.c.k + base, ok[u] ? extent : 0), vr = rows_at(a.c.v + base, ok[u] ? extent : 0);
+      const char* to = ring + u * STEP;
+#pragma unroll
+      for (int i = 0; i < RG::NI; ++i) {
+        const int off = whole[u] || vis.sees(slot0 + rowi[i]) ? voff[i] : kOutOfRange;
+        lds_copy16<true>(kr, off, to + i * 1024);
+        lds_copy16<true>(vr, off, to + RG::BYTES + i * 1024);
+      }
+      return;
+    }
     const auto kr = __builtin_amdgcn_make_buffer_rsrc(a.c.k + base, 0, ok[u] ? extent : 0, kBufferWord3);
     const auto vr = __builtin_amdgcn_make_buffer_rsrc(a.c.v + base, 0, ok[u] ? extent : 0, kBufferWord3);
     auto* dk = (__attribute__((address_space(3))) char*)(ring + u * STEP);

@@ -4,9 +4,9 @@
 // sum, output), so the prefix's part needs no sequence by itself: all b G query heads of a
 // KV head are the columns of one product with the prefix's rows, which are read once for a
 // tile of columns instead of once a sequence.
-//   prefix   a work-group per (split of the prefix, column tile, KV head): states of its
-//            columns.
-//   partial  the own slots, as kvec_paged_decode.hip has them.
+//   both     a work-group per (split of the prefix, column tile, KV head): states of its
+//            columns; and among them those of the own slots, as kvec_paged_decode.hip has
+//            them.  The prefix's keep the matrix cores busy, the others the memory.
 //   combine  the one of kvec_paged_decode.hip, over the splits of both.
 //   weights  (with acc) what every prefix slot receives: sum over the columns of
 //            2^(logit - norm), from the normalisers that the combine leaves.  The logits
@@ -24,6 +24,8 @@ struct ShArgs {
   PdArgs d;
   const int32_t* pages;  // the prefix's
   int columns, tiles, Sp;
+  unsigned first_own;             // work-groups of the prefix, in whole eights
+  GroupDiv by_group;              // division of columns by G (both below 2^20 / 16)
 };
 
 // What a column sees of the prefix's P slots: those from `lo` on, and the first `sinks`.
@@ -133,13 +135,15 @@ __device__ __forceinline__ bool sh_item(const ShArgs& a, int id, int* h, int* sp
 }
 
 // bf16: CW waves of 32 columns, KW times; the k-th of the KW takes every KW-th tile of KT
-// slots, with LDS buffers of its own, and the states meet in LDS.
-template <int D, int CW, int KW, int KT>
+// slots, with a ring of RING LDS buffers of its own, and the states meet in LDS.
+template <int D, int CW, int KW, int KT, int RING>
 __device__ __forceinline__ void prefix32(const ShArgs& a, char* smem_all, int id) {
-  constexpr int ES = 2, HALF = KT * D * ES, GRPS = KT / 16, CPG = D / 32;
+  constexpr int ES = 2, HALF = KT * D * ES, GRPS = KT / 16, CPG = D / 32;  // CPG: copies of a group
   constexpr int PER = GRPS * CPG / CW, DT = D / 32;  // copies per wave of K and of V
-  static_assert(GRPS % CW == 0, "a wave copies whole groups");
-  static_assert((KW - 1) * CW * 32 * (D + 2) * 4 <= KW * 4 * HALF, "states in LDS");
+  constexpr int GPW = PER < CPG ? 1 : PER / CPG;     // groups of a wave (or a part of one)
+  constexpr int TERMS = 2;
+  static_assert(PER >= 1 && (PER % CPG == 0 || CPG % PER == 0), "a wave copies whole groups, or of one");
+  static_assert((KW - 1) * CW * 32 * (D + 2) * 4 <= KW * RING * 2 * HALF, "states in LDS");
   __shared__ int red[CW * KW][2];
   __shared__ bool flags[CW * KW];
   const PagedView& c = a.d.c;
@@ -147,15 +151,13 @@ __device__ __forceinline__ void prefix32(const ShArgs& a, char* smem_all, int id
   if (!sh_item(a, id, &h, &split, &tile)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int w = wave % CW, kw = wave / CW;
-  char* smem = smem_all + kw * 4 * HALF;
+  char* smem = smem_all + kw * RING * 2 * HALF;
   const int P = a.d.prefix(), i = (tile * CW + w) * 32 + (lane & 31);
   const Column mine(a, i, P);
   const PrefixSpan<KT> sp = span_of<KT, CW * KW>(a, mine, P, red);
   const int per = (sp.n + a.Sp - 1) / a.Sp;
   const int t0 = min(split * per, sp.n), t1 = min(t0 + per, sp.n);
 
-  Columns32<D> col;
-  col.init(lane, a.d.q + ((int64_t)mine.b * a.d.qs_b + (int64_t)(h * c.G + mine.g) * a.d.qs_h) * ES, mine.live);
   RowCopy<D> rc[PER];
   int voff[PER];
 #pragma unroll
@@ -165,7 +167,9 @@ __device__ __forceinline__ void prefix32(const ShArgs& a, char* smem_all, int id
   }
   const int extent = 15 * (int)(c.sr * ES) + D * ES;
   PageAhead<KT> ahead;
-  bool missing[2];  // a group of the tile has no page
+  uint32_t missing = 0;  // bit k: of the wave's k-th tile (from its end) a group has no page
+  // The wave's k-th tile, t; those behind the split's last are copied as zeros: the number in
+  // flight stays.
   auto copy = [&](int u, int t, int k) {
     if (k % PageAhead<KT>::AHEAD == 0) ahead.lookup(a, sp, t, KW, lane);
     const int key0 = sp.key0(t);
@@ -174,45 +178,55 @@ __device__ __forceinline__ void prefix32(const ShArgs& a, char* smem_all, int id
     for (int g = 0; g < GRPS; ++g) {
       int row0;
       const int page = ahead.page(a, k, g, &row0);
-      const bool ok = page >= 0 && key0 + 16 * g < P;
       miss |= page < 0;
-      if (g / (GRPS / CW) != w) continue;  // another wave's
+      if (PER <= CPG ? w * PER / CPG != g : g / GPW != w) continue;  // another wave's
+      const bool ok = t < t1 && page >= 0 && key0 + 16 * g < P;
       const int64_t base = ok ? ((int64_t)page * c.sp + (int64_t)h * c.sh + (int64_t)row0 * c.sr) * ES : 0;
-      const auto kr = __builtin_amdgcn_make_buffer_rsrc(c.k + base, 0, ok ? extent : 0, kBufferWord3);
-      const auto vr = __builtin_amdgcn_make_buffer_rsrc(c.v + base, 0, ok ? extent : 0, kBufferWord3);
+      const i32x4 kr = rows_at(c.k + base, ok ? extent : 0), vr = rows_at(c.v + base, ok ? extent : 0);
 #pragma unroll
-      for (int e = 0; e < CPG; ++e) {
-        const int q = g % (GRPS / CW) * CPG + e;
-        auto* dk = (__attribute__((address_space(3))) char*)(smem + u * 2 * HALF + (w * PER + q) * 1024);
-        auto* dv = (__attribute__((address_space(3))) char*)(smem + u * 2 * HALF + HALF + (w * PER + q) * 1024);
+      for (int e = 0; e < (PER < CPG ? PER : CPG); ++e) {
+        const int q = PER <= CPG ? e : g % GPW * CPG + e;
         const bool in = sp.any(key0 + rc[q].row);  // others are copied as zeros
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, dk, 16, in ? voff[q] + rc[q].kb : kOutOfRange, 0, 0, 0);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, dv, 16, in ? voff[q] + rc[q].vb : kOutOfRange, 0, 0, 0);
+        const char* to = smem + u * 2 * HALF + (w * PER + q) * 1024;
+        lds_copy16<false>(kr, in ? voff[q] + rc[q].kb : kOutOfRange, to);
+        lds_copy16<false>(vr, in ? voff[q] + rc[q].vb : kOutOfRange, to + HALF);
       }
     }
-    missing[u] = miss;
+    missing = missing << 1 | (uint32_t)miss;
   };
   auto has_page = [&](int slot) {
     int row0;
     return page_ok(a.d, prefix_page(a, slot >> 4, &row0));
   };
+  const int first = t0 + kw;
+  Columns32<D> col;
+  col.init(lane, a.d.q + ((int64_t)mine.b * a.d.qs_b + (int64_t)(h * c.G + mine.g) * a.d.qs_h) * ES, mine.live);
+  if (sp.n > 0) {
+#pragma unroll
+    for (int k = 0; k < RING - 1; ++k) copy(k, first + k * KW, k);
+  }
+#pragma unroll
+  for (int ks = 0; ks < Columns32<D>::KS; ++ks) asm volatile("" : "+v"(col.q[ks]));  // waited for here, not in the loop
   auto pass = [&](auto careful) {
     col.clear();
-    if (t0 + kw < t1) copy(0, t0 + kw, 0);
     int u = 0, k = 0;
-    for (int t = t0 + kw; t - kw < t1; t += KW, u ^= 1, ++k) {
-      wait_vmem<0>();
+    // (every wave passes the same barriers; a last step may be without a tile)
+#pragma unroll 1
+    for (int t = first; t - kw < t1; t += KW, ++k) {
+      wait_vmem<(RING - 2) * 2 * PER>();
       if (careful.value && t < t1 && !sp.open(sp.key0(t)))
         tame<BF16, PER>(smem + u * 2 * HALF + HALF + w * PER * 1024 + lane * 16);
-      lds_barrier();  // the tile is there, and every wave is done with the other buffer
-      if (t + KW < t1) copy(u ^ 1, t + KW, k + 1);
-      if (KW > 1 && t >= t1) continue;  // behind the last tile (this step's barrier is passed)
+      lds_barrier();  // the tile is there, and every wave is done with the buffer before it
+      const bool miss = missing >> (RING - 2) & 1;
+      copy(u == 0 ? RING - 1 : u - 1, t + (RING - 1) * KW, k + RING - 1);
       const char* kb = smem + u * 2 * HALF;
       const char* vb = kb + HALF;
+      u = u + 1 == RING ? 0 : u + 1;
+      if (KW > 1 && t >= t1) continue;
       f32x16 x[KT / 32];
       col.logits(x, kb);
       const int key0 = sp.key0(t);
-      if (!sp.open(key0) || missing[u]) {
+      if (!sp.open(key0) || miss) {
 #pragma unroll
         for (int g = 0; g < KT / 32; ++g)
 #pragma unroll
@@ -220,16 +234,16 @@ __device__ __forceinline__ void prefix32(const ShArgs& a, char* smem_all, int id
             const int key = key0 + col.key(g, e);
             if (!(key < P && mine.sees(key))) x[g][e] = -INFINITY;
           }
-        if (missing[u]) {
+        if (miss) {
 #pragma unroll
-          for (int g = 0; g < KT / 16; ++g)
+          for (int g = 0; g < GRPS; ++g)
             if (!(key0 + 16 * g < P && has_page(key0 + 16 * g)))
 #pragma unroll
               for (int e = 0; e < 8; ++e) x[g / 2][8 * (g % 2) + e] = -INFINITY;
         }
       }
-      bf16x8 pf[KT / 16], lo[KT / 16];
-      col.template weigh<KT / 32, true>(x, a.d.sc, pf, lo);
+      bf16x8 pf[TERMS][KT / 16];
+      col.template weigh<KT / 32, TERMS>(x, a.d.sc, pf);
 #pragma unroll
       for (int ss = 0; ss < KT / 16; ++ss)
 #pragma unroll
@@ -239,13 +253,14 @@ __device__ __forceinline__ void prefix32(const ShArgs& a, char* smem_all, int id
           const s16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + col.voff[2 * dt]));
           const s16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + col.voff[2 * dt + 1]));
           const bf16x8 v = join8(a0, a1);
-          col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[ss], col.o[dt], 0, 0, 0);
-          col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, lo[ss], col.o[dt], 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < TERMS; ++i) col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[i][ss], col.o[dt], 0, 0, 0);
         }
     }
+    wait_vmem<0>();
     if (careful.value) {
 #pragma unroll 1
-      for (int t = t0 + kw; t < t1; t += KW) {
+      for (int t = first; t < t1; t += KW) {
         if (sp.open(sp.key0(t))) continue;
 #pragma unroll 1
         for (int key = sp.key0(t); key < min(sp.key0(t) + KT, P); ++key) {
@@ -261,7 +276,13 @@ __device__ __forceinline__ void prefix32(const ShArgs& a, char* smem_all, int id
   if (a.d.window > 0) {  // (else no column sees what another does not)
     flags[wave] = __any(col.wild_output());
     lds_barrier();
-    if (__builtin_expect(__any(flags[lane % (CW * KW)]), false)) pass(std::true_type{});
+    if (__builtin_expect(__any(flags[lane % (CW * KW)]), false)) {
+      if (sp.n > 0) {
+#pragma unroll
+        for (int k = 0; k < RING - 1; ++k) copy(k, first + k * KW, k);
+      }
+      pass(std::true_type{});
+    }
   }
   col.close();
   if constexpr (KW > 1) {
@@ -283,12 +304,6 @@ __device__ __forceinline__ void prefix32(const ShArgs& a, char* smem_all, int id
     for (int e = 0; e < 16; e += 4)
       *reinterpret_cast<f32x4_any*>(a.d.part + at * D + col.dim(dt, e)) =
           f32x4{col.o[dt][e], col.o[dt][e + 1], col.o[dt][e + 2], col.o[dt][e + 3]};
-}
-
-template <int D, int CW, int KW, int KT>
-__global__ __launch_bounds__(kShThreads, 2) void sh_prefix32(ShArgs a) {
-  __shared__ __align__(1024) char smem[KW * 4 * KT * D * 2];
-  prefix32<D, CW, KW, KT>(a, smem, blockIdx.x);
 }
 
 // float32: four waves of 16 columns on the 16x16x4 product, tiles of 32 slots.
@@ -315,6 +330,8 @@ __device__ __forceinline__ void prefix16(const ShArgs& a, char* smem, int id) {
   Columns16<TT, D, GRPS> col;
   col.q.zero();
   if (mine.live) col.q.load(a.d.q + ((int64_t)mine.b * a.d.qs_b + (int64_t)(h * c.G + mine.g) * a.d.qs_h) * ES, q4);
+#pragma unroll
+  for (int j = 0; j < Frag<TT, D>::KS; ++j) asm volatile("" : "+v"(col.q.v[j]));  // waited for here, not in the loop
   const int extent = 15 * (int)(c.sr * ES) + D * ES;
   PageAhead<KT> ahead;
   bool missing[2];
@@ -332,13 +349,12 @@ __device__ __forceinline__ void prefix16(const ShArgs& a, char* smem, int id) {
       const int at0 = w * PER, in0 = at0 % (GRPS * RG::NI);
       if (in0 / RG::NI != g) continue;
       const int64_t base = ok ? ((int64_t)page * c.sp + (int64_t)h * c.sh + (int64_t)row0 * c.sr) * ES : 0;
-      const auto r = __builtin_amdgcn_make_buffer_rsrc((at0 >= GRPS * RG::NI ? c.v : c.k) + base, 0, ok ? extent : 0, kBufferWord3);
+      const i32x4 r = rows_at((at0 >= GRPS * RG::NI ? c.v : c.k) + base, ok ? extent : 0);
 #pragma unroll
       for (int e = 0; e < PER; ++e) {
         const int row = row_in_copy<TT, D>((in0 + e) % RG::NI, lane);
         const int off = sp.any(key0 + 16 * g + row) ? row * (int)(c.sr * ES) + piece_in_copy<TT, D>((in0 + e) % RG::NI, lane) * 16 : kOutOfRange;
-        auto* dst = (__attribute__((address_space(3))) char*)(smem + u * BUF + (at0 + e) * 1024);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 16, off, 0, 0, 0);
+        lds_copy16<false>(r, off, smem + u * BUF + (at0 + e) * 1024);
       }
     }
     missing[u] = miss;
@@ -402,86 +418,137 @@ __device__ __forceinline__ void prefix16(const ShArgs& a, char* smem, int id) {
   for (int t = 0; t < D / 16; ++t) *reinterpret_cast<f32x4_any*>(a.d.part + at * D + 16 * t + 4 * q4) = col.o[t];
 }
 
-template <int D>
-__global__ __launch_bounds__(kShThreads) void sh_prefix16(ShArgs a) {
-  __shared__ __align__(1024) char smem[4 * 32 * D * 4];
-  prefix16<D>(a, smem, blockIdx.x);
+enum { kSh16 = 1, kSh2x2, kSh4x1 };  // how the prefix's columns are laid out
+
+// The prefix's work-groups first: at most one for every compute unit as long as their
+// columns allow it, so that those of the own slots share the units with them.
+template <class TT, int D, int KERNEL>
+__global__ __launch_bounds__(kShThreads, 2) void sh_both(ShArgs a) {
+  constexpr int OWN = kPdWaves * kPdRing * 2 * RowGroup<TT, D>::BYTES, PREFIX = KERNEL == kSh16 ? 4 * 32 * D * 4 : 4 * 2 * 32 * D * 2;
+  __shared__ __align__(1024) char smem[OWN > PREFIX ? OWN : PREFIX];
+  const bool own = blockIdx.x >= a.first_own;
+  const int id = blockIdx.x - (own ? a.first_own : 0);
+  if (own) {
+    const int h = id / a.d.So % a.d.c.H, b = id / a.d.So / a.d.c.H;
+    partial<TT, D, false, KERNEL>(a.d, smem, id % a.d.So, h, b);
+  } else if constexpr (KERNEL == kSh16) {
+    prefix16<D>(a, smem, id);
+  } else if constexpr (KERNEL == kSh2x2) {
+    prefix32<D, 2, 2, 32, 2>(a, smem, id);
+  } else {
+    prefix32<D, 4, 1, 64, 2>(a, smem, id);
+  }
 }
 
-// What the prefix's slots receive: a wave has 16 NG slots' keys in registers and goes over
-// the columns, 16 at a time.
-template <class TT, int D, int NG>
-__global__ __launch_bounds__(kShThreads) void sh_weights(ShArgs a) {
-  constexpr int ES = elem_bytes<TT>();
+// What the prefix's slots receive: every wave of a work-group has the keys of the same 16 NG
+// slots in registers and goes over every fourth tile of 16 columns, its queries loaded a
+// tile ahead; the waves' sums meet in LDS.
+constexpr int kWtThreads = 256;
+template <class TT, int D, int NG, bool WINDOW>
+__global__ __launch_bounds__(kWtThreads, 2) void sh_weights(ShArgs a) {
+  constexpr int ES = elem_bytes<TT>(), WAVES = kWtThreads / 64;
+  __shared__ float part[WAVES][16 * NG];
   const PagedView& c = a.d.c;
   const int h = blockIdx.y, P = a.d.prefix();
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int n = lane & 15, q4 = lane >> 4;
-  const int key0 = (blockIdx.x * (kShThreads / 64) + w) * 16 * NG;
+  const int key0 = blockIdx.x * 16 * NG;
   if (key0 >= P) return;
   Frag<TT, D> k[NG];
-  int64_t meta[NG];
-  bool ok[NG];
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
     int row0 = 0;
     const int page = key0 + 16 * g < P ? prefix_page(a, (key0 >> 4) + g, &row0) : -1;
-    ok[g] = page_ok(a.d, page);
-    meta[g] = ((int64_t)page * c.H + h) * c.ps + row0;
     k[g].zero();
-    if (ok[g]) k[g].load(c.k + ((int64_t)page * c.sp + (int64_t)h * c.sh + (int64_t)(row0 + n) * c.sr) * ES, q4);
+    if (page_ok(a.d, page)) k[g].load(c.k + ((int64_t)page * c.sp + (int64_t)h * c.sh + (int64_t)(row0 + n) * c.sr) * ES, q4);
   }
-  float sum[NG][4];
+  f32x4 sum[NG];
 #pragma unroll
-  for (int g = 0; g < NG; ++g)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sum[g][e] = 0.f;
-#pragma unroll 1
-  for (int i0 = 0; i0 < a.columns; i0 += 16) {
-    const Column mine(a, i0 + n, P);
+  for (int g = 0; g < NG; ++g) sum[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // queries, normaliser and length of a column (behind the last one: of that)
+  struct Tile {
     Frag<TT, D> q;
-    q.zero();
-    if (mine.live) q.load(a.d.q + ((int64_t)mine.b * a.d.qs_b + (int64_t)(h * c.G + mine.g) * a.d.qs_h) * ES, q4);
-    const float norm = mine.live ? a.d.norm[(int64_t)mine.b * c.HQ + h * c.G + mine.g] : 0.f;
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const f32x4 x = mma(k[g], q, f32x4{0.f, 0.f, 0.f, 0.f}) * a.d.sc;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float p = __builtin_amdgcn_exp2f(x[e] - norm);
-        sum[g][e] += mine.live && mine.sees(key0 + 16 * g + 4 * q4 + e) ? p : 0.f;
+    float norm;
+    int len;
+  };
+  auto load = [&](Tile& t, int i) {
+    const int at = min(i, a.columns - 1);
+    const int b = (int)(((uint64_t)(uint32_t)at * a.by_group.magic) >> 32), j = at - b * c.G + h * c.G;
+    t.q.load(a.d.q + ((int64_t)b * a.d.qs_b + (int64_t)j * a.d.qs_h) * ES, q4);
+    t.norm = a.d.norm[(int64_t)b * c.HQ + j];
+    t.len = c.lens[b];
+  };
+  Tile next;
+  load(next, w * 16 + n);
+#pragma unroll 1
+  for (int i0 = w * 16; i0 < a.columns; i0 += WAVES * 16) {
+    Tile t = next;
+    load(next, i0 + WAVES * 16 + n);
+    // a column that is none takes part with a weight of 0, whatever its query holds
+    const bool live = i0 + n < a.columns && t.len >= 0;
+    if (__any(!live)) {
+      if (!live) {
+        t.q.zero();
+        t.norm = INFINITY;
       }
     }
+    f32x4 x[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) x[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < Frag<TT, D>::KS; ++j)
+#pragma unroll
+      for (int g = 0; g < NG; ++g) x[g] = mma1(k[g], t.q, x[g], j);
+    const int lo = max(P + min(t.len, c.max_len) - a.d.window, 0) - key0, sinks = a.d.sinks - key0;
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(x[g][e], a.d.sc, -t.norm));
+        const int at = 16 * g + 4 * q4 + e;
+        sum[g][e] += !WINDOW || at >= lo || at < sinks ? p : 0.f;
+      }
   }
 #pragma unroll
   for (int g = 0; g < NG; ++g)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       float v = sum[g][e];
-#pragma unroll
-      for (int d = 8; d > 0; d >>= 1) v += __shfl_xor(v, d);
-      const int slot = key0 + 16 * g + 4 * q4 + e;
-      if (n == 0 && ok[g] && slot < P) a.d.acc[meta[g] + 4 * q4 + e] += v / c.G;
+      v += dpp_f<kDppSwap1>(v);
+      v += dpp_f<kDppSwap2>(v);
+      v += dpp_f<kDppHalfMirror>(v);
+      v += dpp_f<0x140>(v);  // mirror of the row of 16
+      if (n == 0) part[w][16 * g + 4 * q4 + e] = v;
     }
+  __syncthreads();
+  if (threadIdx.x < 16 * NG) {
+    const int slot = key0 + threadIdx.x;
+    if (slot >= P) return;
+    int row0;
+    const int page = prefix_page(a, slot >> 4, &row0);
+    if (!page_ok(a.d, page)) return;
+    float v = 0.f;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) v += part[i][threadIdx.x];
+    a.d.acc[((int64_t)page * c.H + h) * c.ps + row0 + (slot & 15)] += v / c.G;
+  }
 }
 
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
-
-enum { kSh16, kSh1x4, kSh2x2, kSh4x1 };  // kernels
 
 }  // namespace
 
 SharedPlan shared_plan(const PagedView& c, int max_prefix, bool acc) {
   SharedPlan p;
   const int columns = c.batch * c.G;
-  p.kernel = c.esize == 4 ? kSh16 : columns <= 32 ? kSh1x4 : columns <= 64 ? kSh2x2 : kSh4x1;
-  const int wide = p.kernel == kSh1x4 ? 32 : p.kernel == kSh4x1 ? 128 : 64;
+  p.kernel = c.esize == 4 ? kSh16 : columns <= 64 ? kSh2x2 : kSh4x1;
+  const int wide = p.kernel == kSh4x1 ? 128 : 64;
   p.tiles = (columns + wide - 1) / wide;
-  int64_t Sp = (512 + (int64_t)c.H * p.tiles - 1) / ((int64_t)c.H * p.tiles);
-  const int most = (max_prefix + 127) / 128;
+  int Sp = 256 / (c.H * p.tiles);
+  const int most = (max_prefix + 63) / 64;
   if (Sp > most) Sp = most;
   if (Sp > 64) Sp = 64;
-  p.Sp = (int)(Sp < 1 ? 1 : Sp);
+  p.Sp = Sp < 1 ? 1 : Sp;
   p.own = paged_decode_plan(c, 0, 0, acc);
   const size_t rows = (size_t)c.batch * c.HQ;
   p.part = up256(rows * (p.Sp + p.own.S) * (c.D + 2) * 4);
@@ -507,41 +574,38 @@ hipError_t run_paged_shared(const PagedView& c, const SharedPrefix& p, const voi
   a.columns = c.batch * c.G;
   a.tiles = pl.tiles;
   a.Sp = pl.Sp;
-  const dim3 group(kShThreads), prefix((unsigned)((c.H * pl.Sp + 7) / 8 * 8 * pl.tiles)), own(pl.own.S, c.H, c.batch);
+  a.first_own = (unsigned)((c.H * pl.Sp + 7) / 8 * 8 * pl.tiles);
+  const dim3 group(kShThreads), grid(a.first_own + (unsigned)((int64_t)c.batch * c.H * pl.own.S));
   const bool d64 = c.D == 64;
-  hipError_t e;
   if (pl.kernel == kSh16) {
-    if (d64) hipLaunchKernelGGL((sh_prefix16<64>), prefix, group, 0, s, a);
-    else hipLaunchKernelGGL((sh_prefix16<128>), prefix, group, 0, s, a);
-  } else if (pl.kernel == kSh1x4) {
-    if (d64) hipLaunchKernelGGL((sh_prefix32<64, 1, 4, 32>), prefix, group, 0, s, a);
-    else hipLaunchKernelGGL((sh_prefix32<128, 1, 4, 32>), prefix, group, 0, s, a);
+    if (d64) hipLaunchKernelGGL((sh_both<F32, 64, kSh16>), grid, group, 0, s, a);
+    else hipLaunchKernelGGL((sh_both<F32, 128, kSh16>), grid, group, 0, s, a);
   } else if (pl.kernel == kSh2x2) {
-    if (d64) hipLaunchKernelGGL((sh_prefix32<64, 2, 2, 32>), prefix, group, 0, s, a);
-    else hipLaunchKernelGGL((sh_prefix32<128, 2, 2, 32>), prefix, group, 0, s, a);
+    if (d64) hipLaunchKernelGGL((sh_both<BF16, 64, kSh2x2>), grid, group, 0, s, a);
+    else hipLaunchKernelGGL((sh_both<BF16, 128, kSh2x2>), grid, group, 0, s, a);
   } else {
-    if (d64) hipLaunchKernelGGL((sh_prefix32<64, 4, 1, 64>), prefix, group, 0, s, a);
-    else hipLaunchKernelGGL((sh_prefix32<128, 4, 1, 64>), prefix, group, 0, s, a);
+    if (d64) hipLaunchKernelGGL((sh_both<BF16, 64, kSh4x1>), grid, group, 0, s, a);
+    else hipLaunchKernelGGL((sh_both<BF16, 128, kSh4x1>), grid, group, 0, s, a);
   }
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (c.esize == 4) {
-    if (d64) hipLaunchKernelGGL((pd_partial<F32, 64, false>), own, group, 0, s, a.d);
-    else hipLaunchKernelGGL((pd_partial<F32, 128, false>), own, group, 0, s, a.d);
-  } else {
-    if (d64) hipLaunchKernelGGL((pd_partial<BF16, 64, false>), own, group, 0, s, a.d);
-    else hipLaunchKernelGGL((pd_partial<BF16, 128, false>), own, group, 0, s, a.d);
-  }
-  if ((e = hipGetLastError()) != hipSuccess) return e;
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
   if ((e = d64 ? pd_join<64>(a.d, s) : pd_join<128>(a.d, s)) != hipSuccess || !acc) return e;
-  constexpr int NG = 2, KEYS = kShThreads / 64 * 16 * NG;
-  const dim3 keys((unsigned)((p.max_len + KEYS - 1) / KEYS), c.H);
-  if (c.esize == 4) {
-    if (d64) hipLaunchKernelGGL((sh_weights<F32, 64, NG>), keys, group, 0, s, a);
-    else hipLaunchKernelGGL((sh_weights<F32, 128, NG>), keys, group, 0, s, a);
-  } else {
-    if (d64) hipLaunchKernelGGL((sh_weights<BF16, 64, NG>), keys, group, 0, s, a);
-    else hipLaunchKernelGGL((sh_weights<BF16, 128, NG>), keys, group, 0, s, a);
-  }
+  a.by_group = group_div(c.G);
+  auto weights = [&](auto window) {
+    constexpr bool W = decltype(window)::value;
+    auto launch = [&](auto kernel, int ng) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)((p.max_len + 16 * ng - 1) / (16 * ng)), c.H), dim3(kWtThreads), 0, s, a);
+    };
+    if (c.esize == 4) {
+      if (d64) launch(sh_weights<F32, 64, 2, W>, 2);
+      else launch(sh_weights<F32, 128, 2, W>, 2);
+    } else {
+      if (d64) launch(sh_weights<BF16, 64, 8, W>, 8);
+      else launch(sh_weights<BF16, 128, 8, W>, 8);
+    }
+  };
+  if (window > 0) weights(std::true_type{});
+  else weights(std::false_type{});
   return hipGetLastError();
 }
 

@@ -373,8 +373,8 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
           for (int e = 0; e < 16; ++e)
             if (!sp.sees(key0 + col.key(g, e), pos)) x[g][e] = -INFINITY;
       }
-      bf16x8 pf[KT / 16];
-      col.template weigh<KT / 32, false>(x, a.sc, pf, pf);
+      bf16x8 pf[1][KT / 16];
+      col.template weigh<KT / 32, 1>(x, a.sc, pf);
       // (the compiler's transposing read waits for the copies in flight, which were
       // issued half a tile before; written out with waits of its own it was slower, 566
       // us for 545, because then the products cannot be scheduled between the reads)
@@ -386,7 +386,7 @@ __device__ __forceinline__ void rows32(const PfArgs& a) {
           const char* vs = vb + ss * 16 * D * 2;
           const s16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + col.voff[2 * dt]));
           const s16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + col.voff[2 * dt + 1]));
-          col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(join8(a0, a1), pf[ss], col.o[dt], 0, 0, 0);
+          col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(join8(a0, a1), pf[0][ss], col.o[dt], 0, 0, 0);
         }
     }
     if (careful.value) each_wild<KT>(sp, t0 + kw, t1, KW, [&](int key) { col.add_wild(v_of(key), sp.sees(key, pos)); });
@@ -478,8 +478,8 @@ __device__ __forceinline__ void few(const PfArgs& a) {
           if (!sp.sees(key0 + col.key(0, e), pos)) x[0][e] = -INFINITY;
         if (careful.value) tame<BF16, PER>(ring + u * STEP + HALF + lane * 16);
       }
-      bf16x8 pf[2], lo[2];
-      col.template weigh<1, true>(x, a.sc, pf, lo);
+      bf16x8 pf[2][2];
+      col.template weigh<1, 2>(x, a.sc, pf);
       uint32_t at[2 * DT];
 #pragma unroll
       for (int e = 0; e < 2 * DT; ++e) at[e] = lds_addr(kb) + HALF + col.voff[e];
@@ -492,10 +492,10 @@ __device__ __forceinline__ void few(const PfArgs& a) {
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         const bf16x8 a0 = join8(v0[2 * dt], v0[2 * dt + 1]), a1 = join8(v1[2 * dt], v1[2 * dt + 1]);
-        col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a0, pf[0], col.o[dt], 0, 0, 0);
-        col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1, pf[1], col.o[dt], 0, 0, 0);
-        col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a0, lo[0], col.o[dt], 0, 0, 0);
-        col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1, lo[1], col.o[dt], 0, 0, 0);
+        col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a0, pf[0][0], col.o[dt], 0, 0, 0);
+        col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1, pf[0][1], col.o[dt], 0, 0, 0);
+        col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a0, pf[1][0], col.o[dt], 0, 0, 0);
+        col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1, pf[1][1], col.o[dt], 0, 0, 0);
       }
     }
     wait_vmem<0>();

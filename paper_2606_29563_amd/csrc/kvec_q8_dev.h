@@ -1,13 +1,11 @@
 // Rows of a cache in eight bits: codes and what they stand for (kvec_q8_format).
 #pragma once
 
-#include "kvec_score_dev.h"
+#include "kvec_attn_dev.h"
 
 namespace kvec {
 
 constexpr int kPlain = -1;  // pools of the rows' own type
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 template <int FORMAT>
 struct Codes;
