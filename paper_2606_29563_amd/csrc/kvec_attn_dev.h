@@ -146,8 +146,8 @@ __device__ __forceinline__ void tame(char* lds) {
 
 // Softmax state and output of 16 query columns, NG groups of 16 keys a step.  bf16
 // probabilities go into the V product as the sum of two bf16 numbers, 2^-16 relative
-// instead of 2^-8, at twice the products.
-template <class TT, int D, int NG>
+// instead of 2^-8, at twice the products; or of three (TERMS), as exact as float32.
+template <class TT, int D, int NG, int TERMS = 2>
 struct Columns16 {
   using RG = RowGroup<TT, D>;
   static constexpr int DT = D / 16;
@@ -222,12 +222,16 @@ struct Columns16 {
     }
     if constexpr (__is_same(TT, BF16)) {
       static_assert(NG == 1, "keys of a bf16 step");
-      s16x4 hi, lo;
+      s16x4 w[TERMS];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const __bf16 top = (__bf16)p[0][i];
-        hi[i] = __builtin_bit_cast(short, top);
-        lo[i] = __builtin_bit_cast(short, (__bf16)(p[0][i] - (float)top));
+        float left = p[0][i];
+#pragma unroll
+        for (int k = 0; k < TERMS; ++k) {
+          const __bf16 top = (__bf16)left;
+          w[k][i] = __builtin_bit_cast(short, top);
+          if (k + 1 < TERMS) left -= (float)top;
+        }
       }
       uint32_t at[DT];
       vt_offsets(lane, at);
@@ -238,8 +242,8 @@ struct Columns16 {
       vt_read<0>(at, a0);
 #pragma unroll
       for (int t = 0; t < DT; ++t) {
-        o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a0[t], hi, o[t], 0, 0, 0);
-        o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a0[t], lo, o[t], 0, 0, 0);
+#pragma unroll
+        for (int k = 0; k < TERMS; ++k) o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a0[t], w[k], o[t], 0, 0, 0);
       }
     } else {
       const int n = lane & 15, c = lane >> 4;

@@ -160,8 +160,9 @@ __device__ __forceinline__ void finish(const PdArgs& a, const Visible& vis, Colu
 constexpr int kPdRing = 2;  // groups of 16 slots in flight per wave
 
 // ONE: the sequence is not split, its work-group finishes the results itself.  CALLER: 0, or
-// of another kernel, where the compiler would wait for the copies in flight at every read of
-// LDS.  (An instance for each: the host's compilation refuses a second use of one.)
+// of another kernel (kvec_paged_shared.hip), where the compiler would wait for the copies in
+// flight at every read of LDS, and probabilities have three bf16 terms, as its other part's.
+// (An instance for each: the host's compilation refuses a second use of one.)
 template <class TT, int D, bool ONE, int CALLER = 0>
 __device__ __forceinline__ void partial(const PdArgs& a, char* smem, int s, int h, int b) {
   using RG = RowGroup<TT, D>;
@@ -174,7 +175,7 @@ __device__ __forceinline__ void partial(const PdArgs& a, char* smem, int s, int 
   const int per = split_groups(vis, a.So);
   const int st0 = min(s * per, vis.groups), st1 = min(st0 + per, vis.groups);
 
-  Columns16<TT, D, 1> col;
+  Columns16<TT, D, 1, CALLER == 0 ? 2 : 3> col;
   col.clear();
   col.q.zero();
   if (n < G) col.q.load(a.q + ((int64_t)b * a.qs_b + (int64_t)(h * G + n) * a.qs_h) * ES, c);

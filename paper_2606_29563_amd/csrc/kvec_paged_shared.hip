@@ -141,7 +141,7 @@ __device__ __forceinline__ void prefix32(const ShArgs& a, char* smem_all, int id
   constexpr int ES = 2, HALF = KT * D * ES, GRPS = KT / 16, CPG = D / 32;  // CPG: copies of a group
   constexpr int PER = GRPS * CPG / CW, DT = D / 32;  // copies per wave of K and of V
   constexpr int GPW = PER < CPG ? 1 : PER / CPG;     // groups of a wave (or a part of one)
-  constexpr int TERMS = 2;
+  constexpr int TERMS = 3;  // bf16 terms of a probability
   static_assert(PER >= 1 && (PER % CPG == 0 || CPG % PER == 0), "a wave copies whole groups, or of one");
   static_assert((KW - 1) * CW * 32 * (D + 2) * 4 <= KW * RING * 2 * HALF, "states in LDS");
   __shared__ int red[CW * KW][2];
@@ -223,39 +223,53 @@ __device__ __forceinline__ void prefix32(const ShArgs& a, char* smem_all, int id
       const char* vb = kb + HALF;
       u = u + 1 == RING ? 0 : u + 1;
       if (KW > 1 && t >= t1) continue;
-      f32x16 x[KT / 32];
-      col.logits(x, kb);
       const int key0 = sp.key0(t);
-      if (!sp.open(key0) || miss) {
-#pragma unroll
-        for (int g = 0; g < KT / 32; ++g)
+      const bool masked = !sp.open(key0) || miss;
+      // Blocks of 32 keys in turn, the logits of the next one before the exponentials of this
+      // one and these before the V product of the last: the matrix cores and the vector work
+      // overlap where the instructions of the two stand together.
+      f32x16 x[2][1];
+      bf16x8 pf[2][TERMS][2];
+      auto logits = [&](int g) { col.logits(x[g & 1], kb + g * 32 * D * 2); };
+      auto weigh = [&](int g) {
+        f32x16& y = x[g & 1][0];
+        if (masked) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const int key = key0 + col.key(g, e);
-            if (!(key < P && mine.sees(key))) x[g][e] = -INFINITY;
+            if (!(key < P && mine.sees(key))) y[e] = -INFINITY;
           }
-        if (miss) {
+          if (miss) {
 #pragma unroll
-          for (int g = 0; g < GRPS; ++g)
-            if (!(key0 + 16 * g < P && has_page(key0 + 16 * g)))
+            for (int i = 0; i < 2; ++i)
+              if (!(key0 + 32 * g + 16 * i < P && has_page(key0 + 32 * g + 16 * i)))
 #pragma unroll
-              for (int e = 0; e < 8; ++e) x[g / 2][8 * (g % 2) + e] = -INFINITY;
+                for (int e = 0; e < 8; ++e) y[8 * i + e] = -INFINITY;
+          }
         }
+        col.template weigh<1, TERMS>(x[g & 1], a.d.sc, pf[g & 1]);
+      };
+      auto product = [&](int g) {
+#pragma unroll
+        for (int ss = 0; ss < 2; ++ss)
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) {
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            const char* vs = vb + (2 * g + ss) * 16 * D * 2;
+            const s16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + col.voff[2 * dt]));
+            const s16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + col.voff[2 * dt + 1]));
+            const bf16x8 v = join8(a0, a1);
+#pragma unroll
+            for (int i = 0; i < TERMS; ++i) col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[g & 1][i][ss], col.o[dt], 0, 0, 0);
+          }
+      };
+      logits(0);
+#pragma unroll
+      for (int g = 0; g < KT / 32; ++g) {
+        if (g + 1 < KT / 32) logits(g + 1);
+        weigh(g);
+        product(g);
       }
-      bf16x8 pf[TERMS][KT / 16];
-      col.template weigh<KT / 32, TERMS>(x, a.d.sc, pf);
-#pragma unroll
-      for (int ss = 0; ss < KT / 16; ++ss)
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-          const char* vs = vb + ss * 16 * D * 2;
-          const s16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + col.voff[2 * dt]));
-          const s16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + col.voff[2 * dt + 1]));
-          const bf16x8 v = join8(a0, a1);
-#pragma unroll
-          for (int i = 0; i < TERMS; ++i) col.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[i][ss], col.o[dt], 0, 0, 0);
-        }
     }
     wait_vmem<0>();
     if (careful.value) {
@@ -600,8 +614,9 @@ hipError_t run_paged_shared(const PagedView& c, const SharedPrefix& p, const voi
       if (d64) launch(sh_weights<F32, 64, 2, W>, 2);
       else launch(sh_weights<F32, 128, 2, W>, 2);
     } else {
-      if (d64) launch(sh_weights<BF16, 64, 8, W>, 8);
-      else launch(sh_weights<BF16, 128, 8, W>, 8);
+      const bool few = (int64_t)(p.max_len + 127) / 128 * c.H < 256;
+      if (d64) few ? launch(sh_weights<BF16, 64, 2, W>, 2) : launch(sh_weights<BF16, 64, 8, W>, 8);
+      else few ? launch(sh_weights<BF16, 128, 2, W>, 2) : launch(sh_weights<BF16, 128, 8, W>, 8);
     }
   };
   if (window > 0) weights(std::true_type{});
