@@ -32,39 +32,40 @@ __global__ __launch_bounds__(kRdThreads) void read_kernel(PagedView c, ReadArgs 
   constexpr int CPR = D / 16, ROWS = kRdThreads / CPR;
   const int h = blockIdx.y, b = blockIdx.z, p = threadIdx.x % CPR;
   const int n = min(max(c.lens[b], 0), c.max_len);
-  const int64_t s0 = (int64_t)blockIdx.x * ROWS + threadIdx.x / CPR;
-  if (s0 >= n) return;
-  const int s = (int)s0;
-  const int pg = (int)(((uint64_t)(uint32_t)(s >> 4) * c.gdiv.magic) >> 32), row = s - pg * c.ps;
-  const int page = c.table[(int64_t)b * c.max_pages + pg];
-  const bool ok = page >= 0 && page < c.n_pages;
-  uint4 k = make_uint4(0, 0, 0, 0), v = k;
-  float zk = 0.f, zv = 0.f;
-  if (ok) {
-    const int64_t at = (int64_t)page * c.sp + h * c.sh + row * c.sr, meta = ((int64_t)page * c.H + h) * c.ps + row;
-    k = reinterpret_cast<const uint4*>(c.k + at)[p];
-    v = reinterpret_cast<const uint4*>(c.v + at)[p];
-    zk = c.ks[meta];
-    zv = c.vs[meta];
+  for (int s = blockIdx.x * ROWS + threadIdx.x / CPR; s < n; s += gridDim.x * ROWS) {
+    const int pg = (int)(((uint64_t)(uint32_t)(s >> 4) * c.gdiv.magic) >> 32), row = s - pg * c.ps;
+    const int page = c.table[(int64_t)b * c.max_pages + pg];
+    const bool ok = page >= 0 && page < c.n_pages;
+    uint4 k = make_uint4(0, 0, 0, 0), v = k;
+    float zk = 0.f, zv = 0.f;
+    if (ok) {
+      const int64_t at = (int64_t)page * c.sp + h * c.sh + row * c.sr, meta = ((int64_t)page * c.H + h) * c.ps + row;
+      k = reinterpret_cast<const uint4*>(c.k + at)[p];
+      v = reinterpret_cast<const uint4*>(c.v + at)[p];
+      zk = c.ks[meta];
+      zv = c.vs[meta];
+    }
+    auto out = [&](const uint4& u, float z, char* dst) {
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+      float f[16];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) Codes<FORMAT>::numbers(w[i], f + 4 * i);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) f[i] *= z;
+      put<T>(dst, f);
+    };
+    out(k, zk, a.k + ((int64_t)b * a.ks[0] + h * a.ks[1] + s * a.ks[2] + 16 * p) * sizeof(T));
+    out(v, zv, a.v + ((int64_t)b * a.vs[0] + h * a.vs[1] + s * a.vs[2] + 16 * p) * sizeof(T));
   }
-  auto out = [&](const uint4& u, float z, char* dst) {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-    float f[16];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) Codes<FORMAT>::numbers(w[i], f + 4 * i);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) f[i] *= z;
-    put<T>(dst, f);
-  };
-  out(k, zk, a.k + ((int64_t)b * a.ks[0] + h * a.ks[1] + s * a.ks[2] + 16 * p) * sizeof(T));
-  out(v, zv, a.v + ((int64_t)b * a.vs[0] + h * a.vs[1] + s * a.vs[2] + 16 * p) * sizeof(T));
 }
 
 }  // namespace
 
 hipError_t run_paged_read(const PagedView& c, const ReadArgs& a, hipStream_t s) {
   const int rows = kRdThreads / (c.D / 16);
-  const dim3 grid((unsigned)((c.max_len + rows - 1) / rows), c.H, c.batch);
+  // fewer than 2^32 threads (batch * H is below 2^22)
+  const int64_t all = (c.max_len + rows - 1) / rows, most = (((int64_t)1 << 32) - 1) / ((int64_t)kRdThreads * c.H * c.batch);
+  const dim3 grid((unsigned)(all < most ? all : most), c.H, c.batch);
   auto launch = [&](auto format) {
     constexpr int F = decltype(format)::value;
     if (c.esize == 2) {

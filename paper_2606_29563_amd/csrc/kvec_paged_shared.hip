@@ -24,8 +24,8 @@ struct ShArgs {
   PdArgs d;
   const int32_t* pages;  // the prefix's
   int columns, tiles, Sp;
-  unsigned first_own;             // work-groups of the prefix, in whole eights
-  GroupDiv by_group;              // division of columns by G (both below 2^20 / 16)
+  unsigned first_own;  // work-groups of the prefix
+  GroupDiv by_group;   // division of columns by G
 };
 
 // What a column sees of the prefix's P slots: those from `lo` on, and the first `sinks`.
@@ -123,15 +123,29 @@ struct PageAhead {
   }
 };
 
-// Work-group -> (KV head, split, column tile): the column tiles of a split follow one
-// another on one XCD, whose L2 then holds the split's rows.
+// Work-group -> (KV head, split, column tile).  Work-groups go round the eight XCDs, each
+// with an L2 of its own: the column tiles of a split run on the same XCD, whose L2 then holds
+// the split's rows, or, with fewer than eight (head, split) pairs, on as few as that takes.
 __device__ __forceinline__ bool sh_item(const ShArgs& a, int id, int* h, int* split, int* tile) {
-  const int at = (id & 7) + 8 * ((id >> 3) / a.tiles);
-  *tile = (id >> 3) % a.tiles;
-  if (at >= a.d.c.H * a.Sp) return false;
+  const int pairs = a.d.c.H * a.Sp;
+  int at;
+  if (pairs % 8 == 0) {
+    at = (id & 7) + 8 * ((id >> 3) / a.tiles);
+    *tile = (id >> 3) % a.tiles;
+  } else if (8 % pairs == 0) {
+    at = (id & 7) % pairs;
+    *tile = (id >> 3) * (8 / pairs) + (id & 7) / pairs;
+  } else {
+    at = id % pairs;
+    *tile = id / pairs;
+  }
   *h = at / a.Sp;
   *split = at % a.Sp;
-  return true;
+  return *tile < a.tiles;
+}
+int64_t sh_items(int H, const SharedPlan& p) {
+  const int64_t pairs = (int64_t)H * p.Sp;
+  return 8 % pairs == 0 ? (p.tiles + 8 / pairs - 1) / (8 / pairs) * 8 : pairs * p.tiles;
 }
 
 // bf16: CW waves of 32 columns, KW times; the k-th of the KW takes every KW-th tile of KT
@@ -458,6 +472,7 @@ __global__ __launch_bounds__(kShThreads, 2) void sh_both(ShArgs a) {
 // slots in registers and goes over every fourth tile of 16 columns, its queries loaded a
 // tile ahead; the waves' sums meet in LDS.
 constexpr int kWtThreads = 256;
+constexpr int kWtMost = 1 << 13;  // work-groups of a KV head: fewer than 2^32 threads with 1024 heads
 template <class TT, int D, int NG, bool WINDOW>
 __global__ __launch_bounds__(kWtThreads, 2) void sh_weights(ShArgs a) {
   constexpr int ES = elem_bytes<TT>(), WAVES = kWtThreads / 64;
@@ -466,85 +481,86 @@ __global__ __launch_bounds__(kWtThreads, 2) void sh_weights(ShArgs a) {
   const int h = blockIdx.y, P = a.d.prefix();
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int n = lane & 15, q4 = lane >> 4;
-  const int key0 = blockIdx.x * 16 * NG;
-  if (key0 >= P) return;
-  Frag<TT, D> k[NG];
-#pragma unroll
-  for (int g = 0; g < NG; ++g) {
-    int row0 = 0;
-    const int page = key0 + 16 * g < P ? prefix_page(a, (key0 >> 4) + g, &row0) : -1;
-    k[g].zero();
-    if (page_ok(a.d, page)) k[g].load(c.k + ((int64_t)page * c.sp + (int64_t)h * c.sh + (int64_t)(row0 + n) * c.sr) * ES, q4);
-  }
-  f32x4 sum[NG];
-#pragma unroll
-  for (int g = 0; g < NG; ++g) sum[g] = f32x4{0.f, 0.f, 0.f, 0.f};
-  // queries, normaliser and length of a column (behind the last one: of that)
-  struct Tile {
-    Frag<TT, D> q;
-    float norm;
-    int len;
-  };
-  auto load = [&](Tile& t, int i) {
-    const int at = min(i, a.columns - 1);
-    const int b = (int)(((uint64_t)(uint32_t)at * a.by_group.magic) >> 32), j = at - b * c.G + h * c.G;
-    t.q.load(a.d.q + ((int64_t)b * a.d.qs_b + (int64_t)j * a.d.qs_h) * ES, q4);
-    t.norm = a.d.norm[(int64_t)b * c.HQ + j];
-    t.len = c.lens[b];
-  };
-  Tile next;
-  load(next, w * 16 + n);
 #pragma unroll 1
-  for (int i0 = w * 16; i0 < a.columns; i0 += WAVES * 16) {
-    Tile t = next;
-    load(next, i0 + WAVES * 16 + n);
-    // a column that is none takes part with a weight of 0, whatever its query holds
-    const bool live = i0 + n < a.columns && t.len >= 0;
-    if (__any(!live)) {
-      if (!live) {
-        t.q.zero();
-        t.norm = INFINITY;
-      }
+  for (int key0 = blockIdx.x * 16 * NG; key0 < P; key0 += gridDim.x * 16 * NG) {
+    Frag<TT, D> k[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      int row0 = 0;
+      const int page = key0 + 16 * g < P ? prefix_page(a, (key0 >> 4) + g, &row0) : -1;
+      k[g].zero();
+      if (page_ok(a.d, page)) k[g].load(c.k + ((int64_t)page * c.sp + (int64_t)h * c.sh + (int64_t)(row0 + n) * c.sr) * ES, q4);
     }
-    f32x4 x[NG];
+    f32x4 sum[NG];
 #pragma unroll
-    for (int g = 0; g < NG; ++g) x[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int g = 0; g < NG; ++g) sum[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // queries, normaliser and length of a column (behind the last one: of that)
+    struct Tile {
+      Frag<TT, D> q;
+      float norm;
+      int len;
+    };
+    auto load = [&](Tile& t, int i) {
+      const int at = min(i, a.columns - 1);
+      const int b = (int)(((uint64_t)(uint32_t)at * a.by_group.magic) >> 32), j = at - b * c.G + h * c.G;
+      t.q.load(a.d.q + ((int64_t)b * a.d.qs_b + (int64_t)j * a.d.qs_h) * ES, q4);
+      t.norm = a.d.norm[(int64_t)b * c.HQ + j];
+      t.len = c.lens[b];
+    };
+    Tile next;
+    load(next, w * 16 + n);
+#pragma unroll 1
+    for (int i0 = w * 16; i0 < a.columns; i0 += WAVES * 16) {
+      Tile t = next;
+      load(next, i0 + WAVES * 16 + n);
+      f32x4 x[NG];
 #pragma unroll
-    for (int j = 0; j < Frag<TT, D>::KS; ++j)
+      for (int g = 0; g < NG; ++g) x[g] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int g = 0; g < NG; ++g) x[g] = mma1(k[g], t.q, x[g], j);
-    const int lo = max(P + min(t.len, c.max_len) - a.d.window, 0) - key0, sinks = a.d.sinks - key0;
+      for (int j = 0; j < Frag<TT, D>::KS; ++j)
+#pragma unroll
+        for (int g = 0; g < NG; ++g) x[g] = mma1(k[g], t.q, x[g], j);
+      // a column that is none gives a weight of 0, whatever its query and the keys hold
+      const bool live = i0 + n < a.columns && t.len >= 0;
+      if (__any(!live)) {
+        if (!live) {
+          t.norm = INFINITY;
+#pragma unroll
+          for (int g = 0; g < NG; ++g) x[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+      }
+      const int lo = max(P + min(t.len, c.max_len) - a.d.window, 0) - key0, sinks = a.d.sinks - key0;
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(x[g][e], a.d.sc, -t.norm));
+          const int at = 16 * g + 4 * q4 + e;
+          sum[g][e] += !WINDOW || at >= lo || at < sinks ? p : 0.f;
+        }
+    }
 #pragma unroll
     for (int g = 0; g < NG; ++g)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(x[g][e], a.d.sc, -t.norm));
-        const int at = 16 * g + 4 * q4 + e;
-        sum[g][e] += !WINDOW || at >= lo || at < sinks ? p : 0.f;
+        float v = sum[g][e];
+        v += dpp_f<kDppSwap1>(v);
+        v += dpp_f<kDppSwap2>(v);
+        v += dpp_f<kDppHalfMirror>(v);
+        v += dpp_f<0x140>(v);  // mirror of the row of 16
+        if (n == 0) part[w][16 * g + 4 * q4 + e] = v;
       }
-  }
-#pragma unroll
-  for (int g = 0; g < NG; ++g)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float v = sum[g][e];
-      v += dpp_f<kDppSwap1>(v);
-      v += dpp_f<kDppSwap2>(v);
-      v += dpp_f<kDppHalfMirror>(v);
-      v += dpp_f<0x140>(v);  // mirror of the row of 16
-      if (n == 0) part[w][16 * g + 4 * q4 + e] = v;
-    }
-  __syncthreads();
-  if (threadIdx.x < 16 * NG) {
+    __syncthreads();
     const int slot = key0 + threadIdx.x;
-    if (slot >= P) return;
-    int row0;
-    const int page = prefix_page(a, slot >> 4, &row0);
-    if (!page_ok(a.d, page)) return;
-    float v = 0.f;
+    if (threadIdx.x < 16 * NG && slot < P) {
+      int row0;
+      const int page = prefix_page(a, slot >> 4, &row0);
+      float v = 0.f;
 #pragma unroll
-    for (int i = 0; i < WAVES; ++i) v += part[i][threadIdx.x];
-    a.d.acc[((int64_t)page * c.H + h) * c.ps + row0 + (slot & 15)] += v / c.G;
+      for (int i = 0; i < WAVES; ++i) v += part[i][threadIdx.x];
+      if (page_ok(a.d, page)) a.d.acc[((int64_t)page * c.H + h) * c.ps + row0 + (slot & 15)] += v / c.G;
+    }
+    __syncthreads();  // part, before the next slots
   }
 }
 
@@ -552,14 +568,27 @@ size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 }  // namespace
 
+// Two waves of columns with two halves of the slots up to 64 columns, four waves of columns
+// beyond (14 x 4 columns over 16k slots: 29.4 us with two, 34.5 with four).
+//
+// Splits of the prefix: one work-group for every compute unit, of 64 slots at least in
+// float32, of 128 with up to 64 columns and of 192 with more (below, a split's prologue and
+// state cost more than its share).  us on the device, work-groups 128 / 192 / 256 / 320 / 384:
+// 16k slots and 32 sequences (8 KV heads, 4 query heads each, d 128) 56 / 48 / 44 / 54 / 54, 4
+// sequences 33 / 27 / 24 / 26 / 25, 100 of them 161 / 114 / 92 / 96 / 90, 8k slots and 96
+// sequences (4 heads, 7 each) with weights 94 / 73 / 66 / 74 / 72.  Slots of a split at least 64
+// / 128 / 192 / 256: 2k slots and 4 sequences 14.6 / 14.5 / 15.6 / 16.5, 14 of them 24.0 / 19.7
+// / 19.1 / 20.2, 3k and 32 37.0 / 33.6 / 31.6 / 31.3, 2k and 64 of 7 heads 30.3 / 30.1 / 28.5 /
+// 27.1, 600 and 64 25.3 / 24.9 / 24.5 / 25.2; float32, 2k and 3 (4 heads, 2 each, d 64) 16.1 /
+// 19.0 / 22.2 / 25.8.
 SharedPlan shared_plan(const PagedView& c, int max_prefix, bool acc) {
   SharedPlan p;
   const int columns = c.batch * c.G;
   p.kernel = c.esize == 4 ? kSh16 : columns <= 64 ? kSh2x2 : kSh4x1;
-  const int wide = p.kernel == kSh4x1 ? 128 : 64;
+  const int wide = p.kernel == kSh4x1 ? 128 : 64, least = p.kernel == kSh16 ? 64 : p.kernel == kSh2x2 ? 128 : 192;
   p.tiles = (columns + wide - 1) / wide;
   int Sp = 256 / (c.H * p.tiles);
-  const int most = (max_prefix + 63) / 64;
+  const int most = (max_prefix + least - 1) / least;
   if (Sp > most) Sp = most;
   if (Sp > 64) Sp = 64;
   p.Sp = Sp < 1 ? 1 : Sp;
@@ -588,7 +617,7 @@ hipError_t run_paged_shared(const PagedView& c, const SharedPrefix& p, const voi
   a.columns = c.batch * c.G;
   a.tiles = pl.tiles;
   a.Sp = pl.Sp;
-  a.first_own = (unsigned)((c.H * pl.Sp + 7) / 8 * 8 * pl.tiles);
+  a.first_own = (unsigned)sh_items(c.H, pl);
   const dim3 group(kShThreads), grid(a.first_own + (unsigned)((int64_t)c.batch * c.H * pl.own.S));
   const bool d64 = c.D == 64;
   if (pl.kernel == kSh16) {
@@ -608,7 +637,8 @@ hipError_t run_paged_shared(const PagedView& c, const SharedPrefix& p, const voi
   auto weights = [&](auto window) {
     constexpr bool W = decltype(window)::value;
     auto launch = [&](auto kernel, int ng) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)((p.max_len + 16 * ng - 1) / (16 * ng)), c.H), dim3(kWtThreads), 0, s, a);
+      const int all = (p.max_len + 16 * ng - 1) / (16 * ng);
+      hipLaunchKernelGGL(kernel, dim3(all < kWtMost ? all : kWtMost, c.H), dim3(kWtThreads), 0, s, a);
     };
     if (c.esize == 4) {
       if (d64) launch(sh_weights<F32, 64, 2, W>, 2);

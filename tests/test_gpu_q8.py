@@ -200,11 +200,11 @@ def _decode(c, q, window=0, sinks=0, acc=True, max_len=None, stream=None):
 
 def _check_decode(c, q, out, lse, acc0, window=0, sinks=0, max_len=None):
     """out, lse and the accumulated weights of every slot of the pool.  A logit has two more
-    roundings than a plain dot product (the scales' products), so d + 4 of them; probabilities
-    enter the product as two bf16 terms, 2^-16 relative (2^-24 with float32 queries)."""
+    roundings than a plain dot product (the scales' products), so d + 4 of them; queries in
+    float32 and probabilities enter the products as three bf16 terms, 2^-24 relative each."""
     (kn, vn), qn = c.values(), ref.f64(q)
     got, got_lse = ref.f64(out), ref.f64(lse)
-    terms = 2.0 ** -16 if c.dt == "bf16" else 2.0 ** -23
+    terms = 2.0 ** -23
     want_acc = None if acc0 is None else ref.f64(acc0)
     slack = None if acc0 is None else np.zeros_like(want_acc)
     for i, n in enumerate(c.lens_l):

@@ -76,11 +76,11 @@ def _decode(c, q, window=0, sinks=0, acc=True, max_prefix=None, max_len=None, st
 
 def _check(c, q, out, lse, acc0, window=0, sinks=0, max_prefix=None, max_len=None, heads=None):
     """out, lse and the accumulated weights of every slot of the pool.  Bounds as for a single
-    sequence, with probabilities in two bf16 terms (2^-16); a prefix slot's weight is a sum of
-    as many terms as there are columns."""
+    sequence, with probabilities in three bf16 terms (2^-24); a prefix slot's weight is a sum
+    of as many terms as there are columns."""
     kn, vn, qn = ref.f64(c.k), ref.f64(c.v), ref.f64(q)
     got, got_lse = ref.f64(out), ref.f64(lse)
-    terms = 2.0 ** -16 if c.dt == "bf16" else 0.0
+    terms = 2.0 ** -24
     want_acc = None if acc0 is None else ref.f64(acc0)
     slack = None if acc0 is None else np.zeros_like(want_acc)
     P = max(0, min(c.P, max_prefix or len(c.pages) * c.page))
@@ -251,6 +251,49 @@ def test_rows_that_are_no_numbers(gpu_lib, dt, b):
     nan = c.acc[p, 1, r].isnan().cpu()
     assert nan[low:].all() and nan[:sinks].all() and not nan[sinks:low].any()
     assert not c.acc[p, 0, r].isnan().any() and c.acc[p[sinks:low], 1, r[sinks:low]].equal(acc0[p[sinks:low], 1, r[sinks:low]])
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("window", [0, 50])
+def test_rows_that_are_none_do_not_matter(gpu_lib, dt, window):
+    """Padding rows: neither what their queries hold nor keys that are no numbers, which no
+    sequence sees, reach the weights; a batch of padding alone leaves everything as it is."""
+    import torch
+    c = Shared(gpu_lib, 300, [20, -1, 30, -5, -2**31], 2, 4, 64, 16, dt, seed=23).cuda()
+    q = c.rand(5, 8, 64).to(_dt(dt)).cuda()
+    q[1], q[3], q[4] = float("nan"), float("inf"), 1e30
+    p, r = c._rows(c.pages, 300)
+    if window:
+        c.k[p[100], :, r[100]] = float("nan")  # behind every window
+    acc0 = c.acc.clone()
+    out, lse = _decode(c, q, window)
+    _check(c, q.nan_to_num(0, 0, 0), out, lse, acc0, window)
+    assert torch.all(out[[1, 3, 4]] == 0) and torch.all(lse[[1, 3, 4]] == -math.inf)
+    c.lens.fill_(-1)
+    c.k[p[200], :, r[200]] = float("nan")
+    before = c.acc.clone()
+    out, lse = _decode(c, q, window)
+    assert torch.all(out == 0) and torch.all(lse == -math.inf) and c.acc.nan_to_num(7).equal(before.nan_to_num(7))
+
+
+@pytest.mark.parametrize("H,b,G", [(1, 300, 16), (3, 200, 8), (4, 400, 7), (2, 700, 3)])
+def test_many_columns(gpu_lib, H, b, G):
+    """More column tiles than compute units have work-groups, on few KV heads: every column and
+    tile, against single sequences' attention of the same rows."""
+    import torch
+    kv = gpu_lib
+    lens = [(7 * i) % 23 for i in range(b)]
+    c = Shared(kv, 256, lens, H, G, 64, 16, "bf16", seed=b).cuda()
+    q = c.rand(b, H * G, 64).bfloat16().cuda()
+    out, lse = _decode(c, q, acc=False)
+    table = torch.cat([c.pages[None, :16].expand(b, -1), c.table], 1).contiguous()
+    one = kv.PagedConfig(b, H, H * G, 64, 16, c.cfg.n_pages, table.shape[1], kv.KVEC_BF16)
+    o, l = torch.empty_like(out), torch.empty_like(lse)
+    ws = torch.empty(kv.kvec_paged_decode_workspace_size(one), dtype=torch.uint8, device="cuda")
+    kv.kvec_paged_decode(one, q, c.k, c.v, table, c.lens + 256, o, ws, lse=l)
+    # sums of the same terms in other orders, each within its bounds
+    assert torch.all((o - out).abs() <= 2.0 ** -14 * c.v.float().nan_to_num().abs().max())
+    assert torch.all((l - lse).abs() <= 2.0 ** -14 * (1 + lse.abs()))
 
 
 def test_extreme_logits(gpu_lib):
