@@ -32,56 +32,44 @@ struct CodeGroup {
   static __device__ __forceinline__ int swizzle(int r) { return D == 128 ? r >> 1 & 7 : (r ^ r >> 2) & 3; }
 };
 
-// Reads of K and the transposing ones of V, written out with the wait in the same
-// statement: for those that the compiler issues it waits for every copy in flight first (it
-// cannot tell the addresses apart), which would stop the copies of the next step.
-// Two pieces (four) of the two groups, OFF bytes apart.
+// Reads of a step's K pieces of two groups, OFF bytes apart, and the transposing ones of its
+// V, written out with one wait for all in the same statement: for those that the compiler
+// issues it waits for every copy in flight first (it cannot tell the addresses apart), which
+// would stop the copies of the next step.
 template <int OFF>
-__device__ __forceinline__ void k_read(const uint32_t (&at)[1], u32x4 (&u)[2][1]) {
+__device__ __forceinline__ void kv_read(const uint32_t (&at)[1], const uint32_t (&vat)[4], u32x4 (&u)[2][1], i32x2 (&v)[4]) {
   asm volatile(
-      "ds_read_b128 %0, %2\n\t"
-      "ds_read_b128 %1, %2 offset:%3\n\t"
+      "ds_read_b128 %0, %6\n\t"
+      "ds_read_b128 %1, %6 offset:%11\n\t"
+      "ds_read_b64_tr_b8 %2, %7\n\t"
+      "ds_read_b64_tr_b8 %3, %8\n\t"
+      "ds_read_b64_tr_b8 %4, %9\n\t"
+      "ds_read_b64_tr_b8 %5, %10\n\t"
       "s_waitcnt lgkmcnt(0)"
-      : "=&v"(u[0][0]), "=&v"(u[1][0])
-      : "v"(at[0]), "n"(OFF)
+      : "=&v"(u[0][0]), "=&v"(u[1][0]), "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+      : "v"(at[0]), "v"(vat[0]), "v"(vat[1]), "v"(vat[2]), "v"(vat[3]), "n"(OFF)
       : "memory");
 }
 template <int OFF>
-__device__ __forceinline__ void k_read(const uint32_t (&at)[2], u32x4 (&u)[2][2]) {
+__device__ __forceinline__ void kv_read(const uint32_t (&at)[2], const uint32_t (&vat)[8], u32x4 (&u)[2][2], i32x2 (&v)[8]) {
   asm volatile(
-      "ds_read_b128 %0, %4\n\t"
-      "ds_read_b128 %1, %5\n\t"
-      "ds_read_b128 %2, %4 offset:%6\n\t"
-      "ds_read_b128 %3, %5 offset:%6\n\t"
+      "ds_read_b128 %0, %12\n\t"
+      "ds_read_b128 %1, %13\n\t"
+      "ds_read_b128 %2, %12 offset:%22\n\t"
+      "ds_read_b128 %3, %13 offset:%22\n\t"
+      "ds_read_b64_tr_b8 %4, %14\n\t"
+      "ds_read_b64_tr_b8 %5, %15\n\t"
+      "ds_read_b64_tr_b8 %6, %16\n\t"
+      "ds_read_b64_tr_b8 %7, %17\n\t"
+      "ds_read_b64_tr_b8 %8, %18\n\t"
+      "ds_read_b64_tr_b8 %9, %19\n\t"
+      "ds_read_b64_tr_b8 %10, %20\n\t"
+      "ds_read_b64_tr_b8 %11, %21\n\t"
       "s_waitcnt lgkmcnt(0)"
-      : "=&v"(u[0][0]), "=&v"(u[0][1]), "=&v"(u[1][0]), "=&v"(u[1][1])
-      : "v"(at[0]), "v"(at[1]), "n"(OFF)
-      : "memory");
-}
-__device__ __forceinline__ void vt_read8(const uint32_t (&at)[4], i32x2 (&v)[4]) {
-  asm volatile(
-      "ds_read_b64_tr_b8 %0, %4\n\t"
-      "ds_read_b64_tr_b8 %1, %5\n\t"
-      "ds_read_b64_tr_b8 %2, %6\n\t"
-      "ds_read_b64_tr_b8 %3, %7\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
-      : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3])
-      : "memory");
-}
-__device__ __forceinline__ void vt_read8(const uint32_t (&at)[8], i32x2 (&v)[8]) {
-  asm volatile(
-      "ds_read_b64_tr_b8 %0, %8\n\t"
-      "ds_read_b64_tr_b8 %1, %9\n\t"
-      "ds_read_b64_tr_b8 %2, %10\n\t"
-      "ds_read_b64_tr_b8 %3, %11\n\t"
-      "ds_read_b64_tr_b8 %4, %12\n\t"
-      "ds_read_b64_tr_b8 %5, %13\n\t"
-      "ds_read_b64_tr_b8 %6, %14\n\t"
-      "ds_read_b64_tr_b8 %7, %15\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7])
-      : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]), "v"(at[7])
+      : "=&v"(u[0][0]), "=&v"(u[0][1]), "=&v"(u[1][0]), "=&v"(u[1][1]), "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]),
+        "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7])
+      : "v"(at[0]), "v"(at[1]), "v"(vat[0]), "v"(vat[1]), "v"(vat[2]), "v"(vat[3]), "v"(vat[4]), "v"(vat[5]), "v"(vat[6]),
+        "v"(vat[7]), "n"(OFF)
       : "memory");
 }
 
@@ -140,14 +128,24 @@ struct Columns16Q8 {
     }
   }
 
-  // Products with the codes of the two groups at `grp`; lane: keys 4c + i of each.
-  __device__ __forceinline__ void logits(f32x4 (&x)[2], const char* grp, int lane) const {
-    const int n = lane & 15, c = lane >> 4;
-    uint32_t at[KP];
-    u32x4 u[2][KP];
+  // What a step has of its two groups in LDS, K's at kgrp and V's at vgrp.
+  struct Step {
+    u32x4 u[2][KP];  // K pieces
+    i32x2 v[DT];     // elements of V: of eight rows each
+    __device__ __forceinline__ void read(const char* kgrp, const char* vgrp, int lane) {
+      const int n = lane & 15, c = lane >> 4, r = 4 * c + (n >> 1 & 3);
+      uint32_t at[KP], vat[DT];
 #pragma unroll
-    for (int p = 0; p < KP; ++p) at[p] = lds_addr(grp) + n * D + (((c + 4 * p) ^ CG::swizzle(n)) << 4);
-    k_read<CG::BYTES>(at, u);
+      for (int p = 0; p < KP; ++p) at[p] = lds_addr(kgrp) + n * D + (((c + 4 * p) ^ CG::swizzle(n)) << 4);
+      const uint32_t base = lds_addr(vgrp) + (n >> 3) * CG::BYTES + r * D + (n & 1) * 8;
+#pragma unroll
+      for (int t = 0; t < DT; ++t) vat[t] = base + ((t ^ CG::swizzle(r)) << 4);
+      kv_read<CG::BYTES>(at, vat, u, v);
+    }
+  };
+
+  // Products with the codes of the two groups; lane: keys 4c + i of each.
+  __device__ __forceinline__ void logits(f32x4 (&x)[2], const u32x4 (&u)[2][KP]) const {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       x[g] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -165,7 +163,7 @@ struct Columns16Q8 {
 
   // One step of the online softmax (see Columns16): x base-2 logits, -inf where masked;
   // z the values' scales, 0 where masked.
-  __device__ __forceinline__ void absorb(const f32x4 (&x)[2], const f32x4 (&z)[2], const char* vgrp, int lane) {
+  __device__ __forceinline__ void absorb(const f32x4 (&x)[2], const f32x4 (&z)[2], const i32x2 (&v)[DT]) {
     float mx = m;
 #pragma unroll
     for (int g = 0; g < 2; ++g) mx = fmaxf(mx, fmaxf(fmaxf(x[g][0], x[g][1]), fmaxf(x[g][2], x[g][3])));
@@ -191,13 +189,6 @@ struct Columns16Q8 {
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[t][i] *= f;
     }
-    const int n = lane & 15, c = lane >> 4, r = 4 * c + (n >> 1 & 3);
-    uint32_t at[DT];
-    const uint32_t base = lds_addr(vgrp) + (n >> 3) * CG::BYTES + r * D + (n & 1) * 8;
-#pragma unroll
-    for (int t = 0; t < DT; ++t) at[t] = base + ((t ^ CG::swizzle(r)) << 4);
-    i32x2 v[DT];
-    vt_read8(at, v);
 #pragma unroll
     for (int t = 0; t < DT; ++t) {
       const bf16x8 a = Codes<FORMAT>::bf16((uint32_t)v[t][0], (uint32_t)v[t][1]);
@@ -278,30 +269,55 @@ __device__ __forceinline__ void partial_q8(const PdArgs& a, char* smem, int s, i
     }
   };
   float* lg = a.logits && n < G ? a.logits + (((int64_t)b * a.c.H + h) * G + n) * a.pad + 4 * c : nullptr;
+  // A step's logits are stored by the next one, before its copies: behind them, the wait for
+  // the copies in flight would wait for the first of these as well.
+  f32x4 kept[2];
+  float* kept_at[2] = {nullptr, nullptr};
+  auto store = [&]() {
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+      if (kept_at[g]) *reinterpret_cast<f32x4*>(kept_at[g]) = kept[g];
+  };
   auto step = [&](auto U, int k) {
     constexpr int u = decltype(U)::value;
     wait_vmem<(kQ8Ring - 1) * LOADS>();
+    // all that the step needs in registers: the next copy into the ring slot starts before
+    // the products (behind them, and with V read after the exponentials: 16 sequences of 8k
+    // to 16k int8 slots without weights 86.7 us for 81.7, a window of 4096 of 8 sequences in
+    // e4m3 14.6 for 13.6)
+    typename Columns16Q8<D, FORMAT, NQ>::Step in;
     const char* slot = ring + u * STEP;
+    in.read(slot, slot + 2 * CG::BYTES, lane);
+    f32x4 kz[2], vz[2];
+    bool there[2], all[2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      kz[g] = zk[u][g];
+      vz[g] = zv[u][g];
+      there[g] = ok[u][g];
+      all[g] = whole[u][g];
+      asm volatile("" : "+v"(kz[g]), "+v"(vz[g]));  // waited for here, not behind the next copy
+    }
+    store();
+    copy(U, k + kQ8Ring);
     f32x4 x[2];
-    col.logits(x, slot, lane);
+    col.logits(x, in.u);
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       const int s0 = vis.slot0(group_of(k, g));
-      x[g] *= zk[u][g] * a.sc;
-      if (!whole[u][g]) {
+      x[g] *= kz[g] * a.sc;
+      if (!all[g]) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (!(ok[u][g] && vis.sees(s0 + 4 * c + i))) {
+          if (!(there[g] && vis.sees(s0 + 4 * c + i))) {
             x[g][i] = -INFINITY;
-            zv[u][g][i] = 0.f;
+            vz[g][i] = 0.f;
           }
       }
-      if (lg && group_of(k, g) < vis.groups) *reinterpret_cast<f32x4*>(lg + s0) = x[g];
+      kept[g] = x[g];
+      kept_at[g] = lg && group_of(k, g) < vis.groups ? lg + s0 : nullptr;
     }
-    col.absorb(x, zv[u], slot + 2 * CG::BYTES, lane);
-    // the ring slot is read out before the next copy into it starts
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    copy(U, k + kQ8Ring);
+    col.absorb(x, vz, in.v);
   };
   if (count > 0) {
     copy(std::integral_constant<int, 0>{}, 0);
@@ -315,12 +331,13 @@ __device__ __forceinline__ void partial_q8(const PdArgs& a, char* smem, int s, i
     }
     if (k < count) step(std::integral_constant<int, 0>{}, k);
   }
+  store();
   wait_vmem<0>();
   finish<D, ONE>(a, vis, col, smem, s, h, b);
 }
 
 template <int D, int FORMAT, int NQ, bool ONE>
-__global__ __launch_bounds__(kPdThreads) void pd_partial_q8(PdArgs a) {
+__global__ __launch_bounds__(kPdThreads, 2) void pd_partial_q8(PdArgs a) {
   constexpr int RING = kPdWaves * kQ8Ring * kQ8Step<D>;
   __shared__ __align__(1024) char smem[RING > kPdMerge<D> ? RING : kPdMerge<D>];
   partial_q8<D, FORMAT, NQ, ONE>(a, smem, blockIdx.x, blockIdx.y, blockIdx.z);

@@ -97,13 +97,18 @@ __device__ __forceinline__ void move_rows(const EvArgs& a, int b, int h, int cou
     const uint4 kx = reinterpret_cast<const uint4*>(a.c.k + from)[p];
     const uint4 vx = reinterpret_cast<const uint4*>(a.c.v + from)[p];
     if (p == 0) {
+      // (all loads before the first store, which could be to the same memory for all that the
+      // compiler knows: each would wait for the one before)
       const int64_t f = (ps * (int64_t)H + h) * a.c.ps + rs, t = (pd * (int64_t)H + h) * a.c.ps + rd;
-      a.acc[t] = a.acc[f];
-      a.pos[t] = a.pos[f];
+      const float weight = a.acc[f];
+      const int32_t at = a.pos[f];
       if (a.c.ks) {
-        a.c.ks[t] = a.c.ks[f];
-        a.c.vs[t] = a.c.vs[f];
+        const float zk = a.c.ks[f], zv = a.c.vs[f];
+        a.c.ks[t] = zk;
+        a.c.vs[t] = zv;
       }
+      a.acc[t] = weight;
+      a.pos[t] = at;
     }
     reinterpret_cast<uint4*>(a.c.k + to)[p] = kx;
     reinterpret_cast<uint4*>(a.c.v + to)[p] = vx;
