@@ -144,6 +144,35 @@ __device__ __forceinline__ void tame(char* lds) {
   }
 }
 
+// Products of 16 columns with the 16 keys of each of NG float32 fragments.  Sums of d terms
+// in turn are off by up to d / 2 steps of the largest, and a logit's error is its weight's:
+// eight sums, added in pairs, have a quarter to half of that (2k slots, d 64, logits up to 60:
+// outputs off by 0.9 to 1.7e-6 with one sum, by 4 to 7e-7 with eight and `scaled`).
+template <int D, int NG>
+__device__ __forceinline__ void dots(const Frag<F32, D> (&k)[NG], const Frag<F32, D>& q, f32x4 (&x)[NG]) {
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    f32x4 y[8];
+#pragma unroll
+    for (int j = 0; j < Frag<F32, D>::KS; ++j) y[j % 8] = mma1(k[g], q, j < 8 ? f32x4{0.f, 0.f, 0.f, 0.f} : y[j % 8], j);
+#pragma unroll
+    for (int n = 4; n > 0; n /= 2)
+#pragma unroll
+      for (int c = 0; c < n; ++c) y[c] += y[c + n];
+    x[g] = y[0];
+  }
+}
+
+// x s, s + lo being the scale: y its rounding, and what that leaves.  A logit of 60 is off by
+// 2e-6 by its rounding alone, and so would its weight be.  (Infinite products leave a number.)
+__device__ __forceinline__ void scaled(f32x4 x, f32x4 s, f32x4 lo, f32x4& y, f32x4& left) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[i] = x[i] * s[i];
+    left[i] = fminf(fmaf(x[i], lo[i], fmaf(x[i], s[i], -y[i])), 1.f);
+  }
+}
+
 // Softmax state and output of 16 query columns, NG groups of 16 keys a step.  bf16
 // probabilities go into the V product as the sum of two bf16 numbers, 2^-16 relative
 // instead of 2^-8, at twice the products; or of three (TERMS), as exact as float32.
@@ -193,10 +222,20 @@ struct Columns16 {
       for (int g = 0; g < NG; ++g) x[g] = mma1(k[g], q, x[g], j);
   }
 
+  // ... of float32, in several sums each.
+  __device__ __forceinline__ void logits_in_sums(f32x4 (&x)[NG], const char* grp, int lane) const {
+    Frag<TT, D> k[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) k[g].load_lds(reinterpret_cast<const uint4*>(grp + g * RG::BYTES), lane & 15, lane >> 4, RG::SWZ);
+    dots(k, q, x);
+  }
+
   // One step of the online softmax: x are base-2 logits, -inf where masked.
   // A column that has seen no key keeps m = -inf, and the exponentials use 0
   // for it: 2^(-inf - 0) = 0 instead of 2^(-inf + inf).
-  __device__ __forceinline__ void absorb(const f32x4 (&x)[NG], const char* vgrp, int lane) {
+  // LEFT: the logits are x + left.
+  template <bool LEFT = false>
+  __device__ __forceinline__ void absorb(const f32x4 (&x)[NG], const char* vgrp, int lane, const f32x4* left = nullptr) {
     float mx = m;
 #pragma unroll
     for (int g = 0; g < NG; ++g)
@@ -211,7 +250,7 @@ struct Columns16 {
     for (int g = 0; g < NG; ++g)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        p[g][i] = __builtin_amdgcn_exp2f(x[g][i] - ref);
+        p[g][i] = __builtin_amdgcn_exp2f(LEFT ? x[g][i] - ref + left[g][i] : x[g][i] - ref);
         l += p[g][i];
       }
     if (__any(f != 1.f)) {

@@ -148,22 +148,32 @@ struct Columns16Q8 {
   __device__ __forceinline__ void logits(f32x4 (&x)[2], const u32x4 (&u)[2][KP]) const {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-      x[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+      // The first terms of a float32 query in a sum for every product and all others in one:
+      // a running sum would be rounded at its full size with each.
+      constexpr int SUMS = NQ > 1 ? 2 * KP + 1 : 1;
+      f32x4 y[SUMS];
+#pragma unroll
+      for (int j = 0; j < SUMS; ++j) y[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int p = 0; p < KP; ++p) {
         const bf16x8 k0 = Codes<FORMAT>::bf16(u[g][p][0], u[g][p][1]), k1 = Codes<FORMAT>::bf16(u[g][p][2], u[g][p][3]);
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
-          x[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[i][2 * p], x[g], 0, 0, 0);
-          x[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[i][2 * p + 1], x[g], 0, 0, 0);
+          f32x4 &a = y[NQ == 1 ? 0 : i == 0 ? 2 * p + 1 : 0], &b = y[NQ == 1 ? 0 : i == 0 ? 2 * p + 2 : 0];
+          a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[i][2 * p], a, 0, 0, 0);
+          b = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[i][2 * p + 1], b, 0, 0, 0);
         }
       }
+      x[g] = y[0];
+      if constexpr (KP == 2 && NQ > 1) x[g] += (y[1] + y[2]) + (y[3] + y[4]);
+      else if constexpr (NQ > 1) x[g] += y[1] + y[2];
     }
   }
 
-  // One step of the online softmax (see Columns16): x base-2 logits, -inf where masked;
+  // One step of the online softmax (see Columns16): x base-2 logits, -inf where masked, of
+  // float32 queries less `left`;
   // z the values' scales, 0 where masked.
-  __device__ __forceinline__ void absorb(const f32x4 (&x)[2], const f32x4 (&z)[2], const i32x2 (&v)[DT]) {
+  __device__ __forceinline__ void absorb(const f32x4 (&x)[2], const f32x4 (&left)[2], const f32x4 (&z)[2], const i32x2 (&v)[DT]) {
     float mx = m;
 #pragma unroll
     for (int g = 0; g < 2; ++g) mx = fmaxf(mx, fmaxf(fmaxf(x[g][0], x[g][1]), fmaxf(x[g][2], x[g][3])));
@@ -178,7 +188,7 @@ struct Columns16Q8 {
     for (int g = 0; g < 2; ++g)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float e = __builtin_amdgcn_exp2f(x[g][i] - ref);
+        const float e = __builtin_amdgcn_exp2f(NQ > 1 ? x[g][i] - ref + left[g][i] : x[g][i] - ref);
         l += e;
         w[4 * g + i] = e * z[g][i];
       }
@@ -300,12 +310,19 @@ __device__ __forceinline__ void partial_q8(const PdArgs& a, char* smem, int s, i
     }
     store();
     copy(U, k + kQ8Ring);
-    f32x4 x[2];
+    f32x4 x[2], left[2];
     col.logits(x, in.u);
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       const int s0 = vis.slot0(group_of(k, g));
-      x[g] *= kz[g] * a.sc;
+      if constexpr (NQ > 1) {
+        f32x4 sc = kz[g] * a.sc, lo;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lo[i] = fmaf(kz[g][i], a.sc_lo, fmaf(kz[g][i], a.sc, -sc[i]));
+        scaled(x[g], sc, lo, x[g], left[g]);
+      } else {
+        x[g] *= kz[g] * a.sc;
+      }
       if (!all[g]) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -317,7 +334,7 @@ __device__ __forceinline__ void partial_q8(const PdArgs& a, char* smem, int s, i
       kept[g] = x[g];
       kept_at[g] = lg && group_of(k, g) < vis.groups ? lg + s0 : nullptr;
     }
-    col.absorb(x, vz, in.v);
+    col.absorb(x, left, vz, in.v);
   };
   if (count > 0) {
     copy(std::integral_constant<int, 0>{}, 0);

@@ -24,7 +24,7 @@ struct PdArgs {
   float* lse;
   float* acc;
   int window, sinks, S, pad;
-  float sc;       // log2(e) / sqrt(d)
+  float sc, sc_lo;  // log2(e) / sqrt(d), and what its rounding leaves
   int s0, So;     // the splits of the sequences' own slots: So from s0 on (all but a prefix's)
   const int32_t* prefix_len;  // null, or the slots before them, at most max_prefix
   int max_prefix;
@@ -161,7 +161,8 @@ constexpr int kPdRing = 2;  // groups of 16 slots in flight per wave
 
 // ONE: the sequence is not split, its work-group finishes the results itself.  CALLER: 0, or
 // of another kernel (kvec_paged_shared.hip), where the compiler would wait for the copies in
-// flight at every read of LDS, and probabilities have three bf16 terms, as its other part's.
+// flight at every read of LDS, and what the other part has more exactly is so here as well:
+// three bf16 terms of a probability, float32 logits.
 // (An instance for each: the host's compilation refuses a second use of one.)
 template <class TT, int D, bool ONE, int CALLER = 0>
 __device__ __forceinline__ void partial(const PdArgs& a, char* smem, int s, int h, int b) {
@@ -245,14 +246,21 @@ __device__ __forceinline__ void partial(const PdArgs& a, char* smem, int s, int 
     const char* slot = ring + u * STEP;
     const int s0 = vis.slot0(first + k * kPdWaves);
     f32x4 x[1];
-    x[0] = col.logits(slot, lane) * a.sc;
+    constexpr bool LEFT = CALLER != 0 && __is_same(TT, F32);
+    f32x4 left[1];
+    if constexpr (LEFT) {
+      col.logits_in_sums(x, slot, lane);
+      scaled(x[0], f32x4{a.sc, a.sc, a.sc, a.sc}, f32x4{a.sc_lo, a.sc_lo, a.sc_lo, a.sc_lo}, x[0], left[0]);
+    } else {
+      x[0] = col.logits(slot, lane) * a.sc;
+    }
     if (!whole[u]) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (!(ok[u] && vis.sees(s0 + 4 * c + i))) x[0][i] = -INFINITY;
     }
     if (lg) *reinterpret_cast<f32x4*>(lg + s0) = x[0];
-    col.absorb(x, slot + RG::BYTES, lane);
+    col.template absorb<LEFT>(x, slot + RG::BYTES, lane, left);
     // the ring slot is read out before the next copy into it starts
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     copy(U, k + kPdRing);
@@ -464,7 +472,9 @@ inline PdArgs pd_args(const PagedView& c, const PagedDecodePlan& p, const void* 
   a.sinks = sinks;
   a.S = p.S;
   a.pad = (c.max_len + 15) & ~15;
-  a.sc = (float)(1.4426950408889634 / sqrt((double)c.D));
+  const double sc = 1.4426950408889634 / sqrt((double)c.D);
+  a.sc = (float)sc;
+  a.sc_lo = (float)(sc - a.sc);
   a.s0 = 0;
   a.So = p.S;
   a.prefix_len = nullptr;

@@ -400,9 +400,11 @@ __device__ __forceinline__ void prefix16(const ShArgs& a, char* smem, int id) {
       const char* kb = smem + u * BUF;
       const int key0 = sp.key0(t);
       f32x4 x[GRPS];
-      col.logits(x, kb, lane);
+      col.logits_in_sums(x, kb, lane);
+      f32x4 left[GRPS];
 #pragma unroll
-      for (int g = 0; g < GRPS; ++g) x[g] *= a.d.sc;
+      for (int g = 0; g < GRPS; ++g)
+        scaled(x[g], f32x4{a.d.sc, a.d.sc, a.d.sc, a.d.sc}, f32x4{a.d.sc_lo, a.d.sc_lo, a.d.sc_lo, a.d.sc_lo}, x[g], left[g]);
       if (!sp.open(key0) || missing[u]) {
 #pragma unroll
         for (int g = 0; g < GRPS; ++g) {
@@ -415,7 +417,7 @@ __device__ __forceinline__ void prefix16(const ShArgs& a, char* smem, int id) {
           }
         }
       }
-      col.absorb(x, kb + GRPS * RG::BYTES, lane);
+      col.template absorb<true>(x, kb + GRPS * RG::BYTES, lane, left);
     }
     if (careful.value) {
 #pragma unroll 1
@@ -514,12 +516,16 @@ __global__ __launch_bounds__(kWtThreads, 2) void sh_weights(ShArgs a) {
       Tile t = next;
       load(next, i0 + WAVES * 16 + n);
       f32x4 x[NG];
+      if constexpr (__is_same(TT, F32)) {
+        dots(k, t.q, x);
+      } else {
 #pragma unroll
-      for (int g = 0; g < NG; ++g) x[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int g = 0; g < NG; ++g) x[g] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < Frag<TT, D>::KS; ++j)
+        for (int j = 0; j < Frag<TT, D>::KS; ++j)
 #pragma unroll
-        for (int g = 0; g < NG; ++g) x[g] = mma1(k[g], t.q, x[g], j);
+          for (int g = 0; g < NG; ++g) x[g] = mma1(k[g], t.q, x[g], j);
+      }
       // a column that is none gives a weight of 0, whatever its query and the keys hold
       const bool live = i0 + n < a.columns && t.len >= 0;
       if (__any(!live)) {
