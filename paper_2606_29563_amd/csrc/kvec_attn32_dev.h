@@ -91,13 +91,20 @@ struct Columns32 {
   template <int NB, int TERMS>
   __device__ __forceinline__ void weigh(const f32x16 (&x)[NB], float sc, bf16x8 (&p)[TERMS][2 * NB]) {
     float sum;
-    auto against = [&](float ref) {
+    auto against = [&](float ref, auto huge) {
       sum = 0.f;
 #pragma unroll
       for (int g = 0; g < NB; ++g)
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
-          float v0 = __builtin_amdgcn_exp2f(fmaf(x[g][e], sc, -ref)), v1 = __builtin_amdgcn_exp2f(fmaf(x[g][e + 1], sc, -ref));
+          float v0, v1;
+          if constexpr (decltype(huge)::value) {
+            v0 = __builtin_amdgcn_exp2f(rounded(x[g][e], sc) - ref);
+            v1 = __builtin_amdgcn_exp2f(rounded(x[g][e + 1], sc) - ref);
+          } else {
+            v0 = __builtin_amdgcn_exp2f(fmaf(x[g][e], sc, -ref));
+            v1 = __builtin_amdgcn_exp2f(fmaf(x[g][e + 1], sc, -ref));
+          }
           sum += v0;
           sum += v1;
 #pragma unroll
@@ -112,7 +119,7 @@ struct Columns32 {
           }
         }
     };
-    against(m);
+    against(m, std::false_type{});
     if (__any(!(sum <= 4096.f))) {  // inf or NaN: exponentials against -inf
       float mx = x[0][0];
 #pragma unroll
@@ -129,7 +136,10 @@ struct Columns32 {
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[dt][e] *= f;
-      against(ref);
+      // Beyond 2^24 the rounding of the largest logit, which the reference is, is more than 1:
+      // against it the logit itself would weigh anything.
+      if (TERMS == 3 && __any(fabsf(ref) > 0x1p24f)) against(ref, std::true_type{});
+      else against(ref, std::false_type{});
     }
     l += sum;
   }

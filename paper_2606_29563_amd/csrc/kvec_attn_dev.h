@@ -163,13 +163,20 @@ __device__ __forceinline__ void dots(const Frag<F32, D> (&k)[NG], const Frag<F32
   }
 }
 
+// A product that is rounded before anything is added to it.
+__device__ __forceinline__ float rounded(float x, float s) {
+#pragma clang fp contract(off)
+  return x * s;
+}
+
 // x s, s + lo being the scale: y its rounding, and what that leaves.  A logit of 60 is off by
-// 2e-6 by its rounding alone, and so would its weight be.  (Infinite products leave a number.)
+// 2e-6 by its rounding alone, and so would its weight be.  (Where y is infinite or its steps
+// are more than 1, a number within 1, which leaves the largest logit's weight one.)
 __device__ __forceinline__ void scaled(f32x4 x, f32x4 s, f32x4 lo, f32x4& y, f32x4& left) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    y[i] = x[i] * s[i];
-    left[i] = fminf(fmaf(x[i], lo[i], fmaf(x[i], s[i], -y[i])), 1.f);
+    y[i] = rounded(x[i], s[i]);
+    left[i] = fmaxf(fminf(fmaf(x[i], lo[i], fmaf(x[i], s[i], -y[i])), 1.f), -1.f);
   }
 }
 

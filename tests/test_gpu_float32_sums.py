@@ -54,3 +54,74 @@ def test_decode_q8(gpu_lib, fmt):
     gpu_lib.kvec_paged_decode_q8(cfg, q, k, k, z, z, table, lens, out, ws, lse=lse)
     assert abs(lse.item() - 64 * V * held / 8) <= BOUND
     assert abs(out - held).max().item() <= 2.0 ** -23
+
+
+# Logits from 2^20 to 2^100 and more, whose steps are up to 2^76: the largest of three is above
+# the others by far more than a step, so its value is the output, exactly, and it the log-sum-exp
+# to three half steps (sum, scaling, logarithm: d / 2 + 3 with sums of equal signs).
+HUGE = [10, 14, 20, 35, 50]
+
+
+def _huge(power):
+    import torch
+    k = torch.zeros((2, 1, 16, 64), device="cuda")
+    v = torch.randn((2, 1, 16, 64), generator=torch.Generator().manual_seed(power)).cuda()
+    for slot, x in enumerate((-3.0, 1.37, 0.61)):
+        k[1, 0, slot] = x * 2.0 ** power
+    q = torch.full((1, 1, 64), 1.1 * 2.0 ** power, device="cuda")
+    return q, k, v, 64 * q[0, 0, 0].double().item() * k[1, 0, 1, 0].double().item() / 8
+
+
+@pytest.mark.parametrize("power", HUGE)
+@pytest.mark.parametrize("where", ["prefix", "own"])
+def test_huge_logits_shared(gpu_lib, where, power):
+    import torch
+    cfg = gpu_lib.PagedConfig(1, 1, 1, 64, 16, 2, 1, gpu_lib.KVEC_F32)
+    q, k, v, x = _huge(power)
+    one = torch.ones(1, dtype=torch.int32, device="cuda")
+    n = [3 * one, 0 * one] if where == "prefix" else [0 * one, 3 * one]
+    out, lse = torch.empty_like(q), torch.empty((1, 1), device="cuda")
+    ws = torch.empty(gpu_lib.kvec_paged_decode_shared_workspace_size(cfg, 16, 16), dtype=torch.uint8, device="cuda")
+    gpu_lib.kvec_paged_decode_shared(cfg, q, k, v, one, n[0], one.view(1, 1), n[1], out, ws, lse=lse)
+    # (the weight cancels but for the rounding of its product and quotient)
+    assert torch.all((out[0, 0] - v[1, 0, 1]).abs() <= 2.0 ** -22 * v[1, 0, 1].abs())
+    assert abs(lse.item() - x) <= 35 * 2.0 ** -24 * x
+
+
+@pytest.mark.parametrize("power", HUGE)
+@pytest.mark.parametrize("where", ["prefix", "own"])
+@pytest.mark.parametrize("b", [1, 70])
+def test_huge_logits_shared_bf16(gpu_lib, b, where, power):
+    """(Three bf16 terms of a weight are 2^-24 relative.)"""
+    import torch
+    cfg = gpu_lib.PagedConfig(b, 1, 1, 64, 16, 2, 1, gpu_lib.KVEC_BF16)
+    q, k, v, _ = _huge(power)
+    q, k, v = q.bfloat16().repeat(b, 1, 1), k.bfloat16(), v.bfloat16()
+    x = 64 * q[0, 0, 0].double().item() * k[1, 0, 1, 0].double().item() / 8
+    one, all_ = torch.ones(1, dtype=torch.int32, device="cuda"), torch.ones(b, dtype=torch.int32, device="cuda")
+    n = [3 * one, 0 * all_] if where == "prefix" else [0 * one, 3 * all_]
+    out, lse = torch.empty((b, 1, 64), device="cuda"), torch.empty((b, 1), device="cuda")
+    ws = torch.empty(gpu_lib.kvec_paged_decode_shared_workspace_size(cfg, 16, 16), dtype=torch.uint8, device="cuda")
+    gpu_lib.kvec_paged_decode_shared(cfg, q, k, v, one, n[0], all_.view(b, 1), n[1], out, ws, lse=lse)
+    assert torch.all((out[:, 0] - v[1, 0, 1].float()).abs() <= 2.0 ** -22 * v[1, 0, 1].float().abs())
+    assert torch.all((lse.double() - x).abs() <= 35 * 2.0 ** -24 * x)
+
+
+@pytest.mark.parametrize("power", HUGE)
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_huge_logits_q8(gpu_lib, fmt, power):
+    import torch
+    form, code, top = (gpu_lib.KVEC_Q8_INT8, torch.int8, 127.0) if fmt == "int8" else (gpu_lib.KVEC_Q8_E4M3, torch.float8_e4m3fn, 448.0)
+    cfg = gpu_lib.PagedQ8Config(1, 1, 1, 64, 16, 2, 1, gpu_lib.KVEC_F32, form)
+    q, k, v, _ = _huge(power)
+    kz = (k.abs().amax(-1) / top).clamp(min=2.0 ** -126)
+    kc = (torch.sign(k) * top).to(code)
+    vc, vz = torch.round(v.clamp(-1, 1) * 100).to(code), torch.full((2, 1, 16), 0.01, device="cuda")
+    one = torch.ones(1, dtype=torch.int32, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty((1, 1), device="cuda")
+    ws = torch.empty(gpu_lib.kvec_paged_decode_q8_workspace_size(cfg), dtype=torch.uint8, device="cuda")
+    gpu_lib.kvec_paged_decode_q8(cfg, q, kc, vc, kz, vz, one.view(1, 1), 3 * one, out, ws, lse=lse)
+    want = vc[1, 0, 1].float() * 0.01
+    assert torch.all((out[0, 0] - want).abs() <= 2.0 ** -21 * want.abs())
+    x = 64 * q[0, 0, 0].double().item() * top * kz[1, 0, 1].double().item() / 8
+    assert abs(lse.item() - x) <= 35 * 2.0 ** -24 * x
