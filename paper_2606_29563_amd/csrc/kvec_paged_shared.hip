@@ -509,42 +509,52 @@ __global__ __launch_bounds__(kWtThreads, 2) void sh_weights(ShArgs a) {
       t.norm = a.d.norm[(int64_t)b * c.HQ + j];
       t.len = c.lens[b];
     };
-    Tile next;
-    load(next, w * 16 + n);
+    // Beyond 2^24 a normaliser's rounding is more than 1 (see Columns32::weigh): such columns are
+    // left for a second time round.
+    bool huge = false;
+    auto columns = [&](auto again) {
+      Tile next;
+      load(next, w * 16 + n);
 #pragma unroll 1
-    for (int i0 = w * 16; i0 < a.columns; i0 += WAVES * 16) {
-      Tile t = next;
-      load(next, i0 + WAVES * 16 + n);
-      f32x4 x[NG];
-      if constexpr (__is_same(TT, F32)) {
-        dots(k, t.q, x);
-      } else {
-#pragma unroll
-        for (int g = 0; g < NG; ++g) x[g] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < Frag<TT, D>::KS; ++j)
-#pragma unroll
-          for (int g = 0; g < NG; ++g) x[g] = mma1(k[g], t.q, x[g], j);
-      }
-      // a column that is none gives a weight of 0, whatever its query and the keys hold
-      const bool live = i0 + n < a.columns && t.len >= 0;
-      if (__any(!live)) {
-        if (!live) {
-          t.norm = INFINITY;
+      for (int i0 = w * 16; i0 < a.columns; i0 += WAVES * 16) {
+        Tile t = next;
+        load(next, i0 + WAVES * 16 + n);
+        f32x4 x[NG];
+        if constexpr (__is_same(TT, F32)) {
+          dots(k, t.q, x);
+        } else {
 #pragma unroll
           for (int g = 0; g < NG; ++g) x[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int j = 0; j < Frag<TT, D>::KS; ++j)
+#pragma unroll
+            for (int g = 0; g < NG; ++g) x[g] = mma1(k[g], t.q, x[g], j);
         }
+        // a column that is none gives a weight of 0, whatever its query and the keys hold
+        const bool big = fabsf(t.norm) > 0x1p24f, live = i0 + n < a.columns && t.len >= 0 && big == again.value;
+        huge |= big;
+        if (__any(!live)) {
+          if (!live) {
+            t.norm = INFINITY;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) x[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+          }
+        }
+        const int lo = max(P + min(t.len, c.max_len) - a.d.window, 0) - key0, sinks = a.d.sinks - key0;
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float y = again.value ? rounded(x[g][e], a.d.sc) - t.norm : fmaf(x[g][e], a.d.sc, -t.norm);
+            if (again.value && y > 0.f) y = 0.f;  // (the same products, added up in another order)
+            const float p = __builtin_amdgcn_exp2f(y);
+            const int at = 16 * g + 4 * q4 + e;
+            sum[g][e] += !WINDOW || at >= lo || at < sinks ? p : 0.f;
+          }
       }
-      const int lo = max(P + min(t.len, c.max_len) - a.d.window, 0) - key0, sinks = a.d.sinks - key0;
-#pragma unroll
-      for (int g = 0; g < NG; ++g)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(x[g][e], a.d.sc, -t.norm));
-          const int at = 16 * g + 4 * q4 + e;
-          sum[g][e] += !WINDOW || at >= lo || at < sinks ? p : 0.f;
-        }
-    }
+    };
+    columns(std::false_type{});
+    if (__builtin_expect(__any(huge), false)) columns(std::true_type{});
 #pragma unroll
     for (int g = 0; g < NG; ++g)
 #pragma unroll

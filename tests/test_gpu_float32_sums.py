@@ -80,9 +80,10 @@ def test_huge_logits_shared(gpu_lib, where, power):
     q, k, v, x = _huge(power)
     one = torch.ones(1, dtype=torch.int32, device="cuda")
     n = [3 * one, 0 * one] if where == "prefix" else [0 * one, 3 * one]
-    out, lse = torch.empty_like(q), torch.empty((1, 1), device="cuda")
-    ws = torch.empty(gpu_lib.kvec_paged_decode_shared_workspace_size(cfg, 16, 16), dtype=torch.uint8, device="cuda")
-    gpu_lib.kvec_paged_decode_shared(cfg, q, k, v, one, n[0], one.view(1, 1), n[1], out, ws, lse=lse)
+    out, lse, acc = torch.empty_like(q), torch.empty((1, 1), device="cuda"), torch.zeros((2, 1, 16), device="cuda")
+    ws = torch.empty(gpu_lib.kvec_paged_decode_shared_workspace_size(cfg, 16, 16, True), dtype=torch.uint8, device="cuda")
+    gpu_lib.kvec_paged_decode_shared(cfg, q, k, v, one, n[0], one.view(1, 1), n[1], out, ws, lse=lse, acc=acc)
+    assert acc[1, 0, 1] == 1 and acc.sum() == 1
     # (the weight cancels but for the rounding of its product and quotient)
     assert torch.all((out[0, 0] - v[1, 0, 1]).abs() <= 2.0 ** -22 * v[1, 0, 1].abs())
     assert abs(lse.item() - x) <= 35 * 2.0 ** -24 * x
@@ -100,9 +101,14 @@ def test_huge_logits_shared_bf16(gpu_lib, b, where, power):
     x = 64 * q[0, 0, 0].double().item() * k[1, 0, 1, 0].double().item() / 8
     one, all_ = torch.ones(1, dtype=torch.int32, device="cuda"), torch.ones(b, dtype=torch.int32, device="cuda")
     n = [3 * one, 0 * all_] if where == "prefix" else [0 * one, 3 * all_]
-    out, lse = torch.empty((b, 1, 64), device="cuda"), torch.empty((b, 1), device="cuda")
-    ws = torch.empty(gpu_lib.kvec_paged_decode_shared_workspace_size(cfg, 16, 16), dtype=torch.uint8, device="cuda")
-    gpu_lib.kvec_paged_decode_shared(cfg, q, k, v, one, n[0], all_.view(b, 1), n[1], out, ws, lse=lse)
+    out, lse, acc = torch.empty((b, 1, 64), device="cuda"), torch.empty((b, 1), device="cuda"), torch.zeros((2, 1, 16), device="cuda")
+    ws = torch.empty(gpu_lib.kvec_paged_decode_shared_workspace_size(cfg, 16, 16, True), dtype=torch.uint8, device="cuda")
+    # (with the own slots of several sequences in one page, there is no acc)
+    gpu_lib.kvec_paged_decode_shared(cfg, q, k, v, one, n[0], all_.view(b, 1), n[1], out, ws, lse=lse,
+                                     acc=acc if where == "prefix" or b == 1 else None)
+    # the prefix's weights are made of logits that are added up in another order: a step of them may
+    # be all of the weight
+    assert torch.all((acc >= 0) & (acc <= b)) and acc.sum() == acc[1, 0, 1]
     assert torch.all((out[:, 0] - v[1, 0, 1].float()).abs() <= 2.0 ** -22 * v[1, 0, 1].float().abs())
     assert torch.all((lse.double() - x).abs() <= 35 * 2.0 ** -24 * x)
 
