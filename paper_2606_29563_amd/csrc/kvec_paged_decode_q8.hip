@@ -374,14 +374,21 @@ hipError_t launch(const PdArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// Splits: as many work-groups as for rows of more bytes (paged_decode_plan); a wave's step
-// is twice as many slots.
+// Splits: up to 1024 work-groups, in whole rounds of the 512 that run at once (two a compute unit),
+// of 64 groups of slots at least, or 256 work-groups.  us in a graph, e4m3 without weights, 8 KV
+// heads of d 128, sequences of half to all of the length, so / with up to 1024 work-groups in no
+// whole rounds: 12 of 8000 35.4 / 40.8, 32 of 4000 43.2 / 49.8, 20 of 8000 54.8 / 57.6, of
+// 12000 76.7 / 81.1; always one round instead takes 32 of 12000 in int8 from 140 to 148, and 1536
+// work-groups or splits half as long gain nothing that holds.  Up to 256 slots a sequence stays in
+// one piece (with weights, int8, in one / split: 256 slots 9.1 / 10.3, 300 11.0 / 10.3, 512 12.3 /
+// 9.9).
 PagedDecodePlan paged_decode_q8_plan(const PagedView& c, int window, int sinks, bool acc) {
   const int64_t bh = (int64_t)c.batch * c.H;
   const int groups = most_groups(c, window, sinks);
   auto per_bh = [&](int64_t work_groups) { return (work_groups + bh - 1) / bh; };
-  int64_t S = per_bh(1024);
+  int64_t S = 1024 / bh;
   if (S > groups / 64) S = groups / 64;
+  if (bh * S > 512) S = bh * S / 512 * 512 / bh;
   if (S < per_bh(256)) S = per_bh(256);
   const int most_s = (groups + 2 * kPdWaves - 1) / (2 * kPdWaves);
   if (S > most_s) S = most_s;
