@@ -590,7 +590,8 @@ kvec_status kvec_paged_decode_shared_workspace_size(const kvec_paged_config* cfg
  * The others as for kvec_paged_decode, also for what masked slots hold and for logits
  * that are no numbers (a NaN or +infinity among a row's logits makes the weights that it
  * adds NaN).  With acc a page must have one place, in the prefix or in one row of the
- * table.  batch * n_q_heads must be below 2^20 (KVEC_ERR_UNSUPPORTED). */
+ * table.  batch * n_q_heads must be below 2^20, and with acc batch * n_kv_heads *
+ * ceil(max_len / 1024) below 2^24 (KVEC_ERR_UNSUPPORTED). */
 kvec_status kvec_paged_decode_shared(const kvec_paged_config* cfg,
                                      const void* q, const int64_t q_strides[2],
                                      const void* k_pool, const void* v_pool,

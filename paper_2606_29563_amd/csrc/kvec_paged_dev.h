@@ -10,7 +10,7 @@
 namespace kvec {
 namespace {
 
-constexpr int kPdThreads = 256;
+constexpr int kPdThreads = kJoinThreads;
 constexpr int kPdWaves = kPdThreads / 64;
 
 struct PdArgs {
@@ -320,6 +320,7 @@ __device__ __forceinline__ float wave_total(float v) {
 // 131k slots 124 us for 118, one of 32k with 16 query heads on one KV head 25.2 for 21.6, of
 // 8k without weights 12.7 for 11.9.)
 constexpr int kPdAccGroups = kPdThreads / 4;
+static_assert(16 * kPdAccGroups == kJoinSlots, "slots of a work-group");
 constexpr int kPdAhead = 8;  // outputs loaded ahead by a thread
 
 template <int D, bool ACC>

@@ -62,6 +62,9 @@ PagedDecodePlan paged_decode_q8_plan(const PagedView& c, int window, int sinks, 
 hipError_t run_paged_decode_q8(const PagedView& c, const void* q, const int64_t qs[2], int window, int sinks,
                                float* out, float* lse, float* acc, char* ws, hipStream_t s);
 
+constexpr int kJoinSlots = 1024;  // slots whose weights a work-group of the join adds
+constexpr int kJoinThreads = 256;
+
 // What a batch's sequences begin with.
 struct SharedPrefix {
   const int32_t* pages;

@@ -134,6 +134,14 @@ kvec_status set_lens(PagedView* v, const int32_t* table, const int32_t* lens, in
   return KVEC_OK;
 }
 
+// Behind a prefix the splits are always joined, and with weights by a work-group for every
+// kJoinSlots own slots of a (sequence, KV head): fewer than 2^32 threads.  (The calls without a
+// prefix split, and so join, fewer than 1024 such pairs only.)
+kvec_status check_join(const PagedView& c, bool acc) {
+  const int64_t chunks = (c.max_len + kJoinSlots - 1) / kJoinSlots;
+  return acc && (int64_t)c.batch * c.H * chunks * kJoinThreads >= (int64_t)1 << 32 ? KVEC_ERR_UNSUPPORTED : KVEC_OK;
+}
+
 // A prompt's launch stays below 2^32 threads.  Up to eight a row, and 512 for every
 // (sequence, KV head), can pass that from 2^28 rows on.
 kvec_status check_plan(const PrefillShape& a, const PfPlan& p) {
@@ -352,11 +360,12 @@ kvec_status kvec_paged_evict(const kvec_paged_config* cfg, int32_t budget, int32
 kvec_status kvec_paged_decode_shared_workspace_size(const kvec_paged_config* cfg, int32_t max_prefix, int32_t max_len,
                                                     int32_t with_acc, size_t* bytes) {
   PagedView c;
-  const kvec_status st = make_shared(cfg, &c);
+  kvec_status st = make_shared(cfg, &c);
   if (st != KVEC_OK) return st;
   if (!bytes || max_prefix < 1 || max_len < 1 || max_len > c.max_pages * c.ps) return KVEC_ERR_INVALID;
   if (max_prefix > kMaxLen) return KVEC_ERR_UNSUPPORTED;
   c.max_len = max_len;
+  if ((st = check_join(c, with_acc != 0)) != KVEC_OK) return st;
   *bytes = shared_plan(c, max_prefix, with_acc != 0).total();
   return KVEC_OK;
 }
@@ -378,6 +387,7 @@ kvec_status kvec_paged_decode_shared(const kvec_paged_config* cfg, const void* q
       !aligned_or_null(acc, 4))
     return KVEC_ERR_INVALID;
   if ((int64_t)n_prefix_pages * c.ps > kMaxLen) return KVEC_ERR_UNSUPPORTED;
+  if ((st = check_join(c, acc != nullptr)) != KVEC_OK) return st;
   const int total = max_prefix + max_len;  // (both at most 2^20)
   const int w = window >= total ? 0 : window;
   const int sinks = w == 0 ? 0 : n_sinks < total ? n_sinks : total;
