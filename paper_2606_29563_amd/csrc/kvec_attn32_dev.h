@@ -37,6 +37,7 @@ struct Columns32 {
   bf16x8 q[KS];
   f32x16 o[DT];
   float m, l;  // reference (base-2 logits); this lane's part of the sum
+  bool far;    // the reference of one of the wave's columns is beyond 2^24 (kept for three terms)
   int n, hh;   // column of the lane, which half of the keys it holds
   int koff[KS];          // bytes of the lane's K fragments in a block of 32 rows
   uint32_t voff[2 * DT];  // ... of its V reads in 16 rows: of the first (2 dt) and the last four of eight
@@ -62,6 +63,7 @@ struct Columns32 {
   __device__ __forceinline__ void clear() {
     m = -INFINITY;
     l = 0.f;
+    far = false;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -88,19 +90,24 @@ struct Columns32 {
 
   // Probabilities of a tile's logits, -inf where masked, as 16-key steps of the V product:
   // the sum of TERMS bf16 numbers, each the rounding of what those before it leave.
+  // With three terms, a column whose reference is beyond 2^24 weighs rounded logits: the rounding
+  // of the largest one, which the reference is, is more than 1 there, and against it the logit
+  // itself would weigh anything.  So do all its tiles, and equal logits weigh the same in each;
+  // the columns beside it keep the exact difference.
   template <int NB, int TERMS>
   __device__ __forceinline__ void weigh(const f32x16 (&x)[NB], float sc, bf16x8 (&p)[TERMS][2 * NB]) {
     float sum;
-    auto against = [&](float ref, auto huge) {
+    auto against = [&](float ref, auto some_far) {
+      const bool mine = fabsf(ref) > 0x1p24f;
       sum = 0.f;
 #pragma unroll
       for (int g = 0; g < NB; ++g)
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
           float v0, v1;
-          if constexpr (decltype(huge)::value) {
-            v0 = __builtin_amdgcn_exp2f(rounded(x[g][e], sc) - ref);
-            v1 = __builtin_amdgcn_exp2f(rounded(x[g][e + 1], sc) - ref);
+          if constexpr (decltype(some_far)::value) {
+            v0 = __builtin_amdgcn_exp2f(mine ? rounded(x[g][e], sc) - ref : fmaf(x[g][e], sc, -ref));
+            v1 = __builtin_amdgcn_exp2f(mine ? rounded(x[g][e + 1], sc) - ref : fmaf(x[g][e + 1], sc, -ref));
           } else {
             v0 = __builtin_amdgcn_exp2f(fmaf(x[g][e], sc, -ref));
             v1 = __builtin_amdgcn_exp2f(fmaf(x[g][e + 1], sc, -ref));
@@ -120,7 +127,7 @@ struct Columns32 {
         }
     };
     against(m, std::false_type{});
-    if (__any(!(sum <= 4096.f))) {  // inf or NaN: exponentials against -inf
+    if (__any(!(sum <= 4096.f)) || (TERMS == 3 && far)) {  // inf or NaN: exponentials against -inf
       float mx = x[0][0];
 #pragma unroll
       for (int e = 0; e < 16; ++e)
@@ -136,9 +143,8 @@ struct Columns32 {
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[dt][e] *= f;
-      // Beyond 2^24 the rounding of the largest logit, which the reference is, is more than 1:
-      // against it the logit itself would weigh anything.
-      if (TERMS == 3 && __any(fabsf(ref) > 0x1p24f)) against(ref, std::true_type{});
+      if constexpr (TERMS == 3) far = __any(fabsf(ref) > 0x1p24f);
+      if (TERMS == 3 && far) against(ref, std::true_type{});
       else against(ref, std::false_type{});
     }
     l += sum;
