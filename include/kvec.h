@@ -518,6 +518,9 @@ kvec_status kvec_paged_decode_workspace_size(const kvec_paged_config* cfg, int32
  *               normaliser (-inf with no visible slot).
  *   acc         nullable device in/out: acc[s] += mean over the G query heads of
  *               p_{j,s}, every visible slot (always the same bits: no atomics).
+ *               p is 2^(logit - normaliser) of float32 numbers: half a step of the
+ *               normaliser shows in it, and where base-2 logits pass 2^24 slots with
+ *               equal largest ones may count for up to 1 each.
  *   ws          device workspace of kvec_paged_decode_workspace_size() bytes.
  * What masked and missing slots hold (NaN too) never matters.  A head whose visible
  * logits are all -infinity counts as one with no visible slot (and adds nothing to acc);

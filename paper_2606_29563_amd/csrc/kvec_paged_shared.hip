@@ -509,8 +509,11 @@ __global__ __launch_bounds__(kWtThreads, 2) void sh_weights(ShArgs a) {
       t.norm = a.d.norm[(int64_t)b * c.HQ + j];
       t.len = c.lens[b];
     };
-    // Beyond 2^24 a normaliser's rounding is more than 1 (see Columns32::weigh): such columns are
-    // left for a second time round.
+    // The logits are those of the first launch, bit for bit: the 16x16x32 product adds up as the
+    // 32x32x16 one does (0 of 614400 dot products of d 64 and 128 differ).  So a weight passes 1 by
+    // the normaliser's rounding at most, which beyond 2^16 is more than 2^-8, and from 2^24 on, where
+    // logits are rounded (see Columns32::weigh), more than 1: columns beyond 2^16 are left for a second
+    // time round, which holds them to 1.
     bool huge = false;
     auto columns = [&](auto again) {
       Tile next;
@@ -531,7 +534,7 @@ __global__ __launch_bounds__(kWtThreads, 2) void sh_weights(ShArgs a) {
             for (int g = 0; g < NG; ++g) x[g] = mma1(k[g], t.q, x[g], j);
         }
         // a column that is none gives a weight of 0, whatever its query and the keys hold
-        const bool big = fabsf(t.norm) > 0x1p24f, live = i0 + n < a.columns && t.len >= 0 && big == again.value;
+        const bool big = fabsf(t.norm) > 0x1p16f, live = i0 + n < a.columns && t.len >= 0 && big == again.value;
         huge |= big;
         if (__any(!live)) {
           if (!live) {
@@ -545,8 +548,11 @@ __global__ __launch_bounds__(kWtThreads, 2) void sh_weights(ShArgs a) {
         for (int g = 0; g < NG; ++g)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            float y = again.value ? rounded(x[g][e], a.d.sc) - t.norm : fmaf(x[g][e], a.d.sc, -t.norm);
-            if (again.value && y > 0.f) y = 0.f;  // (the same products, added up in another order)
+            float y = fmaf(x[g][e], a.d.sc, -t.norm);
+            if constexpr (again.value) {
+              if (fabsf(t.norm) > 0x1p24f) y = rounded(x[g][e], a.d.sc) - t.norm;
+              if (y > 0.f) y = 0.f;
+            }
             const float p = __builtin_amdgcn_exp2f(y);
             const int at = 16 * g + 4 * q4 + e;
             sum[g][e] += !WINDOW || at >= lo || at < sinks ? p : 0.f;

@@ -71,3 +71,80 @@ def test_a_far_column_leaves_its_neighbours_exact(gpu_lib, b, c, t):
     out, _ = _call(gpu_lib, cfg, q, k, v, [1], 2, [[0]] * b, [0] * b)
     assert torch.all((out[0] - 1).abs() <= 2.0 ** -22)
     assert torch.all((out[1:].double() - 1 / (1 + math.exp(-2 * t / 8))).abs() <= 2.0 ** -19)
+
+
+def _winners(b, G, H, P, d, size, window, seed, page=16):
+    """Queries of b sequences, keys of a prefix of P slots, in which each sequence's own key
+    beats all others: key i is query i, of the length that makes its base-2 logit about `size`.
+    With a window, a key that would beat all of them lies before it."""
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    q = torch.randn((b, 1, d), generator=g)
+    q = q / q.norm(dim=-1, keepdim=True) * math.sqrt(size * math.sqrt(d) / 1.4426950408889634)
+    slots = [P - 1 - i for i in range(b)]
+    pages = (P + page - 1) // page
+    k = torch.randn((pages * page, d), generator=g)
+    k[slots] = q[:, 0]
+    if window:
+        k[10] = 4 * q.sum((0, 1))
+    k = k.view(pages, 1, page, d).expand(pages, H, page, d).contiguous()
+    v = torch.randn(k.shape, generator=g)
+    return q.repeat(1, H * G, 1).bfloat16().cuda(), k.bfloat16().cuda(), v.bfloat16().cuda(), slots
+
+
+WEIGHTS = [  # sequences, G, H, P: few and many columns, keys of 32 and of 128 slots a work-group
+    (3, 2, 1, 150), (70, 1, 1, 150), (20, 3, 2, 170), (3, 2, 32, 1100), (70, 1, 33, 1001)]
+
+
+@pytest.mark.parametrize("size", [2.0 ** 16.4, 2.0 ** 18.4, 2.0 ** 20.4, 2.0 ** 22.4, 2.0 ** 23.4, 2.0 ** 26, 2.0 ** 40, 2.0 ** 90])
+@pytest.mark.parametrize("window", [0, 120])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("b,G,H,P", WEIGHTS)
+def test_weights_of_far_columns(gpu_lib, b, G, H, P, d, window, size):
+    """Every sequence gives its whole weight to its own key of the prefix, however large its
+    logits are: 2^(logit - normaliser), which is the logit rounded to float32, so off by half a
+    step of it and the exponential's rounding, and never more than 1; from 2^24 on the logits
+    are rounded too and the weight is 1.  All other slots get nothing: their logits are lower
+    by thousands and more."""
+    import torch
+    q, k, v, slots = _winners(b, G, H, P, d, size, window, b + P)
+    cfg = gpu_lib.PagedConfig(b, H, H * G, d, 16, k.shape[0], 1, gpu_lib.KVEC_BF16)
+    acc = torch.zeros(k.shape[:3], device="cuda")
+    out, lse = _call(gpu_lib, cfg, q, k, v, list(range(k.shape[0])), P, [[-1]] * b, [0] * b, acc, window, 4 if window else 0)
+    flat = acc.transpose(1, 2).reshape(-1, H)
+    own = flat[slots]
+    top = (lse.double() / math.log(2)).max().item()
+    step = 0.0 if top > 1.01 * 2.0 ** 24 else 2.0 ** (math.floor(math.log2(top * 1.0001)) - 23)
+    assert top > 2.0 ** 16
+    assert torch.all((own <= 1) & (own >= 2.0 ** (-step / 2) - 2.0 ** -22)), (own.min(), own.max(), step)
+    flat[slots] = 0
+    assert torch.all(flat == 0)
+    want = v.transpose(1, 2).reshape(-1, H, d)[slots].float()
+    assert torch.all((out.view(b, H, G, d) - want[:, :, None]).abs() <= 2.0 ** -22 * want[:, :, None].abs())
+
+
+def test_weights_of_far_columns_and_others(gpu_lib):
+    """Far columns among ordinary ones, padding rows and missing pages: the ordinary ones' weights
+    are those of the same batch without the far ones' (bounds of two sums of the same terms)."""
+    import torch
+    b, G, H, P, d = 70, 1, 32, 1100, 64
+    q, k, v, slots = _winners(b, G, H, P, d, 2.0 ** 30, 0, 3)
+    near = torch.randn((b, H, d), generator=torch.Generator().manual_seed(4)).bfloat16().cuda()
+    near *= 2.0 ** -12  # (logits of the far keys to a few)
+    far = torch.zeros(b, dtype=torch.bool)
+    far[[0, 17, 33, 40, 69]] = True
+    lens = torch.zeros(b, dtype=torch.int32)
+    lens[[5, 17, 60]] = -1  # one of the far ones is none
+    mixed = torch.where(far[:, None, None].cuda(), q, near)
+    cfg = gpu_lib.PagedConfig(b, H, H, d, 16, k.shape[0], 1, gpu_lib.KVEC_BF16)
+    pages = list(range(k.shape[0]))
+    pages[20] = -1
+    accs = [torch.zeros(k.shape[:3], device="cuda") for _ in range(2)]
+    _call(gpu_lib, cfg, mixed, k, v, pages, P, [[-1]] * b, lens.tolist(), accs[0])
+    _call(gpu_lib, cfg, near, k, v, pages, P, [[-1]] * b, torch.where(far, -1, lens).tolist(), accs[1])
+    got = (accs[0].double() - accs[1].double()).transpose(1, 2).reshape(-1, H)
+    want = torch.zeros_like(got)
+    want[[s for i, s in enumerate(slots) if far[i] and lens[i] >= 0]] = 1
+    # 62 weights of at most 1, each off by 2^-15 in either batch
+    assert torch.all((got - want).abs() <= 62 * 2.0 ** -14)
+    assert torch.all(accs[0][20] == 0)
