@@ -543,7 +543,8 @@ __global__ __launch_bounds__(kWtThreads, 2) void sh_weights(ShArgs a) {
             for (int g = 0; g < NG; ++g) x[g] = f32x4{0.f, 0.f, 0.f, 0.f};
           }
         }
-        const int lo = max(P + min(t.len, c.max_len) - a.d.window, 0) - key0, sinks = a.d.sinks - key0;
+        // counted from the lane's first slot: a register for every slot of the lane less
+        const int first = key0 + 4 * q4, lo = max(P + min(t.len, c.max_len) - a.d.window, 0) - first, sinks = a.d.sinks - first;
 #pragma unroll
         for (int g = 0; g < NG; ++g)
 #pragma unroll
@@ -554,7 +555,7 @@ __global__ __launch_bounds__(kWtThreads, 2) void sh_weights(ShArgs a) {
               if (y > 0.f) y = 0.f;
             }
             const float p = __builtin_amdgcn_exp2f(y);
-            const int at = 16 * g + 4 * q4 + e;
+            const int at = 16 * g + e;
             sum[g][e] += !WINDOW || at >= lo || at < sinks ? p : 0.f;
           }
       }
