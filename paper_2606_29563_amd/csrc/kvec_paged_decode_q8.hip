@@ -353,6 +353,9 @@ __device__ __forceinline__ void partial_q8(const PdArgs& a, char* smem, int s, i
   finish<D, ONE>(a, vis, col, smem, s, h, b);
 }
 
+// (Float32 queries, d 128: five registers are spilled before the loop and read back behind it.  16
+// sequences of 8k to 16k slots, 8 KV heads of 4 query heads, without weights: 94.7 us in int8, 91.7 in e4m3,
+// 4.5 and 4.6 TB/s.)
 template <int D, int FORMAT, int NQ, bool ONE>
 __global__ __launch_bounds__(kPdThreads, 2) void pd_partial_q8(PdArgs a) {
   constexpr int RING = kPdWaves * kQ8Ring * kQ8Step<D>;

@@ -451,7 +451,10 @@ __device__ __forceinline__ void prefix16(const ShArgs& a, char* smem, int id) {
 enum { kSh16 = 1, kSh2x2, kSh4x1 };  // how the prefix's columns are laid out
 
 // The prefix's work-groups first: at most one for every compute unit as long as their
-// columns allow it, so that those of the own slots share the units with them.
+// columns allow it, so that those of the own slots share the units with them.  Not so in float32
+// with d 128: the rings of the own slots' waves are 128 KiB, and the registers are those of one
+// work-group a unit too (8 KV heads of 4 query heads, 16384 slots and own ones of 550 to 1061: 8
+// sequences 84.9 us, 32 of them 174, where the bytes take 37 and 68).
 template <class TT, int D, int KERNEL>
 __global__ __launch_bounds__(kShThreads, 2) void sh_both(ShArgs a) {
   constexpr int OWN = kPdWaves * kPdRing * 2 * RowGroup<TT, D>::BYTES, PREFIX = KERNEL == kSh16 ? 4 * 32 * D * 4 : 4 * 2 * 32 * D * 2;
@@ -473,6 +476,13 @@ __global__ __launch_bounds__(kShThreads, 2) void sh_both(ShArgs a) {
 // What the prefix's slots receive: every wave of a work-group has the keys of the same 16 NG
 // slots in registers and goes over every fourth tile of 16 columns, its queries loaded a
 // tile ahead; the waves' sums meet in LDS.
+//
+// bf16: 128 slots a work-group (NG 8) where that makes 256 of them, one for every compute unit,
+// else 32 (NG 2).  us of the whole call, d 128, NG 2 / 4 / 8: 8 KV heads of 4 query heads, 4
+// sequences behind 500 slots 15.9 / 17.2 / 19.5, 2000 17.4 / 17.8 / 20.1, 4096 (256 work-groups of 128
+// slots) 21.0 / 21.2 / 21.1, 8192 31.1 / 32.4 / 30.0, 32 behind 16384 71.0 / 63.9 / 60.6; 4 KV heads of 7, 96
+// sequences behind 4096 (128 of them) 51.5 / 47.0 / 50.6, behind 8191 74.9 / 65.7 / 62.6, with a window of
+// 6000 70.5 / 61.2 / 61.7.  8 takes 250 registers, two waves a vector unit.
 constexpr int kWtThreads = 256;
 constexpr int kWtMost = 1 << 13;  // work-groups of a KV head: fewer than 2^32 threads with 1024 heads
 template <class TT, int D, int NG, bool WINDOW>
