@@ -100,9 +100,12 @@ DIGEST_SKIP = ("kvec_decode.hip", "kvec_serve_api.hip", "kvec_serve.h", "kvec_at
                "kvec_attn32_dev.h", "kvec_paged_dev.h", "kvec_q8_dev.h", "kvec_paged_decode_q8.hip", "kvec_paged_shared.hip",
                "kvec_paged_read.hip")
 
+# and the part of the C header, from this heading on, that declares the calls of those sources
+DIGEST_HEADER = ("kvec.h", b"The prompt's attention")
+
 
 def source_digest() -> str:
-    """sha256 over the HIP sources and headers the kernels are built from."""
+    """sha256 over the HIP sources and headers the step kernel is built from."""
     import hashlib
     h = hashlib.sha256()
     for d in SOURCE_DIRS:
@@ -110,7 +113,8 @@ def source_digest() -> str:
             if name.endswith((".hip", ".h")) and name not in DIGEST_SKIP:
                 h.update(name.encode())
                 with open(os.path.join(d, name), "rb") as f:
-                    h.update(f.read())
+                    text = f.read()
+                h.update(text.split(DIGEST_HEADER[1])[0] if name == DIGEST_HEADER[0] else text)
     return h.hexdigest()[:16]
 
 
