@@ -602,7 +602,11 @@ size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 }  // namespace
 
 // Two waves of columns with two halves of the slots up to 64 columns, four waves of columns
-// beyond (14 x 4 columns over 16k slots: 29.4 us with two, 34.5 with four).
+// beyond.  us of the whole call with two / four, d 128, no weights: 8 KV heads, 8 columns over 4k
+// slots 12.4 / 15.4, 16k 22.5 / 28.9, 32 over 4k 14.5 / 16.8, 16k 23.3 / 29.6, 64 over 16k 25.2 / 31.3, 80 over 4k
+// 18.7 / 20.2, 96 over 16k 34.2 / 33.2; 4 KV heads over 8k, 28 columns 15.1 / 16.6, 91 19.2 / 21.0.  (Beyond 64
+// columns two is the better one for short prefixes only; up to 32 the second wave of columns has
+// none that is live.)
 //
 // Splits of the prefix: one work-group for every compute unit, of 64 slots at least in
 // float32, of 128 with up to 64 columns and of 192 with more (below, a split's prologue and

@@ -123,6 +123,24 @@ def test_weights_of_far_columns(gpu_lib, b, G, H, P, d, window, size):
     assert torch.all((out.view(b, H, G, d) - want[:, :, None]).abs() <= 2.0 ** -22 * want[:, :, None].abs())
 
 
+@pytest.mark.parametrize("power,kk", FAR + [(35, 1.37), (50, 1.37)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_weights_of_far_own_slots(gpu_lib, d, power, kk):
+    """bf16: own slots' weights come from the logits that the normaliser was made of: the largest
+    one's is 1, exactly, and the others, 2^-4 of it below, have none."""
+    import torch
+    cfg = gpu_lib.PagedConfig(1, 1, 2, d, 16, 4, 3, gpu_lib.KVEC_BF16)
+    q = torch.full((1, 2, d), 1.1 * 2.0 ** power, device="cuda").bfloat16()
+    k = torch.zeros((4, 1, 16, d), device="cuda")
+    k[0, 0, 7], k[1, 0, 3], k[2, 0, 1] = kk * 2.0 ** power * 15 / 16, kk * 2.0 ** power, -kk * 2.0 ** power
+    v = torch.randn(k.shape, generator=torch.Generator().manual_seed(power)).cuda().bfloat16()
+    for P, pages in ((0, [3]), (9, [3])):  # alone, and behind a prefix whose keys are zeros
+        acc = torch.zeros((4, 1, 16), device="cuda")
+        out, _ = _call(gpu_lib, cfg, q, k.bfloat16(), v, pages, P, [[0, 1, 2]], [40], acc)
+        assert acc[1, 0, 3] == 1 and acc.sum() == 1
+        assert torch.all((out - v[1, 0, 3].float()).abs() <= 2.0 ** -22 * v[1, 0, 3].float().abs())
+
+
 def test_weights_of_far_columns_and_others(gpu_lib):
     """Far columns among ordinary ones, padding rows and missing pages: the ordinary ones' weights
     are those of the same batch without the far ones' (bounds of two sums of the same terms)."""
