@@ -15,15 +15,16 @@ def check_attention(k, v, q, out, lse, rows, G, window=0, sinks=0, acc=None, acc
     want_acc, slack = (None, None) if acc is None else (acc0.double().clone(), torch.zeros_like(acc0, dtype=torch.float64))
     for i, where in enumerate(rows):
         o, l = out[i].double().view(H, G, d), lse[i].double().view(H, G)
-        if where is None or len(where[0]) == 0:
+        if where is not None:
+            page, row = (torch.from_numpy(x).long().cuda() for x in where)
+            n = len(page)
+            slot = torch.arange(n, device="cuda")
+            seen = page >= 0
+            if window:
+                seen &= (slot >= n - window) | (slot < sinks)
+        if where is None or not seen.any():
             assert torch.all(o == 0) and torch.all(l == -math.inf), i
             continue
-        page, row = (torch.from_numpy(x).long().cuda() for x in where)
-        n = len(page)
-        slot = torch.arange(n, device="cuda")
-        seen = page >= 0
-        if window:
-            seen &= (slot >= n - window) | (slot < sinks)
         page, row = page[seen], row[seen]
         kk, vv = (x[page, :, row].transpose(0, 1).contiguous() for x in (k, v))  # [H][n][d]
         qq, kt = q[i].double().view(H, G, d), kk.transpose(1, 2).contiguous()
